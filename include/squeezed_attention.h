@@ -1,7 +1,8 @@
 /*
  * squeezed_attention.h -- C ABI of the MI355X (gfx950) implementation of the online path of
  * Squeezed Attention (arxiv 2411.09688): centroid scoring, threshold selection with key-range
- * compaction, sparse flash attention for decode and prefill, and the two-level centroid lookup.
+ * compaction, sparse flash attention for decode and prefill, and the two-level centroid lookup; and
+ * of keys and values in 8 bits: rotation, quantization, a paged user cache, and decode on them.
  *
  * Conventions shared by every entry point
  *   - Every tensor pointer is a DEVICE pointer owned by the caller, contiguous in the stated
@@ -64,7 +65,8 @@ typedef enum sq_call {
     SQ_CALL_CALIBRATE = 15,
     SQ_CALL_HIER_PREFILL_MEAN_STEP = 16,
     SQ_CALL_GQA_MEAN_DECODE_STEP = 17,
-    SQ_CALL_HIER_PREFILL_STEP = 18
+    SQ_CALL_HIER_PREFILL_STEP = 18,
+    SQ_CALL_ATTN_DECODE_Q8 = 19
 } sq_call;
 
 /*
@@ -509,6 +511,120 @@ int sq_cluster_nest(const sq_shape_t *shape, int32_t C1, const int32_t *assign_f
 int sq_calibrate_threshold(const sq_shape_t *shape, const float *logits, const float *row_max, const float *denom,
                            const int32_t *sizes, int64_t target_keys, float *thresh,
                            void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * KEYS AND VALUES IN 8 BITS -- from a projection's rows to a decode step's attention.  Keys and values are held as e4m3
+ * codes (one sign, four exponent, three mantissa bits; largest value 448, no infinity) with ONE scale per head and block
+ * of tokens: 64 keys of the fixed context in their stored order, or one page of the user cache.  A scale written here is
+ * the least power of two 2^e, -64 <= e <= 64, with |x| <= 448 * 2^e for every finite x of the block (2^-64 for a block
+ * of zeros), so that dividing by it is exact and each value is rounded once, to nearest even: by at most 2^-4 of itself,
+ * or 2^-10 of the scale where that is more.  NaN and infinities become the NaN code, and set no scale.
+ * ---------------------------------------------------------------------------------------------------------------- */
+
+/*
+ * Norm and rotation of the heads of a projection.  For a row x[0..d) of one head:
+ *   norm (weight given):  x[i] <- x[i] / sqrt(mean_i x[i]^2 + eps) * weight[i]
+ *   rotation:             pair (i, i + rot_dim/2) of the first rot_dim dimensions, or (2i, 2i + 1) if interleaved != 0:
+ *                         (a, b) <- (a c - b s, b c + a s),  (c, s) = cos_sin[position][i]
+ * Dimensions from rot_dim on are only normed.  rot_dim: a multiple of 8 in [0, d]; 0: no rotation (cos_sin not read).  A
+ * position outside [0, n_positions) is read as the nearest one inside.  eps must be finite and not negative.
+ */
+typedef struct sq_rotary_t {
+    int32_t rot_dim, interleaved, n_positions;
+    float eps;
+    const float *cos_sin;      /* f32 [n_positions, rot_dim/2, 2], cosine then sine */
+    const void *q_weight;      /* f16 [d] or NULL: queries are not normed */
+    const void *k_weight;      /* f16 [d] or NULL: keys are not normed */
+} sq_rotary_t;
+
+/*
+ * A projection's rows to the layouts of the calls above: token t of sequence b is row b * Lq + t of q, k and v, f16, each
+ * row holding its heads one after the other ([heads, d] contiguous, H * G query heads or H K/V heads), rows q_stride,
+ * k_stride and v_stride elements apart (multiples of 8; the parts of one fused projection are three pointers into it).
+ * Queries and keys are normed and rotated (fp32 arithmetic, rounded to f16 once), values are copied.
+ * In:  positions i32 [B, Lq] (may be NULL if rot_dim is 0).
+ * Out: q_out f16 [B,H*G,Lq,d]; k_out, v_out f16 [B,H,Lq,d] -- q of a prefill step, K_user and V_user of one, or the keys and
+ *      values of a context on their way to sq_kmeans_normalize and sq_cluster_layout.
+ * Each of the three pairs may be NULL (both of its pointers).  The outputs must not overlap the inputs or one another.
+ * shape: B, H, Lq, d (L = C = 1, U = 0); 1 <= G <= 64.  No workspace.
+ */
+int sq_head_norm_rotate(const sq_shape_t *shape, int32_t G, const sq_rotary_t *rot, const int32_t *positions,
+                        const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                        void *q_out, void *k_out, void *v_out, void *stream);
+
+/*
+ * Keys and values of a context in 8 bits: K8[b,h,i,:] = codes of K[b,h,perm[b,h,i],:] (perm NULL: of K[b,h,i,:]), with a scale
+ * per 64 consecutive i; likewise V.  perm as written by sq_kmeans_step: given K, V and perm of sq_cluster_layout, this makes
+ * the 8-bit form of K_sorted and V_sorted without them.  A perm entry outside [0, L) is read as the nearest row inside.
+ * In:  K, V f16 [B,H,L,d]; perm i32 [B,H,L] or NULL.  shape: B, H, L, d.
+ * Out: K8, V8 e4m3 [B,H,L,d]; k_scale, v_scale f32 [B,H,ceil(L/64)].  V, V8 and v_scale may be NULL (all three).  The outputs
+ *      must not overlap the inputs or one another.  No workspace.
+ */
+int sq_kv_quantize(const sq_shape_t *shape, const void *K, const void *V, const int32_t *perm, void *K8, void *V8,
+                   float *k_scale, float *v_scale, void *stream);
+
+/*
+ * A paged cache of user / generated keys and values: n_pages pages of page_tokens tokens (16, 32 or 64) and H heads.
+ * Token t of sequence b is slot t % page_tokens of page page_table[b][t / page_tokens].  An entry outside [0, n_pages) is
+ * no page: what is appended there is dropped, and its tokens are not attended to.  n_pages * H * page_tokens must stay
+ * below 2^31.  All device pointers.
+ */
+typedef struct sq_cache_t {
+    int32_t page_tokens, n_pages, max_pages;
+    void *K8, *V8;                 /* e4m3 [n_pages, H, page_tokens, d] */
+    float *k_scale, *v_scale;      /* f32 [n_pages, H] */
+    const int32_t *page_table;     /* i32 [B, max_pages] */
+} sq_cache_t;
+
+/*
+ * Appends the keys and values of new tokens to the cache, keys normed and rotated on the way, and norms and rotates the
+ * tokens' queries: one call per layer and step of a serving loop, for one token of every sequence or for whole prompts.
+ * Rows of q, k and v as in sq_head_norm_rotate, n_tokens of them.  Sequence b appends rows cu_tokens[b] .. cu_tokens[b+1]-1
+ * (i32 [B+1], from 0, non-decreasing, at most n_tokens; possibly none) or, with cu_tokens NULL, its shape->Lq rows
+ * b * Lq .. b * Lq + Lq - 1 (n_tokens must be B * Lq).  seq_len i32 [B] is how many tokens the sequence holds BEFORE the
+ * call; the call does not change it.  Tokens past max_pages * page_tokens are dropped; positions i32 [n_tokens] are the
+ * rotation's (NULL if rot_dim is 0) and need not be cache positions.
+ * A page's first token sets its scales anew, whatever the page held.  A later token may raise them: the codes of the
+ * page's earlier tokens are then multiplied by the old scale over the new one, and rounded again (which is exact for all
+ * but the smallest values, those below 2^-6 of the new scale).  Slots behind the last token keep their codes.  Appending
+ * the same rows again with the same seq_len leaves the cache as it is, so a step can be repeated.
+ * The values that are rounded are those of exact arithmetic on the f16 rows, f32 table and f16 weight, up to the rounding
+ * of double precision.
+ * Out: the cache; q_out f16 [n_tokens, H*G, d] = the normed and rotated queries (for one token per sequence that is
+ *      [B,H*G,1,d]); rows that belong to no sequence are left as they are.  q and q_out may both be NULL.  q_out must not
+ *      overlap q, k or v.
+ * A page that a sequence appends to must stand in no other place of the table that this call appends to.
+ * shape: B, H, Lq (if cu_tokens is NULL), d; 1 <= G <= 64.  No workspace.
+ */
+int sq_cache_append(const sq_shape_t *shape, int32_t G, const sq_rotary_t *rot, const sq_cache_t *cache, int32_t n_tokens,
+                    const int32_t *cu_tokens, const int32_t *seq_len, const int32_t *positions,
+                    const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                    void *q_out, void *stream);
+
+/*
+ * sq_sparse_attn_decode over keys and values in 8 bits: exact softmax attention (fp32 accumulation; the probabilities are
+ * not rounded to 16 bits) of each query over the kept ranges of the fixed context together with the seq_len[b] tokens of
+ * its sequence in the paged cache, one softmax over the union.
+ * Lq of the shape is the number of query heads per K/V head, 1 .. 16 (the shape that scored them: logits [B,H,Lq,C]); query
+ * head h * Lq + g reads K/V head h.
+ * In:  q f16 [B,H*Lq,1,d]; K8, V8 e4m3 [H,L,d], k_scale, v_scale f32 [H,ceil(L/64)] as written by sq_kv_quantize (any finite
+ *      scale will do); with one_set == 0, ranges i32 [B,H*Lq,1,C,2], n_ranges, n_keys i32 [B,H*Lq,1]: every query head's own, as
+ *      written by sq_select; with one_set != 0, ranges [B,H,C,2], n_ranges, n_keys [B,H]: one kept set for the query heads of a
+ *      K/V head, as written by sq_select_mean, and each kept key is read once for them.
+ *      Ranges ascending, disjoint, within [0, L); n_keys = the sum of their counts (it is read, and divides the work).
+ *      Input outside this contract never faults and is not reported: a row uses at most C ranges and L keys, entries with
+ *      count <= 0 are skipped, a key row outside [0, L) is read as the nearest row inside, and where n_keys is not the sum of the
+ *      counts, only as many of the listed keys are used as both allow.
+ *      ranges NULL (then n_ranges, n_keys, K8, V8 and the scales are too): no fixed context.  cache NULL (then seq_len is too): no
+ *      user keys; of its sequences' tokens, the first max_pages * page_tokens are used.  Not both.  U of the shape is not used.
+ * Out: out f16 [B,H*Lq,1,d]; lse f32 [B,H*Lq,1], or NULL.  A query with no visible key gets out = 0 and lse = -inf.
+ *      A NaN code reaches the queries that see its key, and no others.
+ * Workspace: sq_workspace_bytes(shape, SQ_CALL_ATTN_DECODE_Q8), the same for either value of one_set.
+ */
+int sq_sparse_attn_decode_q8(const sq_shape_t *shape, int32_t one_set, const void *q, const void *K8, const void *V8,
+                             const float *k_scale, const float *v_scale, const int32_t *ranges, const int32_t *n_ranges,
+                             const int32_t *n_keys, const sq_cache_t *cache, const int32_t *seq_len, void *out, float *lse,
+                             void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------------------------------------------------
  * MEASUREMENT HOOKS -- sq_profile_begin / sq_profile_end / sq_probe_stream_read.  Not part of the method and not

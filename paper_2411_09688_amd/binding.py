@@ -8,6 +8,7 @@ is no fallback: if the HIP library has not been built, importing it raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -21,14 +22,16 @@ SQ_OK, SQ_ERR_INVALID_ARG, SQ_ERR_UNSUPPORTED, SQ_ERR_WORKSPACE, SQ_ERR_HIP = 0,
 (SQ_CALL_CENTROID_SCORE, SQ_CALL_SELECT, SQ_CALL_ATTN_DECODE, SQ_CALL_ATTN_PREFILL, SQ_CALL_HIER_SELECT,
  SQ_CALL_DECODE_STEP, SQ_CALL_HIER_DECODE_STEP, SQ_CALL_SELECT_MEAN, SQ_CALL_ATTN_PREFILL_SHARED,
  SQ_CALL_PREFILL_STEP, SQ_CALL_PREFILL_MEAN_STEP, SQ_CALL_GQA_DECODE_STEP, SQ_CALL_MULTILEVEL_SELECT,
- SQ_CALL_MULTILEVEL_DECODE_STEP, SQ_CALL_KMEANS_STEP, SQ_CALL_CALIBRATE, SQ_CALL_HIER_PREFILL_MEAN_STEP, SQ_CALL_GQA_MEAN_DECODE_STEP, SQ_CALL_HIER_PREFILL_STEP) = range(19)
+ SQ_CALL_MULTILEVEL_DECODE_STEP, SQ_CALL_KMEANS_STEP, SQ_CALL_CALIBRATE, SQ_CALL_HIER_PREFILL_MEAN_STEP, SQ_CALL_GQA_MEAN_DECODE_STEP, SQ_CALL_HIER_PREFILL_STEP,
+ SQ_CALL_ATTN_DECODE_Q8) = range(20)
 SQ_MAX_LEVELS = 4
 
 EXPORTS = ("sq_workspace_bytes", "sq_last_error", "sq_version", "sq_centroid_score", "sq_select",
            "sq_sparse_attn_decode", "sq_sparse_attn_prefill", "sq_prefill_plan", "sq_prefill_form", "sq_hier_select", "sq_decode_step",
            "sq_hier_decode_step", "sq_decode_step_noalloc", "sq_select_mean", "sq_sparse_attn_prefill_shared", "sq_prefill_step",
            "sq_prefill_mean_step", "sq_gqa_decode_step", "sq_multilevel_select", "sq_multilevel_decode_step",
-           "sq_kmeans_normalize", "sq_kmeans_step", "sq_cluster_layout", "sq_cluster_nest", "sq_calibrate_threshold", "sq_hier_prefill_mean_step", "sq_hier_prefill_step", "sq_gqa_mean_decode_step", "sq_profile_begin",
+           "sq_kmeans_normalize", "sq_kmeans_step", "sq_cluster_layout", "sq_cluster_nest", "sq_calibrate_threshold", "sq_hier_prefill_mean_step", "sq_hier_prefill_step", "sq_gqa_mean_decode_step", "sq_head_norm_rotate", "sq_kv_quantize",
+           "sq_cache_append", "sq_sparse_attn_decode_q8", "sq_profile_begin",
            "sq_profile_end", "sq_probe_stream_read")
 
 
@@ -40,6 +43,16 @@ class SqShape(C.Structure):
 class SqLevel(C.Structure):
     _fields_ = [("C", C.c_int32), ("centroids", C.c_void_p), ("sizes", C.c_void_p), ("child_offsets", C.c_void_p),
                 ("thresh", C.c_void_p)]
+
+
+class SqRotary(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_positions", C.c_int32), ("eps", C.c_float),
+                ("cos_sin", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
+
+
+class SqCache(C.Structure):
+    _fields_ = [("page_tokens", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("K8", C.c_void_p),
+                ("V8", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("page_table", C.c_void_p)]
 
 
 class SqError(RuntimeError):
@@ -91,6 +104,11 @@ def lib() -> C.CDLL:
         L.sq_cluster_layout.argtypes = [sp] + [vp] * 8 + [vp]
         L.sq_cluster_nest.argtypes = [sp, C.c_int32] + [vp] * 8 + [vp, sz, vp]
         L.sq_calibrate_threshold.argtypes = [sp] + [vp] * 4 + [C.c_int64, vp] + [vp, sz, vp]
+        rp, ap, i32, i64 = C.POINTER(SqRotary), C.POINTER(SqCache), C.c_int32, C.c_int64
+        L.sq_head_norm_rotate.argtypes = [sp, i32, rp, vp] + [vp, i64] * 3 + [vp] * 4
+        L.sq_kv_quantize.argtypes = [sp] + [vp] * 8
+        L.sq_cache_append.argtypes = [sp, i32, rp, ap, i32] + [vp] * 3 + [vp, i64] * 3 + [vp] * 2
+        L.sq_sparse_attn_decode_q8.argtypes = [sp, i32] + [vp] * 8 + [ap] + [vp] * 4 + [sz, vp]
         L.sq_probe_stream_read.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p, C.c_int, C.c_void_p]
         L.sq_profile_begin.argtypes = [C.c_int]
         L.sq_profile_end.argtypes = [C.POINTER(C.c_float)] * 3
@@ -401,6 +419,143 @@ def sq_hier_prefill_mean_step(shape, C1, q, centroids1, sizes1, child_offsets, t
     """One kept set per (sequence, head): keep_mask2 [B,H,W], n_keys [B,H]."""
     _hier_prefill(lib().sq_hier_prefill_mean_step, shape, C1, q, centroids1, sizes1, child_offsets, thresh1, centroids2,
                   sizes2, offsets2, thresh2, K_fixed, V_fixed, K_user, V_user, out, lse, keep_mask2, n_keys, ws, stream)
+
+
+# ------------------------------------------------------------------------------------------------
+# Keys and values in 8 bits.  These calls take tensors of the current device (and of the stream's) only, with the shapes
+# that the header gives them.
+# ------------------------------------------------------------------------------------------------
+F8 = torch.float8_e4m3fn
+HEAD_DIM = 128
+
+
+def _here(t: Optional[torch.Tensor], shape, dtype, name, device):
+    """The pointer of a contiguous tensor of this shape, type and device."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on the current device {device}, is on {t.device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.numel() != math.prod(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous and hold {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _head_rows(t: Optional[torch.Tensor], n, heads, name, device):
+    """(pointer, elements from row to row) of f16 [n, heads, 128] whose rows may be apart (a part of a fused projection)."""
+    if t is None:
+        return None, 0
+    if t.get_device() != device or t.dtype != F16:
+        raise ValueError(f"{name} must be {F16} on the current device {device}, is {t.dtype} on {t.device}")
+    if t.shape != (n, heads, HEAD_DIM) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != HEAD_DIM):
+        raise ValueError(f"{name} must be [{n}, {heads}, {HEAD_DIM}] with contiguous rows, got {tuple(t.shape)}, strides {t.stride()}")
+    return t.data_ptr(), t.stride(0) if n > 1 else heads * HEAD_DIM
+
+
+class Rotary:
+    """The norms and the rotation of a layer's heads (sq_rotary_t) with the tensors that it points at."""
+
+    def __init__(self, cos_sin, rot_dim, interleaved, q_weight, k_weight, eps):
+        self.tensors = (cos_sin, q_weight, k_weight)
+        device = next((t.get_device() for t in self.tensors if t is not None), None)
+        self.device = device
+        for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            _here(w, (HEAD_DIM,), F16, name, device)
+        if cos_sin is not None:
+            _here(cos_sin, (cos_sin.shape[0], rot_dim // 2, 2), F32, "cos_sin", device)
+        self.c = SqRotary(rot_dim, int(bool(interleaved)), cos_sin.shape[0] if cos_sin is not None else 0, float(eps),
+                          _ptr(cos_sin), _ptr(q_weight), _ptr(k_weight))
+        self.ref = C.byref(self.c)
+
+
+def make_rotary(cos_sin, interleaved=False, q_weight=None, k_weight=None, eps=1e-6) -> Rotary:
+    """cos_sin f32 [n_positions, rot_dim / 2, 2], or None: no rotation; a weight f16 [128], or None: no norm."""
+    return Rotary(cos_sin, 0 if cos_sin is None else 2 * cos_sin.shape[1], interleaved, q_weight, k_weight, eps)
+
+
+class Cache:
+    """A paged 8-bit cache (sq_cache_t) with its tensors."""
+
+    def __init__(self, K8, V8, k_scale, v_scale, page_table):
+        n, H, P, d = K8.shape
+        self.device, self.heads, self.sequences = K8.get_device(), H, page_table.shape[0]
+        self.tensors = (K8, V8, k_scale, v_scale, page_table)
+        p = [_here(t, s, ty, name, self.device) for t, s, ty, name in
+             ((K8, (n, H, P, HEAD_DIM), F8, "K8"), (V8, (n, H, P, HEAD_DIM), F8, "V8"), (k_scale, (n, H), F32, "k_scale"),
+              (v_scale, (n, H), F32, "v_scale"), (page_table, tuple(page_table.shape), I32, "page_table"))]
+        self.c = SqCache(P, n, page_table.shape[1], *p)
+        self.ref = C.byref(self.c)
+
+
+def make_cache(K8, V8, k_scale, v_scale, page_table) -> Cache:
+    """K8, V8 float8_e4m3fn [n_pages, H, page_tokens, 128], scales f32 [n_pages, H], page_table i32 [B, max_pages]."""
+    return Cache(K8, V8, k_scale, v_scale, page_table)
+
+
+def _device_of(stream, *held):
+    """The current device, which has to be the stream's and that of what the call was prepared with."""
+    device = torch.cuda.current_device()
+    if stream is not None and stream.device_index != device:
+        raise ValueError(f"the stream belongs to device {stream.device_index}, the current device is {device}")
+    for h in held:
+        if h is not None and h.device is not None and h.device != device:
+            raise ValueError(f"{type(h).__name__} holds tensors of device {h.device}, the current device is {device}")
+    return device
+
+
+def _for_sequences(cache, shape):
+    if cache is not None and (cache.heads != shape.H or cache.sequences != shape.B):
+        raise ValueError(f"the cache has {cache.heads} heads and pages of {cache.sequences} sequences, the shape {shape.H} and {shape.B}")
+
+
+def sq_head_norm_rotate(shape, G, rot, positions, q, k, v, q_out, k_out, v_out, stream=None):
+    """q [B*Lq, H*G, 128], k, v [B*Lq, H, 128] (rows may be apart) -> q_out [B,H*G,Lq,128], k_out, v_out [B,H,Lq,128]."""
+    dev = _device_of(stream, rot)
+    n, H = shape.B * shape.Lq, shape.H
+    _check(lib().sq_head_norm_rotate(
+        C.byref(shape), int(G), rot.ref, _here(positions, (n,), I32, "positions", dev), *_head_rows(q, n, H * G, "q", dev),
+        *_head_rows(k, n, H, "k", dev), *_head_rows(v, n, H, "v", dev), _here(q_out, (n, H * G, HEAD_DIM), F16, "q_out", dev),
+        _here(k_out, (n, H, HEAD_DIM), F16, "k_out", dev), _here(v_out, (n, H, HEAD_DIM), F16, "v_out", dev), _stream(stream)))
+
+
+def sq_kv_quantize(shape, K, V, perm, K8, V8, k_scale, v_scale, stream=None):
+    dev = _device_of(stream)
+    rows, scales = (shape.B, shape.H, shape.L, HEAD_DIM), (shape.B, shape.H, (shape.L + 63) // 64)
+    _check(lib().sq_kv_quantize(
+        C.byref(shape), _here(K, rows, F16, "K", dev), _here(V, rows, F16, "V", dev), _here(perm, rows[:3], I32, "perm", dev),
+        _here(K8, rows, F8, "K8", dev), _here(V8, rows, F8, "V8", dev), _here(k_scale, scales, F32, "k_scale", dev),
+        _here(v_scale, scales, F32, "v_scale", dev), _stream(stream)))
+
+
+def sq_cache_append(shape, G, rot, cache, seq_len, positions, q, k, v, q_out, cu_tokens=None, stream=None):
+    """k, v [n_tokens, H, 128], q [n_tokens, H*G, 128] or None (rows may be apart); cu_tokens None: Lq rows per sequence."""
+    dev = _device_of(stream, rot, cache)
+    _for_sequences(cache, shape)
+    n, H = k.shape[0], shape.H
+    _check(lib().sq_cache_append(
+        C.byref(shape), int(G), rot.ref, cache.ref, n, _here(cu_tokens, (shape.B + 1,), I32, "cu_tokens", dev),
+        _here(seq_len, (shape.B,), I32, "seq_len", dev), _here(positions, (n,), I32, "positions", dev),
+        *_head_rows(q, n, H * G, "q", dev), *_head_rows(k, n, H, "k", dev), *_head_rows(v, n, H, "v", dev),
+        _here(q_out, (n, H * G, HEAD_DIM), F16, "q_out", dev), _stream(stream)))
+
+
+def sq_sparse_attn_decode_q8(shape, one_set, q, K8, V8, k_scale, v_scale, ranges, n_ranges, n_keys, cache, seq_len, out, lse, ws,
+                             stream=None):
+    """Lq of the shape: query heads per K/V head.  The seven tensors of the fixed context may be None, or cache and seq_len."""
+    dev = _device_of(stream, cache)
+    _for_sequences(cache, shape)
+    B, H, L, Lq = shape.B, shape.H, shape.L, shape.Lq
+    rows = B * H * (1 if one_set else Lq)
+    codes, scales = (H, L, HEAD_DIM), (H, (L + 63) // 64)
+    if ws is not None and ws.get_device() != dev:
+        raise ValueError(f"the workspace must be on the current device {dev}, is on {ws.device}")
+    _check(lib().sq_sparse_attn_decode_q8(
+        C.byref(shape), int(bool(one_set)), _here(q, (B, H * Lq, HEAD_DIM), F16, "q", dev), _here(K8, codes, F8, "K8", dev),
+        _here(V8, codes, F8, "V8", dev), _here(k_scale, scales, F32, "k_scale", dev), _here(v_scale, scales, F32, "v_scale", dev),
+        _here(ranges, (rows, shape.C, 2), I32, "ranges", dev), _here(n_ranges, (rows,), I32, "n_ranges", dev),
+        _here(n_keys, (rows,), I32, "n_keys", dev), None if cache is None else cache.ref, _here(seq_len, (B,), I32, "seq_len", dev),
+        _here(out, (B, H * Lq, HEAD_DIM), F16, "out", dev), _here(lse, (B, H * Lq), F32, "lse", dev), *_ws_args(ws), _stream(stream)))
 
 
 def sq_probe_stream_read(buf: torch.Tensor, sink: torch.Tensor, workgroups: int, nbytes: Optional[int] = None,

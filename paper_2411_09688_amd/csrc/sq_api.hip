@@ -8,6 +8,7 @@
 
 #include "../../include/squeezed_attention.h"
 #include "sq_common.hpp"
+#include "sq_head_row.hpp"
 #include "sq_internal.hpp"
 
 namespace {
@@ -339,6 +340,22 @@ HierWs carve_hier(Carver &cv, const sq_shape_t *sh)
     return w;
 }
 
+// Decode attention on 8-bit keys and values: partial results of the shares and which of them are a row's, for either kind of row
+// (B * H rows of Lq queries need the more partial results, B * H * Lq rows the longer table).
+struct DecodeQ8Ws {
+    float *part;
+    int2 *info;
+};
+
+DecodeQ8Ws carve_decode_q8(Carver &cv, const sq_shape_t *sh)
+{
+    const size_t bh = (size_t)sh->B * sh->H;
+    DecodeQ8Ws w{};
+    w.part = cv.take<float>((sq::Q8_GRID + bh) * sh->Lq * sq::PART_STRIDE);
+    w.info = cv.take<int2>(bh * sh->Lq);
+    return w;
+}
+
 // Second candidate work list, for lookups of more than two levels.
 sq::DecodePlan carve_cand_plan(Carver &cv, const sq_shape_t *sh)
 {
@@ -639,6 +656,9 @@ size_t sq_workspace_bytes(const sq_shape_t *sh, int which)
         return cv.off;
     case SQ_CALL_HIER_DECODE_STEP:
         carve_hier_step(cv, sh);
+        return cv.off;
+    case SQ_CALL_ATTN_DECODE_Q8:
+        carve_decode_q8(cv, sh);
         return cv.off;
     default:
         return 0;
@@ -1613,6 +1633,304 @@ int sq_calibrate_threshold(const sq_shape_t *sh, const float *logits, const floa
     const long long cap = (long long)sh->B * sh->Lq * sh->L;
     SQ_HIP(sq::launch_calibrate(logits, row_max, denom, sizes, S, thresh, (int)(target_keys < cap ? target_keys : cap),
                                 sh->B, sh->H, sh->Lq, sh->C, static_cast<hipStream_t>(stream)));
+    g_err[0] = 0;
+    return SQ_OK;
+}
+
+namespace {
+
+// Extents of the tensors of the calls on 8-bit keys and values, for the checks that outputs overlap nothing.
+struct Extent {
+    const char *name;
+    const void *p;
+    size_t bytes;
+    bool written;
+};
+
+int check_overlap(const char *fn, const Extent *x, int n)
+{
+    for (int i = 0; i < n; ++i)
+        for (int j = 0; x[i].p && x[i].written && j < n; ++j) {
+            if (j == i || !x[j].p || (x[j].written && j < i)) continue;
+            const char *a = static_cast<const char *>(x[i].p), *b = static_cast<const char *>(x[j].p);
+            if (a < b + x[j].bytes && b < a + x[i].bytes)
+                return fail(SQ_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, x[i].name, x[j].name);
+        }
+    return SQ_OK;
+}
+
+// Bytes of `rows` rows of `heads` heads, `stride` elements apart.
+size_t row_bytes(long long rows, int64_t stride, int heads)
+{
+    return rows > 0 ? ((size_t)(rows - 1) * (size_t)stride + (size_t)heads * sq::D) * 2 : 0;
+}
+
+int check_rotary(const char *fn, const sq_rotary_t *rot, const int32_t *positions, sq::RotaryArgs *ra)
+{
+    if (!rot) return fail(SQ_ERR_INVALID_ARG, "%s: rot is NULL", fn);
+    if (rot->rot_dim < 0 || rot->rot_dim > sq::D || rot->rot_dim % 8)
+        return fail(SQ_ERR_INVALID_ARG, "%s: rot_dim = %d must be a multiple of 8 in [0, %d]", fn, rot->rot_dim, sq::D);
+    if (!(rot->eps >= 0.0f) || rot->eps > 3.4e38f) return fail(SQ_ERR_INVALID_ARG, "%s: eps must be finite and not negative", fn);
+    if (rot->rot_dim > 0) {
+        if (rot->n_positions <= 0) return fail(SQ_ERR_INVALID_ARG, "%s: n_positions = %d must be positive", fn, rot->n_positions);
+        if (!rot->cos_sin || !aligned16(rot->cos_sin)) return fail(SQ_ERR_INVALID_ARG, "%s: cos_sin is NULL or not 16-byte aligned", fn);
+        if (!positions || !aligned16(positions)) return fail(SQ_ERR_INVALID_ARG, "%s: positions is NULL or not 16-byte aligned", fn);
+    }
+    if (!aligned16(rot->q_weight) || !aligned16(rot->k_weight))
+        return fail(SQ_ERR_INVALID_ARG, "%s: a norm's weight is not 16-byte aligned", fn);
+    ra->cos_sin = rot->cos_sin;
+    ra->weight[0] = static_cast<const _Float16 *>(rot->q_weight);
+    ra->weight[1] = static_cast<const _Float16 *>(rot->k_weight);
+    ra->rot_dim = rot->rot_dim;
+    ra->adjacent = rot->interleaved != 0;
+    ra->n_positions = rot->n_positions;
+    ra->eps = rot->eps;
+    return SQ_OK;
+}
+
+int check_rows(const char *fn, const char *name, const void *p, int64_t stride, int heads)
+{
+    if (!p || !aligned16(p)) return fail(SQ_ERR_INVALID_ARG, "%s: %s is NULL or not 16-byte aligned", fn, name);
+    if (stride < (int64_t)heads * sq::D || stride % 8 || stride > (1ll << 31))
+        return fail(SQ_ERR_INVALID_ARG, "%s: %s's stride of %lld elements must be a multiple of 8 and hold %d heads", fn, name,
+                    (long long)stride, heads);
+    return SQ_OK;
+}
+
+int check_group(const char *fn, const sq_shape_t *sh, int G, long long tokens)
+{
+    if (G < 1 || G > 64) return fail(SQ_ERR_INVALID_ARG, "%s: G = %d must be in [1, 64]", fn, G);
+    if (tokens * sh->H * (G + 2) > 0x7fffffffll) return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", fn);
+    return SQ_OK;
+}
+
+int check_cache(const char *fn, const sq_shape_t *sh, const sq_cache_t *c, const int32_t *seq_len)
+{
+    if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64)
+        return fail(SQ_ERR_INVALID_ARG, "%s: page_tokens = %d must be 16, 32 or 64", fn, c->page_tokens);
+    if (c->n_pages <= 0 || c->max_pages <= 0)
+        return fail(SQ_ERR_INVALID_ARG, "%s: n_pages = %d and max_pages = %d must be positive", fn, c->n_pages, c->max_pages);
+    if ((long long)c->n_pages * sh->H > 0x7fffffffll / c->page_tokens || (long long)c->max_pages * c->page_tokens > sq::MAX_L)
+        return fail(SQ_ERR_UNSUPPORTED, "%s: cache too large", fn);
+    const void *const p[] = {c->K8, c->V8, c->k_scale, c->v_scale, c->page_table, seq_len};
+    const char *const name[] = {"K8", "V8", "k_scale", "v_scale", "page_table", "seq_len"};
+    for (int i = 0; i < 6; ++i)
+        if (!p[i] || !aligned16(p[i])) return fail(SQ_ERR_INVALID_ARG, "%s: the cache's %s is NULL or not 16-byte aligned", fn, name[i]);
+    return SQ_OK;
+}
+
+}  // namespace
+
+int sq_head_norm_rotate(const sq_shape_t *sh, int32_t G, const sq_rotary_t *rot, const int32_t *positions, const void *q,
+                        int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *q_out,
+                        void *k_out, void *v_out, void *stream)
+{
+    if (int rc = check_shape(sh, __func__, false)) return rc;
+    const long long tokens = (long long)sh->B * sh->Lq;
+    if (int rc = check_group(__func__, sh, G, tokens)) return rc;
+    sq::RotaryArgs ra;
+    if (int rc = check_rotary(__func__, rot, positions, &ra)) return rc;
+    const void *const src[] = {q, k, v};
+    void *const dst[] = {q_out, k_out, v_out};
+    const int64_t stride[] = {q_stride, k_stride, v_stride};
+    const char *const name[] = {"q", "k", "v"}, *const out[] = {"q_out", "k_out", "v_out"};
+    sq::HeadRows hr{};
+    Extent x[6];
+    for (int i = 0; i < 3; ++i) {
+        const int heads = i == 0 ? sh->H * G : sh->H;
+        if (!src[i] != !dst[i])
+            return fail(SQ_ERR_INVALID_ARG, "%s: %s and %s go together", __func__, name[i], out[i]);
+        if (src[i]) {
+            if (int rc = check_rows(__func__, name[i], src[i], stride[i], heads)) return rc;
+            if (!aligned16(dst[i])) return fail(SQ_ERR_INVALID_ARG, "%s: %s is not 16-byte aligned", __func__, out[i]);
+        }
+        hr.src[i] = static_cast<const _Float16 *>(src[i]);
+        hr.dst[i] = static_cast<_Float16 *>(dst[i]);
+        hr.stride[i] = stride[i];
+        hr.n[i] = src[i] ? heads : 0;
+        x[i] = Extent{name[i], src[i], row_bytes(tokens, stride[i], heads), false};
+        x[3 + i] = Extent{out[i], dst[i], (size_t)tokens * heads * sq::D * 2, true};
+    }
+    if (!q && !k && !v) return fail(SQ_ERR_INVALID_ARG, "%s: q, k and v are all NULL", __func__);
+    if (int rc = check_overlap(__func__, x, 6)) return rc;
+    if (int rc = check_device(__func__)) return rc;
+    hr.Lq = sh->Lq;
+    hr.positions = positions;
+    SQ_HIP(sq::launch_head_rows(hr, ra, (int)tokens, static_cast<hipStream_t>(stream)));
+    g_err[0] = 0;
+    return SQ_OK;
+}
+
+int sq_kv_quantize(const sq_shape_t *sh, const void *K, const void *V, const int32_t *perm, void *K8, void *V8, float *k_scale,
+                   float *v_scale, void *stream)
+{
+    if (int rc = check_shape(sh, __func__, false)) return rc;
+    SQ_REQUIRE_PTR(K);
+    SQ_OPTIONAL_PTR(V);
+    SQ_OPTIONAL_PTR(perm);
+    SQ_REQUIRE_PTR(K8);
+    SQ_OPTIONAL_PTR(V8);
+    SQ_REQUIRE_PTR(k_scale);
+    SQ_OPTIONAL_PTR(v_scale);
+    if (!V != !V8 || !V != !v_scale) return fail(SQ_ERR_INVALID_ARG, "%s: V, V8 and v_scale go together", __func__);
+    const size_t bh = (size_t)sh->B * sh->H, rows = bh * sh->L, blocks = (sh->L + sq::KV_BLOCK - 1) / sq::KV_BLOCK;
+    if (bh * blocks * 2 > 0x7fffffff) return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", __func__);
+    const Extent x[] = {{"K", K, rows * sq::D * 2, false},        {"V", V, rows * sq::D * 2, false},
+                        {"perm", perm, rows * 4, false},          {"K8", K8, rows * sq::D, true},
+                        {"V8", V8, rows * sq::D, true},           {"k_scale", k_scale, bh * blocks * 4, true},
+                        {"v_scale", v_scale, bh * blocks * 4, true}};
+    if (int rc = check_overlap(__func__, x, 7)) return rc;
+    if (int rc = check_device(__func__)) return rc;
+    sq::QuantizeArgs a{};
+    a.X[0] = static_cast<const _Float16 *>(K);
+    a.X[1] = static_cast<const _Float16 *>(V);
+    a.codes[0] = static_cast<uint8_t *>(K8);
+    a.codes[1] = static_cast<uint8_t *>(V8);
+    a.scale[0] = k_scale;
+    a.scale[1] = v_scale;
+    a.perm = perm;
+    a.L = sh->L;
+    a.blocks = (int)blocks;
+    a.tensors = V ? 2 : 1;
+    SQ_HIP(sq::launch_kv_quantize(a, (int)bh, static_cast<hipStream_t>(stream)));
+    g_err[0] = 0;
+    return SQ_OK;
+}
+
+int sq_cache_append(const sq_shape_t *sh, int32_t G, const sq_rotary_t *rot, const sq_cache_t *cache, int32_t n_tokens,
+                    const int32_t *cu_tokens, const int32_t *seq_len, const int32_t *positions, const void *q, int64_t q_stride,
+                    const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *q_out, void *stream)
+{
+    if (int rc = check_shape(sh, __func__, false)) return rc;
+    if (!cache) return fail(SQ_ERR_INVALID_ARG, "%s: cache is NULL", __func__);
+    if (int rc = check_cache(__func__, sh, cache, seq_len)) return rc;
+    if (n_tokens < 0) return fail(SQ_ERR_INVALID_ARG, "%s: n_tokens = %d is negative", __func__, n_tokens);
+    if (!cu_tokens && n_tokens != (long long)sh->B * sh->Lq)
+        return fail(SQ_ERR_INVALID_ARG, "%s: without cu_tokens n_tokens = %d must be B * Lq = %lld", __func__, n_tokens,
+                    (long long)sh->B * sh->Lq);
+    SQ_OPTIONAL_PTR(cu_tokens);
+    if (int rc = check_group(__func__, sh, G, n_tokens)) return rc;
+    sq::RotaryArgs ra;
+    if (n_tokens == 0) {
+        g_err[0] = 0;
+        return SQ_OK;
+    }
+    if (int rc = check_rotary(__func__, rot, positions, &ra)) return rc;
+    if (int rc = check_rows(__func__, "k", k, k_stride, sh->H)) return rc;
+    if (int rc = check_rows(__func__, "v", v, v_stride, sh->H)) return rc;
+    if (!q != !q_out) return fail(SQ_ERR_INVALID_ARG, "%s: q and q_out go together", __func__);
+    const int Hq = sh->H * G;
+    if (q) {
+        if (int rc = check_rows(__func__, "q", q, q_stride, Hq)) return rc;
+        if (!aligned16(q_out)) return fail(SQ_ERR_INVALID_ARG, "%s: q_out is not 16-byte aligned", __func__);
+    }
+    const size_t heads = (size_t)cache->n_pages * sh->H, codes = heads * cache->page_tokens * sq::D;
+    const Extent x[] = {{"q", q, row_bytes(n_tokens, q_stride, Hq), false},
+                        {"k", k, row_bytes(n_tokens, k_stride, sh->H), false},
+                        {"v", v, row_bytes(n_tokens, v_stride, sh->H), false},
+                        {"q_out", q_out, (size_t)n_tokens * Hq * sq::D * 2, true},
+                        {"K8", cache->K8, codes, true},
+                        {"V8", cache->V8, codes, true},
+                        {"k_scale", cache->k_scale, heads * 4, true},
+                        {"v_scale", cache->v_scale, heads * 4, true}};
+    if (int rc = check_overlap(__func__, x, 8)) return rc;
+    if (int rc = check_device(__func__)) return rc;
+    sq::AppendArgs a{};
+    a.q = static_cast<const _Float16 *>(q);
+    a.k = static_cast<const _Float16 *>(k);
+    a.v = static_cast<const _Float16 *>(v);
+    a.q_out = static_cast<_Float16 *>(q_out);
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.K8 = static_cast<uint8_t *>(cache->K8);
+    a.V8 = static_cast<uint8_t *>(cache->V8);
+    a.k_scale = cache->k_scale;
+    a.v_scale = cache->v_scale;
+    a.page_table = cache->page_table;
+    a.cu = cu_tokens;
+    a.seq_len = seq_len;
+    a.positions = positions;
+    a.B = sh->B;
+    a.H = sh->H;
+    a.Hq = Hq;
+    a.Lq = sh->Lq;
+    a.n_tokens = n_tokens;
+    a.P = cache->page_tokens;
+    a.n_pages = cache->n_pages;
+    a.max_pages = cache->max_pages;
+    SQ_HIP(sq::launch_cache_append(a, ra, static_cast<hipStream_t>(stream)));
+    g_err[0] = 0;
+    return SQ_OK;
+}
+
+int sq_sparse_attn_decode_q8(const sq_shape_t *sh, int32_t one_set, const void *q, const void *K8, const void *V8,
+                             const float *k_scale, const float *v_scale, const int32_t *ranges, const int32_t *n_ranges,
+                             const int32_t *n_keys, const sq_cache_t *cache, const int32_t *seq_len, void *out, float *lse, void *ws,
+                             size_t ws_bytes, void *stream)
+{
+    if (int rc = check_shape(sh, __func__, false)) return rc;
+    if (sh->Lq > sq::SG)
+        return fail(SQ_ERR_UNSUPPORTED, "%s: Lq = %d query heads per K/V head, at most %d are supported", __func__, sh->Lq, sq::SG);
+    SQ_REQUIRE_PTR(q);
+    SQ_REQUIRE_PTR(out);
+    SQ_OPTIONAL_PTR(lse);
+    if (!ranges && !cache) return fail(SQ_ERR_INVALID_ARG, "%s: neither ranges of a fixed context nor a cache", __func__);
+    if (ranges) {
+        SQ_REQUIRE_PTR(ranges);
+        SQ_REQUIRE_PTR(n_ranges);
+        SQ_REQUIRE_PTR(n_keys);
+        SQ_REQUIRE_PTR(K8);
+        SQ_REQUIRE_PTR(V8);
+        SQ_REQUIRE_PTR(k_scale);
+        SQ_REQUIRE_PTR(v_scale);
+    } else if (n_ranges || n_keys || K8 || V8 || k_scale || v_scale) {
+        return fail(SQ_ERR_INVALID_ARG, "%s: a fixed context without ranges", __func__);
+    }
+    if (!cache && seq_len) return fail(SQ_ERR_INVALID_ARG, "%s: seq_len without a cache", __func__);
+    if (cache)
+        if (int rc = check_cache(__func__, sh, cache, seq_len)) return rc;
+    const long long rows = (long long)sh->B * sh->H * sh->Lq;
+    const long long keys = (ranges ? sh->L : 0) + (cache ? (long long)cache->max_pages * cache->page_tokens : 0);
+    if ((long long)sh->H * sh->L > 0x7fffffffll || rows > (1 << 24) || rows * (keys / 32 + 2) > 0x7fffffffll)
+        return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", __func__);
+    if (int rc = check_ws(__func__, sh, SQ_CALL_ATTN_DECODE_Q8, ws, ws_bytes)) return rc;
+    if (int rc = check_device(__func__)) return rc;
+    Carver cv(ws);
+    const DecodeQ8Ws w = carve_decode_q8(cv, sh);
+    sq::DecodeQ8Args a{};
+    a.q = static_cast<const _Float16 *>(q);
+    a.K8 = static_cast<const uint8_t *>(K8);
+    a.V8 = static_cast<const uint8_t *>(V8);
+    a.ks = k_scale;
+    a.vs = v_scale;
+    a.ranges = ranges;
+    a.n_ranges = n_ranges;
+    a.n_keys = n_keys;
+    if (cache) {
+        a.cK = static_cast<const uint8_t *>(cache->K8);
+        a.cV = static_cast<const uint8_t *>(cache->V8);
+        a.cks = cache->k_scale;
+        a.cvs = cache->v_scale;
+        a.page_table = cache->page_table;
+        a.seq_len = seq_len;
+        a.P = cache->page_tokens;
+        a.n_pages = cache->n_pages;
+        a.max_pages = cache->max_pages;
+    }
+    a.out = static_cast<_Float16 *>(out);
+    a.lse = lse;
+    a.part = w.part;
+    a.info = w.info;
+    a.B = sh->B;
+    a.H = sh->H;
+    a.L = sh->L;
+    a.C = sh->C;
+    a.sblocks = (sh->L + sq::KV_BLOCK - 1) / sq::KV_BLOCK;
+    a.per = one_set ? 1 : sh->Lq;
+    a.g = one_set ? sh->Lq : 1;
+    a.scale = sh->sm_scale * 1.44269504088896341f;
+    SQ_HIP(sq::launch_decode_q8(a, static_cast<hipStream_t>(stream)));
     g_err[0] = 0;
     return SQ_OK;
 }

@@ -347,6 +347,59 @@ hipError_t launch_decode_attn_index(const void *q, const void *Kf, const void *V
                                     void *out, float *lse, int rows, int H, int G, float sm_scale, const UserAttn *user,
                                     hipStream_t s);
 
+// Keys and values in 8 bits (sq_head_rows.hip, sq_quantize.hip, sq_cache.hip, sq_decode_q8.hip).
+struct RotaryArgs;
+struct HeadRows {                  // queries, keys, values; n: heads (0: not given)
+    const _Float16 *src[3];
+    _Float16 *dst[3];
+    long long stride[3];
+    int n[3];
+    int Lq;
+    const int32_t *positions;
+};
+hipError_t launch_head_rows(const HeadRows &hr, const RotaryArgs &ra, int tokens, hipStream_t s);
+
+struct QuantizeArgs {              // keys, values (tensors: 1 or 2 of them)
+    const _Float16 *X[2];
+    uint8_t *codes[2];
+    float *scale[2];
+    const int32_t *perm;
+    int L, blocks, tensors;
+};
+hipError_t launch_kv_quantize(const QuantizeArgs &a, int heads, hipStream_t s);
+
+struct AppendArgs {
+    const _Float16 *q, *k, *v;
+    _Float16 *q_out;
+    long long q_stride, k_stride, v_stride;
+    uint8_t *K8, *V8;
+    float *k_scale, *v_scale;
+    const int32_t *page_table, *cu, *seq_len, *positions;
+    int B, H, Hq, Lq, n_tokens, P, n_pages, max_pages;
+    int per_seq, kv_blocks;        // (the launcher's)
+};
+hipError_t launch_cache_append(AppendArgs a, const RotaryArgs &ra, hipStream_t s);
+
+constexpr int Q8_GRID = 512;       // workgroups that share the keys of a call
+struct DecodeQ8Args {
+    const _Float16 *q;
+    const uint8_t *K8, *V8;
+    const float *ks, *vs;
+    const int32_t *ranges, *n_ranges, *n_keys;
+    const uint8_t *cK, *cV;
+    const float *cks, *cvs;
+    const int32_t *page_table, *seq_len;
+    _Float16 *out;
+    float *lse;
+    float *part;                   // [Q8_GRID + rows][g][PART_STRIDE]
+    int2 *info;                    // per row: first partial result, how many (0: the row is done)
+    int B, H, L, C, sblocks;
+    int per, g;                    // rows per (sequence, K/V head), query heads per row
+    int P, n_pages, max_pages;
+    float scale;                   // sm_scale * log2(e)
+};
+hipError_t launch_decode_q8(const DecodeQ8Args &a, hipStream_t s);
+
 // Records the calling thread's error message (what sq_last_error returns) and hands back `code`.
 int set_error(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 

@@ -33,6 +33,10 @@ struct KeyList {                             // the rows (of 128 codes) of a chu
     uint32_t row[QLIST];
     float ks[QLIST], vs[QLIST];
 };
+struct Tile {                                // what a lane reads of 32 keys
+    u4v k[2][2];                             // keys c16 and 16 + c16, dimensions 32 g4 ..
+    u2v v[8];                                // keys 4 g4 .. and 16 + 4 g4 .., dimensions 8 c16 ..
+};
 struct WaveOut {                             // the four waves' results of a row
     float o[4][16][O_STRIDE];
 };
@@ -91,9 +95,25 @@ __device__ __forceinline__ b8 codes_bf16(uint32_t lo, uint32_t hi)
     return b8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// Dimension d of a query's result: l is zero where it sees no key, and NaN where it sees one.
+__device__ __forceinline__ void store_result(const DecodeQ8Args &a, size_t query, int d, float m, float l, float o)
+{
+    const bool any = l > 0.0f || l != l;
+    a.out[query * D + d] = (_Float16)(any ? o / l : 0.0f);
+    if (d == 0 && a.lse) a.lse[query] = any ? (m + log2f(l)) * 0.69314718055994531f : SQ_NEG_INF;
+}
+
 }  // namespace
 
-__global__ __launch_bounds__(256) void decode_q8_kernel(DecodeQ8Args a)
+// Rows in the order in which they are dealt: head by head, so that the sequences (and query heads) that read the same head of the
+// fixed context are on the same XCD at about the same time, where its L2 holds what several of them keep.
+__device__ __forceinline__ int dealt_row(const DecodeQ8Args &a, int i)
+{
+    const int n = a.B * a.per, h = i / n, rest = i - h * n, b = rest / a.per;
+    return (b * a.H + h) * a.per + rest - b * a.per;
+}
+
+__global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g4 = lane >> 4;
     __shared__ __align__(16) SharedMem sm;
@@ -102,30 +122,32 @@ __global__ __launch_bounds__(256) void decode_q8_kernel(DecodeQ8Args a)
     __shared__ int s_w[4], s_found[2];
     __shared__ float s_ml[2][4][16];
 
-    // This workgroup's share of the tiles.
+    // This workgroup's share of the tiles.  Workgroups go round the 8 XCDs: each XCD takes consecutive shares.
     const int R = a.B * a.H * a.per;
-    const int each = (R + 255) / 256, r_lo = min(R, tid * each), r_hi = min(R, r_lo + each);
+    const int each = (R + 255) / 256, i_lo = min(R, tid * each), i_hi = min(R, i_lo + each);
     int mine = 0, all;
-    for (int r = r_lo; r < r_hi; ++r) mine += row_tiles(a, r).total;
+    for (int i = i_lo; i < i_hi; ++i) mine += row_tiles(a, dealt_row(a, i)).total;
     int before = block_exclusive(mine, tid, s_w, all);
     const int shares = min((int)gridDim.x, (all + 3) / 4);
-    const int per = (all + shares - 1) / shares;
-    const int t0 = blockIdx.x * per, t1 = min(all, t0 + per);
-    if (t0 >= t1) return;
+    const int per = (all + shares - 1) / shares, per_xcd = (shares + 7) / 8;
+    const int share = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per_xcd || (long long)share * per >= all) return;
+    const int t0 = share * per, t1 = min(all, t0 + per);
     if (before <= t0 && t0 < before + mine) {
-        int r = r_lo;
-        for (;; ++r) {
-            const int n = row_tiles(a, r).total;
+        int i = i_lo;
+        for (;; ++i) {
+            const int n = row_tiles(a, dealt_row(a, i)).total;
             if (t0 < before + n) break;
             before += n;
         }
-        s_found[0] = r;
+        s_found[0] = i;
         s_found[1] = before;
     }
     __syncthreads();
-    int r = s_found[0], row_start = s_found[1];
+    int ri = s_found[0], row_start = s_found[1];
 
-    for (; row_start < t1; ++r) {
+    for (; row_start < t1; ++ri) {
+        const int r = dealt_row(a, ri);
         const RowTiles rt = row_tiles(a, r);
         const int bh = r / a.per, h = bh % a.H, b = bh / a.H;
         const int lo = max(t0 - row_start, 0), hi = min(t1 - row_start, rt.total);
@@ -178,127 +200,153 @@ __global__ __launch_bounds__(256) void decode_q8_kernel(DecodeQ8Args a)
                 }
                 listed = range0 < nr ? nfix : max(0, min(p1, range_before) - p0);
                 __syncthreads();
-                unsigned long long bal[QLIST / 256];
+            }
+            unsigned long long bal[QLIST / 256] = {};
+            if (nfix > 0) {
 #pragma unroll
                 for (int i = 0; i < QLIST / 256; ++i) {
                     bal[i] = __ballot(s_delta[(i * 4 + wave) * 64 + lane] != SENTINEL);
                     if (lane == 0) s_bal[i * 4 + wave] = bal[i];
                 }
                 __syncthreads();
+            }
+            // Each thread lists up to four keys.  Their scales are read while the first tile is: they are stored behind its loads.
+            const int ntf = max(0, min(c1, rt.tf) - c0) * QT;   // slots of tiles with fixed keys; the user's are behind them
+            const int u0 = (max(c0, rt.tf) - rt.tf) * QT;        // first user key of the chunk
+            float ks[QLIST / 256], vs[QLIST / 256];
 #pragma unroll
-                for (int i = 0; i < QLIST / 256; ++i) {
-                    const int grp = i * 4 + wave, pos = grp * 64 + lane;
-                    if (pos >= nfix) continue;
+            for (int i = 0; i < QLIST / 256; ++i) {
+                const int grp = i * 4 + wave, pos = grp * 64 + lane;
+                ks[i] = vs[i] = 0.0f;
+                if (pos >= n) continue;
+                uint32_t row = NO_KEY;
+                if (pos < nfix) {
                     unsigned long long w = bal[i] & (~0ull >> (63 - lane));
                     int from = grp;
                     while (w == 0ull && from > 0) w = s_bal[--from];
-                    const bool ok = w != 0ull && pos < listed;
-                    const int d = ok ? s_delta[from * 64 + 63 - __clzll((long long)w)] : 0;
-                    const int key = min(max(p0 + pos + d, 0), a.L - 1);
-                    const int sb = h * a.sblocks + (key >> 6);
-                    sm.list.row[pos] = ok ? (uint32_t)(h * a.L + key) : NO_KEY;
-                    sm.list.ks[pos] = a.ks[sb];
-                    sm.list.vs[pos] = a.vs[sb];
+                    if (w != 0ull && pos < listed) {
+                        const int d = s_delta[from * 64 + 63 - __clzll((long long)w)];
+                        const int key = min(max(p0 + pos + d, 0), a.L - 1);
+                        row = (uint32_t)(h * a.L + key);
+                        const int sb = h * a.sblocks + (key >> 6);
+                        ks[i] = a.ks[sb];
+                        vs[i] = a.vs[sb];
+                    }
+                } else if (pos >= ntf && u0 + pos - ntf < rt.nu) {
+                    const int t = u0 + pos - ntf;
+                    const int page = a.page_table[(size_t)b * a.max_pages + t / a.P];
+                    if (page >= 0 && page < a.n_pages) {
+                        const int ph = page * a.H + h;
+                        row = (uint32_t)(ph * a.P + t % a.P);
+                        ks[i] = a.cks[ph];
+                        vs[i] = a.cvs[ph];
+                    }
                 }
-            }
-            // the rest of the last fixed tile, and the user's keys behind it
-            const int ntf = max(0, min(c1, rt.tf) - c0) * QT;   // slots of tiles with fixed keys
-            const int u0 = (max(c0, rt.tf) - rt.tf) * QT;        // first user key of the chunk
-            for (int pos = max(nfix, 0) + tid; pos < n; pos += 256) {
-                const int t = u0 + pos - ntf;
-                bool ok = pos >= ntf && t < rt.nu;
-                int page = -1;
-                if (ok) page = a.page_table[(size_t)b * a.max_pages + t / a.P];
-                ok = ok && page >= 0 && page < a.n_pages;
-                const int ph = ok ? page * a.H + h : 0;
-                sm.list.row[pos] = ok ? (uint32_t)(ph * a.P + t % a.P) : NO_KEY;
-                sm.list.ks[pos] = ok ? a.cks[ph] : 0.0f;
-                sm.list.vs[pos] = ok ? a.cvs[ph] : 0.0f;
+                sm.list.row[pos] = row;
             }
             __syncthreads();
 
-            for (int t = wave; t < c1 - c0; t += 4) {
+            const int tiles = c1 - c0;
+            auto load = [&](Tile &x, int t) {
                 const bool fixed = c0 + t < rt.tf;
-                const uint8_t *Kb = fixed ? a.K8 : a.cK, *Vb = fixed ? a.V8 : a.cV;
+                const uint8_t *Kb = (fixed ? a.K8 : a.cK) + 32 * g4, *Vb = (fixed ? a.V8 : a.cV) + 8 * c16;
                 const uint32_t *rows = sm.list.row + t * QT;
-                const uint32_t r0 = rows[c16], r1 = rows[16 + c16];
-                const u4v v0 = *reinterpret_cast<const u4v *>(rows + 4 * g4), v1 = *reinterpret_cast<const u4v *>(rows + 16 + 4 * g4);
-                const bool holes = __any(r0 == NO_KEY || r1 == NO_KEY);
+                // (a slot without a key reads row 0, which there is)
                 auto at = [](uint32_t row) { return (size_t)(row == NO_KEY ? 0u : row) * D; };
-                u4v k[2][2];
-                u2v v[8];
-                if (!__any(r0 != NO_KEY || r1 != NO_KEY)) continue;      // (nothing visible: a bad page, an empty row)
-                k[0][0] = *reinterpret_cast<const u4v *>(Kb + at(r0) + 32 * g4);
-                k[0][1] = *reinterpret_cast<const u4v *>(Kb + at(r0) + 32 * g4 + 16);
-                k[1][0] = *reinterpret_cast<const u4v *>(Kb + at(r1) + 32 * g4);
-                k[1][1] = *reinterpret_cast<const u4v *>(Kb + at(r1) + 32 * g4 + 16);
+                const size_t k0 = at(rows[c16]), k1 = at(rows[16 + c16]);
+                const u4v v0 = *reinterpret_cast<const u4v *>(rows + 4 * g4), v1 = *reinterpret_cast<const u4v *>(rows + 16 + 4 * g4);
+                x.k[0][0] = *reinterpret_cast<const u4v *>(Kb + k0);
+                x.k[0][1] = *reinterpret_cast<const u4v *>(Kb + k0 + 16);
+                x.k[1][0] = *reinterpret_cast<const u4v *>(Kb + k1);
+                x.k[1][1] = *reinterpret_cast<const u4v *>(Kb + k1 + 16);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    v[i] = *reinterpret_cast<const u2v *>(Vb + at(v0[i]) + 8 * c16);
-                    v[4 + i] = *reinterpret_cast<const u2v *>(Vb + at(v1[i]) + 8 * c16);
+                    x.v[i] = *reinterpret_cast<const u2v *>(Vb + at(v0[i]));
+                    x.v[4 + i] = *reinterpret_cast<const u2v *>(Vb + at(v1[i]));
                 }
-                float x[8], mx = SQ_NEG_INF;
+            };
+            auto fold = [&](Tile &x, int t) {
+                const uint32_t *rows = sm.list.row + t * QT;
+                float s[8], mx = SQ_NEG_INF;
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     f4 acc = {0.f, 0.f, 0.f, 0.f};
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(k[u][0].x, k[u][0].y), qf[0], acc, 0, 0, 0);
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(k[u][0].z, k[u][0].w), qf[1], acc, 0, 0, 0);
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(k[u][1].x, k[u][1].y), qf[2], acc, 0, 0, 0);
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(k[u][1].z, k[u][1].w), qf[3], acc, 0, 0, 0);
-                    const f4 ks = *reinterpret_cast<const f4 *>(sm.list.ks + t * QT + 16 * u + 4 * g4);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(x.k[u][0].x, x.k[u][0].y), qf[0], acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(x.k[u][0].z, x.k[u][0].w), qf[1], acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(x.k[u][1].x, x.k[u][1].y), qf[2], acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(x.k[u][1].z, x.k[u][1].w), qf[3], acc, 0, 0, 0);
+                    const f4 f = *reinterpret_cast<const f4 *>(sm.list.ks + t * QT + 16 * u + 4 * g4);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[4 * u + i] = acc[i] * (ks[i] * a.scale);
+                    for (int i = 0; i < 4; ++i) s[4 * u + i] = acc[i] * (f[i] * a.scale);
                 }
-                if (holes) {
+                uint32_t w[2][8];                            // V: words of dimensions 8 c16 .. + 3 and .. + 7
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (v0[i] == NO_KEY) {
-                            x[i] = SQ_NEG_INF;
-                            v[i] = u2v{0u, 0u};
+                for (int i = 0; i < 8; ++i) {
+                    w[0][i] = x.v[i].x;
+                    w[1][i] = x.v[i].y;
+                }
+                if (__any(rows[lane & 31] == NO_KEY)) {      // what stands in such a slot's row is not looked at
+                    const u4v v0 = *reinterpret_cast<const u4v *>(rows + 4 * g4), v1 = *reinterpret_cast<const u4v *>(rows + 16 + 4 * g4);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if ((i < 4 ? v0[i & 3] : v1[i & 3]) == NO_KEY) {
+                            s[i] = SQ_NEG_INF;
+                            w[0][i] = w[1][i] = 0u;
                         }
-                        if (v1[i] == NO_KEY) {
-                            x[4 + i] = SQ_NEG_INF;
-                            v[4 + i] = u2v{0u, 0u};
-                        }
-                    }
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) mx = fmaxf(mx, x[i]);
+                for (int i = 0; i < 8; ++i) mx = fmaxf(mx, s[i]);
                 const float mn = fmaxf(m, cross16_max(mx));
                 const float mu = mn == SQ_NEG_INF ? 0.0f : mn;
-                const float alpha = exp2f(m - mu);
+                const float alpha = __builtin_amdgcn_exp2f(m - mu);
                 m = mn;
                 l *= alpha;
                 b8 hi8, lo8;
-                const f4 vs0 = *reinterpret_cast<const f4 *>(sm.list.vs + t * QT + 4 * g4);
-                const f4 vs1 = *reinterpret_cast<const f4 *>(sm.list.vs + t * QT + 16 + 4 * g4);
+                const f4 f0 = *reinterpret_cast<const f4 *>(sm.list.vs + t * QT + 4 * g4);
+                const f4 f1 = *reinterpret_cast<const f4 *>(sm.list.vs + t * QT + 16 + 4 * g4);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float p = exp2f(x[i] - mu);
+                    const float p = __builtin_amdgcn_exp2f(s[i] - mu);
                     l += p;
-                    const float pv = p * (i < 4 ? vs0[i & 3] : vs1[i & 3]);
+                    const float pv = p * (i < 4 ? f0[i & 3] : f1[i & 3]);
                     hi8[i] = (__bf16)pv;
                     lo8[i] = (__bf16)(pv - (float)hi8[i]);
-                }
-                // V^T: the words of keys 0..3 and 4..7 of this lane, dimensions 8 c16 + dt
-                uint32_t w[2][8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    w[0][i] = v[i].x;
-                    w[1][i] = v[i].y;
                 }
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     transpose4(w[i][0], w[i][1], w[i][2], w[i][3]);
                     transpose4(w[i][4], w[i][5], w[i][6], w[i][7]);
                 }
+                if (__any(alpha != 1.0f)) {                  // (the maximum rarely moves behind the first tiles)
+#pragma unroll
+                    for (int dt = 0; dt < 8; ++dt) o[dt] *= alpha;
+                }
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) {
                     const b8 vf = codes_bf16(w[dt >> 2][dt & 3], w[dt >> 2][4 + (dt & 3)]);
-                    o[dt] *= alpha;
                     o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi8, o[dt], 0, 0, 0);
                     o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo8, o[dt], 0, 0, 0);
                 }
+            };
+            // A wave's tiles, the next one on its way while one is folded.
+            Tile x, y;
+            if (wave < tiles) load(x, wave);
+#pragma unroll
+            for (int i = 0; i < QLIST / 256; ++i) {
+                const int pos = (i * 4 + wave) * 64 + lane;
+                if (pos < n) {
+                    sm.list.ks[pos] = ks[i];
+                    sm.list.vs[pos] = vs[i];
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+            for (int t = wave; t < tiles; t += 8) {
+                if (t + 4 < tiles) load(y, t + 4);
+                fold(x, t);
+                if (t + 8 < tiles) load(x, t + 8);
+                if (t + 4 < tiles) fold(y, t + 4);
             }
         }
         // The four waves' results of the row.
@@ -318,7 +366,7 @@ __global__ __launch_bounds__(256) void decode_q8_kernel(DecodeQ8Args a)
         }
         __syncthreads();
         const bool whole = lo == 0 && hi == rt.total;
-        const int slot = blockIdx.x + r;
+        const int slot = share + ri;
         for (int i = tid; i < a.g * D; i += 256) {
             const int qi = i >> 7, d = i & 127;
             float M = fmaxf(fmaxf(s_ml[0][0][qi], s_ml[0][1][qi]), fmaxf(s_ml[0][2][qi], s_ml[0][3][qi]));
@@ -331,9 +379,7 @@ __global__ __launch_bounds__(256) void decode_q8_kernel(DecodeQ8Args a)
                 os += f * sm.out.o[w][qi][d];
             }
             if (whole) {
-                const size_t at = (size_t)r * a.g + qi;
-                a.out[at * D + d] = (_Float16)(ls > 0.0f || ls != ls ? os / ls : 0.0f);
-                if (d == 0 && a.lse) a.lse[at] = ls > 0.0f || ls != ls ? (M + log2f(ls)) * 0.69314718055994531f : SQ_NEG_INF;
+                store_result(a, (size_t)r * a.g + qi, d, M, ls, os);
             } else {
                 float *p = a.part + ((size_t)slot * a.g + qi) * PART_STRIDE;
                 p[4 + d] = os;
@@ -345,33 +391,63 @@ __global__ __launch_bounds__(256) void decode_q8_kernel(DecodeQ8Args a)
         }
         if (tid == 0 && lo == 0) {
             const int last = (row_start + rt.total - 1) / per;
-            a.info[r] = int2{(int)blockIdx.x + r, whole ? 0 : last - (int)blockIdx.x + 1};
+            a.info[r] = int2{slot, whole ? 0 : last - share + 1};
         }
         __syncthreads();
         row_start += rt.total;
     }
 }
 
-// Rows that several workgroups took: one workgroup per row and query.
-__global__ __launch_bounds__(128) void decode_q8_merge_kernel(DecodeQ8Args a)
+// Rows that several workgroups took: one workgroup per row and query.  Eight groups of 32 lanes fold every eighth partial result,
+// a lane four dimensions, and are folded in LDS.
+__global__ __launch_bounds__(256) void decode_q8_merge_kernel(DecodeQ8Args a)
 {
-    const int r = blockIdx.x / a.g, qi = blockIdx.x - r * a.g, d = threadIdx.x;
+    const int r = blockIdx.x / a.g, qi = blockIdx.x - r * a.g, tid = threadIdx.x, grp = tid >> 5, quad = tid & 31;
+    __shared__ float s_m[8], s_l[8];
+    __shared__ __align__(16) float s_o[8][D];
     const int2 info = a.info[r];
     if (info.y == 0) return;
-    float M = SQ_NEG_INF, ls = 0.0f, os = 0.0f;
-    for (int i = 0; i < info.y; ++i) {
-        const float *p = a.part + ((size_t)(info.x + i) * a.g + qi) * PART_STRIDE;
-        const float pm = p[0], pl = p[1], po = p[4 + d];
+    float M = SQ_NEG_INF, ls = 0.0f;
+    f4 os = {0.f, 0.f, 0.f, 0.f};
+    auto part = [&](int i) { return a.part + ((size_t)(info.x + i) * a.g + qi) * PART_STRIDE; };
+    auto fold = [&](float pm, float pl, f4 po) {
         const float mn = fmaxf(M, pm), mu = mn == SQ_NEG_INF ? 0.0f : mn;
         const float fa = exp2f(M - mu), fb = exp2f(pm - mu);
         ls = ls * fa + pl * fb;
         os = os * fa + po * fb;
         M = mn;
+    };
+    int i = grp;
+    for (; i + 8 < info.y; i += 16) {
+        const float *p = part(i), *n = part(i + 8);
+        const float2 a0 = *reinterpret_cast<const float2 *>(p), a1 = *reinterpret_cast<const float2 *>(n);
+        const f4 o0 = *reinterpret_cast<const f4 *>(p + 4 + 4 * quad), o1 = *reinterpret_cast<const f4 *>(n + 4 + 4 * quad);
+        fold(a0.x, a0.y, o0);
+        fold(a1.x, a1.y, o1);
     }
-    const size_t at = (size_t)r * a.g + qi;
-    const bool any = ls > 0.0f || ls != ls;
-    a.out[at * D + d] = (_Float16)(any ? os / ls : 0.0f);
-    if (d == 0 && a.lse) a.lse[at] = any ? (M + log2f(ls)) * 0.69314718055994531f : SQ_NEG_INF;
+    if (i < info.y) {
+        const float *p = part(i);
+        fold(p[0], p[1], *reinterpret_cast<const f4 *>(p + 4 + 4 * quad));
+    }
+    *reinterpret_cast<f4 *>(&s_o[grp][4 * quad]) = os;
+    if (quad == 0) {
+        s_m[grp] = M;
+        s_l[grp] = ls;
+    }
+    __syncthreads();
+    if (tid >= D) return;
+    float MM = s_m[0];
+#pragma unroll
+    for (int g = 1; g < 8; ++g) MM = fmaxf(MM, s_m[g]);
+    const float mu = MM == SQ_NEG_INF ? 0.0f : MM;
+    float lt = 0.0f, ot = 0.0f;
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+        const float f = exp2f(s_m[g] - mu);
+        lt += f * s_l[g];
+        ot += f * s_o[g][tid];
+    }
+    store_result(a, (size_t)r * a.g + qi, tid, MM, lt, ot);
 }
 
 hipError_t launch_decode_q8(const DecodeQ8Args &a, hipStream_t s)
@@ -383,7 +459,7 @@ hipError_t launch_decode_q8(const DecodeQ8Args &a, hipStream_t s)
         hipLaunchKernelGGL(decode_q8_kernel, dim3(Q8_GRID), dim3(256), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(decode_q8_merge_kernel, dim3((unsigned)(a.B * a.H * a.per * a.g)), dim3(128), 0, s, a);
+    hipLaunchKernelGGL(decode_q8_merge_kernel, dim3((unsigned)(a.B * a.H * a.per * a.g)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 

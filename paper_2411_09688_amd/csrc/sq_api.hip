@@ -1914,7 +1914,7 @@ int sq_sparse_attn_decode_q8(const sq_shape_t *sh, int32_t one_set, const void *
         a.cvs = cache->v_scale;
         a.page_table = cache->page_table;
         a.seq_len = seq_len;
-        a.P = cache->page_tokens;
+        a.p_log = cache->page_tokens == 16 ? 4 : cache->page_tokens == 32 ? 5 : 6;
         a.n_pages = cache->n_pages;
         a.max_pages = cache->max_pages;
     }

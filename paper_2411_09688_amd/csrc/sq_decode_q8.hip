@@ -23,26 +23,17 @@ typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 
 constexpr int QT = 32;                       // keys per tile
-constexpr int QCHUNK = 32;                   // tiles whose key rows are listed at a time
-constexpr int QLIST = QT * QCHUNK;           // ... 1024 keys
-constexpr uint32_t NO_KEY = 0xffffffffu;
 constexpr int SENTINEL = INT32_MIN;
 constexpr int O_STRIDE = 132;
+constexpr int GROUP = 64;                    // ranges that a wave holds at a time
+constexpr int MAX_GROUPS = SELECT_MAX_C / GROUP;
 
-struct KeyList {                             // the rows (of 128 codes) of a chunk's keys and their scales
-    uint32_t row[QLIST];
-    float ks[QLIST], vs[QLIST];
-};
-struct Tile {                                // what a lane reads of 32 keys
-    u4v k[2][2];                             // keys c16 and 16 + c16, dimensions 32 g4 ..
-    u2v v[8];                                // keys 4 g4 .. and 16 + 4 g4 .., dimensions 8 c16 ..
+struct KeyList {                             // 64 keys of a wave: where they stand (bytes from the tensor's first) and their scales
+    unsigned long long at[64];               // (0 for a slot without a key: the first row, which there is)
+    float ks[64], vs[64];                    // ks: times the softmax's
 };
 struct WaveOut {                             // the four waves' results of a row
     float o[4][16][O_STRIDE];
-};
-union SharedMem {
-    KeyList list;
-    WaveOut out;
 };
 
 struct RowTiles {
@@ -53,7 +44,7 @@ __device__ __forceinline__ RowTiles row_tiles(const DecodeQ8Args &a, int r)
 {
     RowTiles t;
     t.nf = a.ranges ? min(max(a.n_keys[r], 0), a.L) : 0;
-    t.nu = a.seq_len ? min(max(a.seq_len[r / (a.H * a.per)], 0), a.max_pages * a.P) : 0;
+    t.nu = a.seq_len ? min(max(a.seq_len[r / (a.H * a.per)], 0), a.max_pages << a.p_log) : 0;
     t.tf = (t.nf + QT - 1) / QT;
     t.total = max(1, t.tf + (t.nu + QT - 1) / QT);
     return t;
@@ -113,12 +104,21 @@ __device__ __forceinline__ int dealt_row(const DecodeQ8Args &a, int i)
     return (b * a.H + h) * a.per + rest - b * a.per;
 }
 
+// What one lane writes to LDS another lane of the wave reads.
+__device__ __forceinline__ void wave_lds_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g4 = lane >> 4;
-    __shared__ __align__(16) SharedMem sm;
-    __shared__ int s_delta[QLIST];
-    __shared__ unsigned long long s_bal[QLIST / 64];
+    __shared__ __align__(16) WaveOut s_out;
+    __shared__ __align__(16) KeyList s_list[4][2];
+    __shared__ int s_delta[4][64];
+    __shared__ int s_group[MAX_GROUPS];
     __shared__ int s_w[4], s_found[2];
     __shared__ float s_ml[2][4][16];
 
@@ -163,152 +163,198 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = f4{0.f, 0.f, 0.f, 0.f};
 
-        int range0 = 0, range_before = 0;                   // first range of the batch that holds the next position; keys before it
-        for (int c0 = lo; c0 < hi; c0 += QCHUNK) {
-            const int c1 = min(hi, c0 + QCHUNK), n = (c1 - c0) * QT;
-            // fixed keys: positions [p0, p1) of the row's list
-            const int p0 = min(c0 * QT, rt.nf), p1 = min(c1 * QT, rt.nf);
-            const int nfix = p1 - p0;
-            int listed = 0;                                 // of them, those that the ranges really have
-            __syncthreads();
-            if (nfix > 0) {
-                for (int i = tid; i < QLIST; i += 256) s_delta[i] = SENTINEL;
-                const int nr = min(max(a.n_ranges[r], 0), a.C);
-                const int2 *rg = reinterpret_cast<const int2 *>(a.ranges) + (size_t)r * a.C;
-                int total = 0;
-                for (; range0 < nr; range0 += 1024) {
-                    int2 e[4];
-                    int sum = 0;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int i = range0 + tid * 4 + k;
-                        e[k] = i < nr ? rg[i] : int2{0, 0};
-                        e[k].x = min(max(e[k].x, -MAX_L), MAX_L);
-                        e[k].y = min(max(e[k].y, 0), a.L);
-                        sum += e[k].y;
-                    }
-                    // (counts that sum to more than a row can have are cut, far from overflow)
-                    int at = block_exclusive(min(sum, MAX_L), tid, s_w, total) + range_before;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int from = max(at, p0), to = min(at + e[k].y, p1);
-                        if (from < to) s_delta[from - p0] = e[k].x - at;
-                        at += e[k].y;
-                    }
-                    if (range_before + total >= p1) break;
-                    range_before = min(range_before + total, MAX_L);
-                }
-                listed = range0 < nr ? nfix : max(0, min(p1, range_before) - p0);
-                __syncthreads();
-            }
-            unsigned long long bal[QLIST / 256] = {};
-            if (nfix > 0) {
-#pragma unroll
-                for (int i = 0; i < QLIST / 256; ++i) {
-                    bal[i] = __ballot(s_delta[(i * 4 + wave) * 64 + lane] != SENTINEL);
-                    if (lane == 0) s_bal[i * 4 + wave] = bal[i];
-                }
-                __syncthreads();
-            }
-            // Each thread lists up to four keys.  Their scales are read while the first tile is: they are stored behind its loads.
-            const int ntf = max(0, min(c1, rt.tf) - c0) * QT;   // slots of tiles with fixed keys; the user's are behind them
-            const int u0 = (max(c0, rt.tf) - rt.tf) * QT;        // first user key of the chunk
-            float ks[QLIST / 256], vs[QLIST / 256];
-#pragma unroll
-            for (int i = 0; i < QLIST / 256; ++i) {
-                const int grp = i * 4 + wave, pos = grp * 64 + lane;
-                ks[i] = vs[i] = 0.0f;
-                if (pos >= n) continue;
-                uint32_t row = NO_KEY;
-                if (pos < nfix) {
-                    unsigned long long w = bal[i] & (~0ull >> (63 - lane));
-                    int from = grp;
-                    while (w == 0ull && from > 0) w = s_bal[--from];
-                    if (w != 0ull && pos < listed) {
-                        const int d = s_delta[from * 64 + 63 - __clzll((long long)w)];
-                        const int key = min(max(p0 + pos + d, 0), a.L - 1);
-                        row = (uint32_t)(h * a.L + key);
-                        const int sb = h * a.sblocks + (key >> 6);
-                        ks[i] = a.ks[sb];
-                        vs[i] = a.vs[sb];
-                    }
-                } else if (pos >= ntf && u0 + pos - ntf < rt.nu) {
-                    const int t = u0 + pos - ntf;
-                    const int page = a.page_table[(size_t)b * a.max_pages + t / a.P];
-                    if (page >= 0 && page < a.n_pages) {
-                        const int ph = page * a.H + h;
-                        row = (uint32_t)(ph * a.P + t % a.P);
-                        ks[i] = a.cks[ph];
-                        vs[i] = a.cvs[ph];
-                    }
-                }
-                sm.list.row[pos] = row;
-            }
-            __syncthreads();
+        // The row's ranges in groups of 64: how many keys lie before each group, for a wave to find its first.
+        const int2 *rg = reinterpret_cast<const int2 *>(a.ranges) + (size_t)r * a.C;
+        const int nr = lo < rt.tf ? min(max(a.n_ranges[r], 0), a.C) : 0, groups = (nr + GROUP - 1) / GROUP;
+        auto range_of = [&](int gi) {                       // this lane's range of a group; (0, 0) behind the last
+            const int i = gi * GROUP + lane;
+            int2 e = i < nr ? rg[i] : int2{0, 0};
+            e.x = min(max(e.x, -MAX_L), MAX_L);
+            e.y = min(max(e.y, 0), a.L);
+            return e;
+        };
+        for (int gi = wave; gi < groups; gi += 4) {
+            // (counts that sum to more than a row can have are cut, far from overflow)
+            const int n = min(wave_sum_i(range_of(gi).y), MAX_L);
+            if (lane == 0) s_group[gi] = n;
+        }
+        __syncthreads();
 
-            const int tiles = c1 - c0;
-            auto load = [&](Tile &x, int t) {
-                const bool fixed = c0 + t < rt.tf;
-                const uint8_t *Kb = (fixed ? a.K8 : a.cK) + 32 * g4, *Vb = (fixed ? a.V8 : a.cV) + 8 * c16;
-                const uint32_t *rows = sm.list.row + t * QT;
-                // (a slot without a key reads row 0, which there is)
-                auto at = [](uint32_t row) { return (size_t)(row == NO_KEY ? 0u : row) * D; };
-                const size_t k0 = at(rows[c16]), k1 = at(rows[16 + c16]);
-                const u4v v0 = *reinterpret_cast<const u4v *>(rows + 4 * g4), v1 = *reinterpret_cast<const u4v *>(rows + 16 + 4 * g4);
-                x.k[0][0] = *reinterpret_cast<const u4v *>(Kb + k0);
-                x.k[0][1] = *reinterpret_cast<const u4v *>(Kb + k0 + 16);
-                x.k[1][0] = *reinterpret_cast<const u4v *>(Kb + k1);
-                x.k[1][1] = *reinterpret_cast<const u4v *>(Kb + k1 + 16);
+        // This wave's quarter of the tiles: fixed keys, then the user's, 64 keys listed at a time and a step ahead.
+        const int w0 = lo + (int)((long long)(hi - lo) * wave / 4), w1 = lo + (int)((long long)(hi - lo) * (wave + 1) / 4);
+        for (int phase = 0; phase < 2; ++phase) {
+            const bool fixed = phase == 0;
+            const int f0 = fixed ? w0 : max(w0, rt.tf) - rt.tf;          // first tile of the phase, and how many
+            const int tiles = (fixed ? min(w1, rt.tf) : w1 - rt.tf) - f0;
+            if (tiles <= 0) continue;
+            const uint8_t *Kb = (fixed ? a.K8 : a.cK) + 32 * g4, *Vb = (fixed ? a.V8 : a.cV) + 8 * c16;
+            const float *kscale = fixed ? a.ks : a.cks, *vscale = fixed ? a.vs : a.cvs;
+            int p = f0 * QT;                                // the next position to list
+            int end;                                        // where the row's keys end
+            // ranges in hand: group gi, its lanes' first positions, where it ends; the group behind it is on its way
+            int gi = 0, first = 0, ends = 0;
+            int2 e = {0, 0}, e_next = {0, 0};
+            int page = -1;                                  // user: the page of position p + lane, read ahead
+            if (fixed) {
+                int sum[MAX_GROUPS / 64], at = 0;
+                int total = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x.v[i] = *reinterpret_cast<const u2v *>(Vb + at(v0[i]));
-                    x.v[4 + i] = *reinterpret_cast<const u2v *>(Vb + at(v1[i]));
+                for (int i = 0; i < MAX_GROUPS / 64; ++i) {
+                    sum[i] = 4 * lane + i < groups ? s_group[4 * lane + i] : 0;
+                    total += sum[i];
                 }
+                const int inc = wave_inclusive_scan(total, lane);
+                end = min(rt.nf, __builtin_amdgcn_readlane(inc, 63));
+                at = inc - total;
+                int here = 0, start = 0;                    // groups that end at or before p; the last start at or before it
+#pragma unroll
+                for (int i = 0; i < MAX_GROUPS / 64; ++i) {
+                    const bool passed = 4 * lane + i < groups && at + sum[i] <= p;
+                    here += __popcll(__ballot(passed));
+                    start = max(start, passed ? at + sum[i] : 0);
+                    at += sum[i];
+                }
+                gi = min(here, max(groups - 1, 0));
+                // (groups pass in order, so the last passed end is the found group's start)
+#pragma unroll
+                for (int k = 32; k > 0; k >>= 1) start = max(start, __shfl_xor(start, k));
+                e = range_of(gi);
+                e_next = range_of(gi + 1);
+                const int c = wave_inclusive_scan(e.y, lane);
+                first = start + c - e.y;
+                ends = start + __builtin_amdgcn_readlane(c, 63);
+            } else {
+                end = rt.nu;
+                if (p + lane < end) page = a.page_table[(size_t)b * a.max_pages + ((p + lane) >> a.p_log)];
+            }
+
+            float ks = 0.0f, vs = 0.0f;
+            unsigned long long seen = 0ull, seen_next = 0ull;   // slots with a key, of the list in use and the next
+            // Lists positions p .. p + 63 and starts to read their scales.
+            auto list = [&](int buf) {
+                bool ok = p + lane < end;
+                unsigned long long at = 0ull;
+                int sc = 0;
+                if (fixed) {
+                    s_delta[wave][lane] = SENTINEL;
+                    wave_lds_sync();
+                    for (;;) {
+                        const int from = max(first, p), to = min(first + e.y, p + 64);
+                        if (from < to) s_delta[wave][from - p] = e.x - first;
+                        if (ends >= p + 64 || gi + 1 >= groups) break;
+                        e = e_next;
+                        ++gi;
+                        e_next = range_of(gi + 1);
+                        const int c = wave_inclusive_scan(e.y, lane);
+                        first = ends + c - e.y;
+                        ends = min(ends + __builtin_amdgcn_readlane(c, 63), MAX_L + MAX_L);
+                    }
+                    wave_lds_sync();
+                    const unsigned long long marks = __ballot(s_delta[wave][lane] != SENTINEL) & (~0ull >> (63 - lane));
+                    ok = ok && marks != 0ull;
+                    if (ok) {
+                        const int d = s_delta[wave][63 - __clzll((long long)marks)];
+                        const int key = min(max(p + lane + d, 0), a.L - 1);
+                        at = ((unsigned long long)h * a.L + key) * D;
+                        sc = h * a.sblocks + (key >> 6);
+                    }
+                } else {
+                    const int t = p + lane;
+                    ok = ok && page >= 0 && page < a.n_pages;
+                    if (ok) {
+                        sc = page * a.H + h;
+                        at = (((unsigned long long)sc << a.p_log) + (t & ((1 << a.p_log) - 1))) * D;
+                    }
+                    if (t + 64 < end) page = a.page_table[(size_t)b * a.max_pages + ((t + 64) >> a.p_log)];
+                }
+                ks = vs = 0.0f;
+                if (ok) {
+                    ks = kscale[sc];
+                    vs = vscale[sc];
+                }
+                s_list[wave][buf].at[lane] = at;
+                seen_next = __ballot(ok);
+                p += 64;
+                wave_lds_sync();
             };
-            auto fold = [&](Tile &x, int t) {
-                const uint32_t *rows = sm.list.row + t * QT;
-                float s[8], mx = SQ_NEG_INF;
+            auto list_scales = [&](int buf) {
+                s_list[wave][buf].ks[lane] = ks * a.scale;
+                s_list[wave][buf].vs[lane] = vs;
+                wave_lds_sync();
+            };
+            u4v k[2][2];                                    // keys c16 and 16 + c16, dimensions 32 g4 ..
+            u2v v[8];                                       // keys 4 g4 .. and 16 + 4 g4 .., dimensions 8 c16 ..
+            auto load_k = [&](int t) {
+                const unsigned long long *at = s_list[wave][(t >> 1) & 1].at + (t & 1) * QT;
+                const uint8_t *k0 = Kb + at[c16], *k1 = Kb + at[16 + c16];
+                k[0][0] = *reinterpret_cast<const u4v *>(k0);
+                k[0][1] = *reinterpret_cast<const u4v *>(k0 + 16);
+                k[1][0] = *reinterpret_cast<const u4v *>(k1);
+                k[1][1] = *reinterpret_cast<const u4v *>(k1 + 16);
+            };
+            auto load_v = [&](int t) {
+                const unsigned long long *at = s_list[wave][(t >> 1) & 1].at + (t & 1) * QT;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const u2v *>(Vb + at[(i < 4 ? 0 : 16) + 4 * g4 + (i & 3)]);
+            };
+
+            list(0);
+            load_k(0);
+            load_v(0);
+            list_scales(0);
+            for (int t = 0; t < tiles; ++t) {
+                const int buf = (t >> 1) & 1, slot = (t & 1) * QT;
+                const bool even = !(t & 1);
+                if (even) {
+                    seen = seen_next;
+                    if (t + 2 < tiles) list(buf ^ 1);
+                }
+                f4 acc[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const u4v x = k[u][s >> 1];
+                        acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(s & 1 ? codes_f16(x.z, x.w) : codes_f16(x.x, x.y), qf[s], acc[u], 0, 0, 0);
+                    }
+                if (t + 1 < tiles) load_k(t + 1);            // (as soon as the scores have used this tile's)
+                float s[8];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    f4 acc = {0.f, 0.f, 0.f, 0.f};
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(x.k[u][0].x, x.k[u][0].y), qf[0], acc, 0, 0, 0);
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(x.k[u][0].z, x.k[u][0].w), qf[1], acc, 0, 0, 0);
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(x.k[u][1].x, x.k[u][1].y), qf[2], acc, 0, 0, 0);
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(x.k[u][1].z, x.k[u][1].w), qf[3], acc, 0, 0, 0);
-                    const f4 f = *reinterpret_cast<const f4 *>(sm.list.ks + t * QT + 16 * u + 4 * g4);
+                    const f4 f = *reinterpret_cast<const f4 *>(s_list[wave][buf].ks + slot + 16 * u + 4 * g4);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s[4 * u + i] = acc[i] * (f[i] * a.scale);
+                    for (int i = 0; i < 4; ++i) s[4 * u + i] = acc[u][i] * f[i];
                 }
                 uint32_t w[2][8];                            // V: words of dimensions 8 c16 .. + 3 and .. + 7
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    w[0][i] = x.v[i].x;
-                    w[1][i] = x.v[i].y;
+                    w[0][i] = v[i].x;
+                    w[1][i] = v[i].y;
                 }
-                if (__any(rows[lane & 31] == NO_KEY)) {      // what stands in such a slot's row is not looked at
-                    const u4v v0 = *reinterpret_cast<const u4v *>(rows + 4 * g4), v1 = *reinterpret_cast<const u4v *>(rows + 16 + 4 * g4);
+                const uint32_t keys = (uint32_t)(seen >> slot);
+                if (keys != 0xffffffffu) {                   // what stands in the row of a slot without a key is not looked at
+                    const uint32_t mine = keys >> (4 * g4);
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        if ((i < 4 ? v0[i & 3] : v1[i & 3]) == NO_KEY) {
+                        if (!(mine >> (i < 4 ? i : 12 + i) & 1u)) {
                             s[i] = SQ_NEG_INF;
                             w[0][i] = w[1][i] = 0u;
                         }
                 }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) mx = fmaxf(mx, s[i]);
+                const float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
                 const float mn = fmaxf(m, cross16_max(mx));
                 const float mu = mn == SQ_NEG_INF ? 0.0f : mn;
                 const float alpha = __builtin_amdgcn_exp2f(m - mu);
                 m = mn;
                 l *= alpha;
                 b8 hi8, lo8;
-                const f4 f0 = *reinterpret_cast<const f4 *>(sm.list.vs + t * QT + 4 * g4);
-                const f4 f1 = *reinterpret_cast<const f4 *>(sm.list.vs + t * QT + 16 + 4 * g4);
+                const f4 v0 = *reinterpret_cast<const f4 *>(s_list[wave][buf].vs + slot + 4 * g4);
+                const f4 v1 = *reinterpret_cast<const f4 *>(s_list[wave][buf].vs + slot + 16 + 4 * g4);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(s[i] - mu);
-                    l += p;
-                    const float pv = p * (i < 4 ? f0[i & 3] : f1[i & 3]);
+                    const float x = __builtin_amdgcn_exp2f(s[i] - mu);
+                    l += x;
+                    const float pv = x * (i < 4 ? v0[i & 3] : v1[i & 3]);
                     hi8[i] = (__bf16)pv;
                     lo8[i] = (__bf16)(pv - (float)hi8[i]);
                 }
@@ -317,6 +363,7 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
                     transpose4(w[i][0], w[i][1], w[i][2], w[i][3]);
                     transpose4(w[i][4], w[i][5], w[i][6], w[i][7]);
                 }
+                if (t + 1 < tiles) load_v(t + 1);
                 if (__any(alpha != 1.0f)) {                  // (the maximum rarely moves behind the first tiles)
 #pragma unroll
                     for (int dt = 0; dt < 8; ++dt) o[dt] *= alpha;
@@ -327,31 +374,11 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
                     o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi8, o[dt], 0, 0, 0);
                     o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo8, o[dt], 0, 0, 0);
                 }
-            };
-            // A wave's tiles, the next one on its way while one is folded.
-            Tile x, y;
-            if (wave < tiles) load(x, wave);
-#pragma unroll
-            for (int i = 0; i < QLIST / 256; ++i) {
-                const int pos = (i * 4 + wave) * 64 + lane;
-                if (pos < n) {
-                    sm.list.ks[pos] = ks[i];
-                    sm.list.vs[pos] = vs[i];
-                }
-            }
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-            __builtin_amdgcn_s_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-            for (int t = wave; t < tiles; t += 8) {
-                if (t + 4 < tiles) load(y, t + 4);
-                fold(x, t);
-                if (t + 8 < tiles) load(x, t + 8);
-                if (t + 4 < tiles) fold(y, t + 4);
+                if (even && t + 2 < tiles) list_scales(buf ^ 1);
             }
         }
         // The four waves' results of the row.
         l = cross16_sum(l);
-        __syncthreads();                                    // (the list has been read)
         if (g4 == 0) {
             s_ml[0][wave][c16] = m;
             s_ml[1][wave][c16] = l;
@@ -359,7 +386,7 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
         if (c16 < a.g) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float *dst = &sm.out.o[wave][c16][32 * g4 + 8 * i];
+                float *dst = &s_out.o[wave][c16][32 * g4 + 8 * i];
                 *reinterpret_cast<f4 *>(dst) = f4{o[0][i], o[1][i], o[2][i], o[3][i]};
                 *reinterpret_cast<f4 *>(dst + 4) = f4{o[4][i], o[5][i], o[6][i], o[7][i]};
             }
@@ -376,7 +403,7 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
             for (int w = 0; w < 4; ++w) {
                 const float f = exp2f(s_ml[0][w][qi] - mu);
                 ls += f * s_ml[1][w][qi];
-                os += f * sm.out.o[w][qi][d];
+                os += f * s_out.o[w][qi][d];
             }
             if (whole) {
                 store_result(a, (size_t)r * a.g + qi, d, M, ls, os);

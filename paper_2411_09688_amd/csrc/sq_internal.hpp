@@ -395,7 +395,7 @@ struct DecodeQ8Args {
     int2 *info;                    // per row: first partial result, how many (0: the row is done)
     int B, H, L, C, sblocks;
     int per, g;                    // rows per (sequence, K/V head), query heads per row
-    int P, n_pages, max_pages;
+    int p_log, n_pages, max_pages; // tokens per page: 2^p_log
     float scale;                   // sm_scale * log2(e)
 };
 hipError_t launch_decode_q8(const DecodeQ8Args &a, hipStream_t s);

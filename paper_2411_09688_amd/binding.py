@@ -8,7 +8,6 @@ is no fallback: if the HIP library has not been built, importing it raises.
 from __future__ import annotations
 
 import ctypes as C
-import math
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -429,28 +428,30 @@ F8 = torch.float8_e4m3fn
 HEAD_DIM = 128
 
 
-def _here(t: Optional[torch.Tensor], shape, dtype, name, device):
-    """The pointer of a contiguous tensor of this shape, type and device."""
+# (A call checks up to a dozen tensors: as one expression each, 0.5 us apiece on the calling thread, a third of what the step costs
+# it otherwise.)
+def _here(t: Optional[torch.Tensor], n, dtype, name, device):
+    """The pointer of a contiguous tensor of n elements of this type on this device."""
     if t is None:
         return None
+    if t.dtype is dtype and t.numel() == n and t.is_contiguous() and t.get_device() == device:
+        return t.data_ptr()
     if t.get_device() != device:
         raise ValueError(f"{name} must be on the current device {device}, is on {t.device}")
-    if t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.numel() != math.prod(shape) or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous and hold {tuple(shape)}, got {tuple(t.shape)}")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous {dtype} of {n} elements, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
 
 
 def _head_rows(t: Optional[torch.Tensor], n, heads, name, device):
     """(pointer, elements from row to row) of f16 [n, heads, 128] whose rows may be apart (a part of a fused projection)."""
     if t is None:
         return None, 0
-    if t.get_device() != device or t.dtype != F16:
-        raise ValueError(f"{name} must be {F16} on the current device {device}, is {t.dtype} on {t.device}")
-    if t.shape != (n, heads, HEAD_DIM) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != HEAD_DIM):
-        raise ValueError(f"{name} must be [{n}, {heads}, {HEAD_DIM}] with contiguous rows, got {tuple(t.shape)}, strides {t.stride()}")
-    return t.data_ptr(), t.stride(0) if n > 1 else heads * HEAD_DIM
+    if t.shape == (n, heads, HEAD_DIM):
+        s = t.stride()
+        if (s[1] == HEAD_DIM or heads == 1) and s[2] == 1 and t.dtype is F16 and t.get_device() == device:
+            return t.data_ptr(), s[0] if n > 1 else heads * HEAD_DIM
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on the current device {device}, is on {t.device}")
+    raise ValueError(f"{name} must be {F16} [{n}, {heads}, {HEAD_DIM}] with contiguous rows, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
 
 
 class Rotary:
@@ -461,9 +462,9 @@ class Rotary:
         device = next((t.get_device() for t in self.tensors if t is not None), None)
         self.device = device
         for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-            _here(w, (HEAD_DIM,), F16, name, device)
+            _here(w, HEAD_DIM, F16, name, device)
         if cos_sin is not None:
-            _here(cos_sin, (cos_sin.shape[0], rot_dim // 2, 2), F32, "cos_sin", device)
+            _here(cos_sin, cos_sin.shape[0] * rot_dim, F32, "cos_sin", device)
         self.c = SqRotary(rot_dim, int(bool(interleaved)), cos_sin.shape[0] if cos_sin is not None else 0, float(eps),
                           _ptr(cos_sin), _ptr(q_weight), _ptr(k_weight))
         self.ref = C.byref(self.c)
@@ -482,8 +483,8 @@ class Cache:
         self.device, self.heads, self.sequences = K8.get_device(), H, page_table.shape[0]
         self.tensors = (K8, V8, k_scale, v_scale, page_table)
         p = [_here(t, s, ty, name, self.device) for t, s, ty, name in
-             ((K8, (n, H, P, HEAD_DIM), F8, "K8"), (V8, (n, H, P, HEAD_DIM), F8, "V8"), (k_scale, (n, H), F32, "k_scale"),
-              (v_scale, (n, H), F32, "v_scale"), (page_table, tuple(page_table.shape), I32, "page_table"))]
+             ((K8, n * H * P * HEAD_DIM, F8, "K8"), (V8, n * H * P * HEAD_DIM, F8, "V8"), (k_scale, n * H, F32, "k_scale"),
+              (v_scale, n * H, F32, "v_scale"), (page_table, self.sequences * page_table.shape[1], I32, "page_table"))]
         self.c = SqCache(P, n, page_table.shape[1], *p)
         self.ref = C.byref(self.c)
 
@@ -495,7 +496,7 @@ def make_cache(K8, V8, k_scale, v_scale, page_table) -> Cache:
 
 def _device_of(stream, *held):
     """The current device, which has to be the stream's and that of what the call was prepared with."""
-    device = torch.cuda.current_device()
+    device = torch._C._cuda_getDevice()
     if stream is not None and stream.device_index != device:
         raise ValueError(f"the stream belongs to device {stream.device_index}, the current device is {device}")
     for h in held:
@@ -504,58 +505,71 @@ def _device_of(stream, *held):
     return device
 
 
-def _for_sequences(cache, shape):
-    if cache is not None and (cache.heads != shape.H or cache.sequences != shape.B):
-        raise ValueError(f"the cache has {cache.heads} heads and pages of {cache.sequences} sequences, the shape {shape.H} and {shape.B}")
+def _for_sequences(cache, B, H):
+    if cache.heads != H or cache.sequences != B:
+        raise ValueError(f"the cache has {cache.heads} heads and pages of {cache.sequences} sequences, the shape {H} and {B}")
+
+
+def _raw_stream(stream, device):
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 def sq_head_norm_rotate(shape, G, rot, positions, q, k, v, q_out, k_out, v_out, stream=None):
     """q [B*Lq, H*G, 128], k, v [B*Lq, H, 128] (rows may be apart) -> q_out [B,H*G,Lq,128], k_out, v_out [B,H,Lq,128]."""
     dev = _device_of(stream, rot)
     n, H = shape.B * shape.Lq, shape.H
+    row = n * H * HEAD_DIM
     _check(lib().sq_head_norm_rotate(
-        C.byref(shape), int(G), rot.ref, _here(positions, (n,), I32, "positions", dev), *_head_rows(q, n, H * G, "q", dev),
-        *_head_rows(k, n, H, "k", dev), *_head_rows(v, n, H, "v", dev), _here(q_out, (n, H * G, HEAD_DIM), F16, "q_out", dev),
-        _here(k_out, (n, H, HEAD_DIM), F16, "k_out", dev), _here(v_out, (n, H, HEAD_DIM), F16, "v_out", dev), _stream(stream)))
+        C.byref(shape), G, rot.ref, _here(positions, n, I32, "positions", dev), *_head_rows(q, n, H * G, "q", dev),
+        *_head_rows(k, n, H, "k", dev), *_head_rows(v, n, H, "v", dev), _here(q_out, row * G, F16, "q_out", dev),
+        _here(k_out, row, F16, "k_out", dev), _here(v_out, row, F16, "v_out", dev), _raw_stream(stream, dev)))
 
 
 def sq_kv_quantize(shape, K, V, perm, K8, V8, k_scale, v_scale, stream=None):
     dev = _device_of(stream)
-    rows, scales = (shape.B, shape.H, shape.L, HEAD_DIM), (shape.B, shape.H, (shape.L + 63) // 64)
+    bh, L = shape.B * shape.H, shape.L
+    rows, scales = bh * L, bh * ((L + 63) // 64)
+    n = rows * HEAD_DIM
     _check(lib().sq_kv_quantize(
-        C.byref(shape), _here(K, rows, F16, "K", dev), _here(V, rows, F16, "V", dev), _here(perm, rows[:3], I32, "perm", dev),
-        _here(K8, rows, F8, "K8", dev), _here(V8, rows, F8, "V8", dev), _here(k_scale, scales, F32, "k_scale", dev),
-        _here(v_scale, scales, F32, "v_scale", dev), _stream(stream)))
+        C.byref(shape), _here(K, n, F16, "K", dev), _here(V, n, F16, "V", dev), _here(perm, rows, I32, "perm", dev),
+        _here(K8, n, F8, "K8", dev), _here(V8, n, F8, "V8", dev), _here(k_scale, scales, F32, "k_scale", dev),
+        _here(v_scale, scales, F32, "v_scale", dev), _raw_stream(stream, dev)))
 
 
 def sq_cache_append(shape, G, rot, cache, seq_len, positions, q, k, v, q_out, cu_tokens=None, stream=None):
     """k, v [n_tokens, H, 128], q [n_tokens, H*G, 128] or None (rows may be apart); cu_tokens None: Lq rows per sequence."""
     dev = _device_of(stream, rot, cache)
-    _for_sequences(cache, shape)
-    n, H = k.shape[0], shape.H
+    B, H, n = shape.B, shape.H, k.shape[0]
+    _for_sequences(cache, B, H)
     _check(lib().sq_cache_append(
-        C.byref(shape), int(G), rot.ref, cache.ref, n, _here(cu_tokens, (shape.B + 1,), I32, "cu_tokens", dev),
-        _here(seq_len, (shape.B,), I32, "seq_len", dev), _here(positions, (n,), I32, "positions", dev),
-        *_head_rows(q, n, H * G, "q", dev), *_head_rows(k, n, H, "k", dev), *_head_rows(v, n, H, "v", dev),
-        _here(q_out, (n, H * G, HEAD_DIM), F16, "q_out", dev), _stream(stream)))
+        C.byref(shape), G, rot.ref, cache.ref, n, _here(cu_tokens, B + 1, I32, "cu_tokens", dev),
+        _here(seq_len, B, I32, "seq_len", dev), _here(positions, n, I32, "positions", dev), *_head_rows(q, n, H * G, "q", dev),
+        *_head_rows(k, n, H, "k", dev), *_head_rows(v, n, H, "v", dev), _here(q_out, n * H * G * HEAD_DIM, F16, "q_out", dev),
+        _raw_stream(stream, dev)))
 
 
 def sq_sparse_attn_decode_q8(shape, one_set, q, K8, V8, k_scale, v_scale, ranges, n_ranges, n_keys, cache, seq_len, out, lse, ws,
                              stream=None):
     """Lq of the shape: query heads per K/V head.  The seven tensors of the fixed context may be None, or cache and seq_len."""
     dev = _device_of(stream, cache)
-    _for_sequences(cache, shape)
     B, H, L, Lq = shape.B, shape.H, shape.L, shape.Lq
-    rows = B * H * (1 if one_set else Lq)
-    codes, scales = (H, L, HEAD_DIM), (H, (L + 63) // 64)
-    if ws is not None and ws.get_device() != dev:
-        raise ValueError(f"the workspace must be on the current device {dev}, is on {ws.device}")
+    if cache is not None:
+        _for_sequences(cache, B, H)
+    heads = B * H * Lq
+    rows = B * H if one_set else heads
+    codes, scales, n = H * L * HEAD_DIM, H * ((L + 63) // 64), heads * HEAD_DIM
+    if ws is None:
+        wp, wn = None, 0
+    else:
+        if ws.get_device() != dev:
+            raise ValueError(f"the workspace must be on the current device {dev}, is on {ws.device}")
+        wp, wn = ws.data_ptr(), ws.nbytes
     _check(lib().sq_sparse_attn_decode_q8(
-        C.byref(shape), int(bool(one_set)), _here(q, (B, H * Lq, HEAD_DIM), F16, "q", dev), _here(K8, codes, F8, "K8", dev),
-        _here(V8, codes, F8, "V8", dev), _here(k_scale, scales, F32, "k_scale", dev), _here(v_scale, scales, F32, "v_scale", dev),
-        _here(ranges, (rows, shape.C, 2), I32, "ranges", dev), _here(n_ranges, (rows,), I32, "n_ranges", dev),
-        _here(n_keys, (rows,), I32, "n_keys", dev), None if cache is None else cache.ref, _here(seq_len, (B,), I32, "seq_len", dev),
-        _here(out, (B, H * Lq, HEAD_DIM), F16, "out", dev), _here(lse, (B, H * Lq), F32, "lse", dev), *_ws_args(ws), _stream(stream)))
+        C.byref(shape), 1 if one_set else 0, _here(q, n, F16, "q", dev), _here(K8, codes, F8, "K8", dev), _here(V8, codes, F8, "V8", dev),
+        _here(k_scale, scales, F32, "k_scale", dev), _here(v_scale, scales, F32, "v_scale", dev),
+        _here(ranges, rows * shape.C * 2, I32, "ranges", dev), _here(n_ranges, rows, I32, "n_ranges", dev),
+        _here(n_keys, rows, I32, "n_keys", dev), None if cache is None else cache.ref, _here(seq_len, B, I32, "seq_len", dev),
+        _here(out, n, F16, "out", dev), _here(lse, heads, F32, "lse", dev), wp, wn, _raw_stream(stream, dev)))
 
 
 def sq_probe_stream_read(buf: torch.Tensor, sink: torch.Tensor, workgroups: int, nbytes: Optional[int] = None,

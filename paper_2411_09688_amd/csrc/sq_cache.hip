@@ -90,15 +90,21 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryA
     const int tid = threadIdx.x, j = tid & 15, g = tid >> 4;
     __shared__ int s_scan[6];
     __shared__ uint32_t s_max[4];
-    if ((int)blockIdx.x >= a.kv_blocks) {                   // query rows
-        const long long r = (long long)(blockIdx.x - a.kv_blocks) * 16 + g;
-        const int token = (int)(r / a.Hq), h = (int)(r - (long long)token * a.Hq);
+    if ((int)blockIdx.x >= a.kv_blocks) {                   // query rows: four heads of 16 tokens
+        const int at = blockIdx.x - a.kv_blocks, blocks = (a.n_tokens + 15) / 16, quad = at / blocks;
+        const int token = (at - quad * blocks) * 16 + g;
         if (token >= a.n_tokens) return;
         if (a.cu && (token < a.cu[0] || token >= a.cu[a.B])) return;
-        const LanePieces lp = lane_pieces(j, ra.rot_dim, ra.adjacent != 0);
-        float cs[8];
-        load_turn(cs, ra, ra.rot_dim ? a.positions[token] : 0, j, lp.turns);
-        store_turned_row(a.q_out + r * D, a.q + (size_t)token * a.q_stride + (size_t)h * D, ra.weight[0], ra, lp, cs);
+        TurnRows rows;
+        rows.n = min(ROWS_AT_ONCE, a.Hq - quad * ROWS_AT_ONCE);
+#pragma unroll
+        for (int i = 0; i < ROWS_AT_ONCE; ++i) {
+            const int h = min(quad * ROWS_AT_ONCE + i, a.Hq - 1);
+            rows.kind[i] = 0;
+            rows.src[i] = a.q + (size_t)token * a.q_stride + (size_t)h * D;
+            rows.dst[i] = a.q_out + ((size_t)token * a.Hq + h) * D;
+        }
+        turn_rows(rows, ra, ra.rot_dim ? a.positions[token] : 0, j);
         return;
     }
     const int hv = blockIdx.x % (2 * a.H), unit = blockIdx.x / (2 * a.H);
@@ -176,7 +182,7 @@ hipError_t launch_cache_append(AppendArgs a, const RotaryArgs &ra, hipStream_t s
         a.per_seq = (a.Lq + a.P - 2) / a.P + 1;
         units = (long long)a.B * a.per_seq;
     }
-    const long long kv = units * a.H * 2, q = a.q ? ((long long)a.n_tokens * a.Hq + 15) / 16 : 0;
+    const long long kv = units * a.H * 2, q = a.q ? ((long long)a.n_tokens + 15) / 16 * ((a.Hq + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE) : 0;
     if (kv + q > 0x7fffffffll) return hipErrorInvalidConfiguration;
     if (kv + q == 0) return hipSuccess;
     a.kv_blocks = (int)kv;

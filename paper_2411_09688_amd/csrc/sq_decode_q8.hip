@@ -12,6 +12,8 @@
 //                       (16 significant bits, and fp32's range: a scale may be anything)
 // The order of the 32 keys is the same in both products: a lane's scores of S^T are the operand that P^T wants of it.  V is read row
 // by row, 8 bytes a lane, and turned in registers (4 x 4 byte transposes).
+#include <type_traits>
+
 #include "sq_e4m3.hpp"
 #include "sq_internal.hpp"
 
@@ -19,6 +21,7 @@ namespace sq {
 
 namespace {
 
+typedef int i2v __attribute__((ext_vector_type(2)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 
@@ -28,9 +31,12 @@ constexpr int O_STRIDE = 132;
 constexpr int GROUP = 64;                    // ranges that a wave holds at a time
 constexpr int MAX_GROUPS = SELECT_MAX_C / GROUP;
 
-struct KeyList {                             // 64 keys of a wave: where they stand (bytes from the tensor's first) and their scales
-    unsigned long long at[64];               // (0 for a slot without a key: the first row, which there is)
-    float ks[64], vs[64];                    // ks: times the softmax's
+// 64 keys of a wave: where they stand (bytes from the first of the fixed context's head, or of the pool's) and their scales.
+// Offsets of 32 bits go straight into the loads, beside a scalar base: a pool of more than 4 GB takes those of 64 (WIDE).
+template <bool WIDE>
+struct KeyList {
+    std::conditional_t<WIDE, unsigned long long, uint32_t> at[64];   // (0 for a slot without a key: the first row, which there is)
+    float ks[64], vs[64];                                            // ks: times the softmax's
 };
 struct WaveOut {                             // the four waves' results of a row
     float o[4][16][O_STRIDE];
@@ -40,14 +46,26 @@ struct RowTiles {
     int nf, nu, tf, total;                   // fixed and user keys, tiles of fixed keys, all tiles (at least one)
 };
 
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+template <typename T>
+using global = const __attribute__((address_space(1))) T *;
+template <typename T>
+__device__ __forceinline__ global<T> uniform(const T *p)
+{
+    const unsigned long long v = reinterpret_cast<unsigned long long>(p);
+    const uint32_t lo = uniform((int)(uint32_t)v), hi = uniform((int)(uint32_t)(v >> 32));
+    return reinterpret_cast<global<T>>((unsigned long long)hi << 32 | lo);
+}
+
+__device__ __forceinline__ RowTiles tiles_of(int nf, int nu)
+{
+    const int tf = (nf + QT - 1) / QT;
+    return RowTiles{nf, nu, tf, max(1, tf + (nu + QT - 1) / QT)};
+}
 __device__ __forceinline__ RowTiles row_tiles(const DecodeQ8Args &a, int r)
 {
-    RowTiles t;
-    t.nf = a.ranges ? min(max(a.n_keys[r], 0), a.L) : 0;
-    t.nu = a.seq_len ? min(max(a.seq_len[r / (a.H * a.per)], 0), a.max_pages << a.p_log) : 0;
-    t.tf = (t.nf + QT - 1) / QT;
-    t.total = max(1, t.tf + (t.nu + QT - 1) / QT);
-    return t;
+    return tiles_of(a.ranges ? min(max(a.n_keys[r], 0), a.L) : 0,
+                    a.seq_len ? min(max(a.seq_len[r / (a.H * a.per)], 0), a.max_pages << a.p_log) : 0);
 }
 
 __device__ __forceinline__ int block_exclusive(int v, int tid, int *s_w /*[4]*/, int &total)
@@ -58,7 +76,7 @@ __device__ __forceinline__ int block_exclusive(int v, int tid, int *s_w /*[4]*/,
     __syncthreads();
     int ex = inc - v;
     for (int w = 0; w < (tid >> 6); ++w) ex += s_w[w];
-    total = s_w[0] + s_w[1] + s_w[2] + s_w[3];
+    total = uniform(s_w[0] + s_w[1] + s_w[2] + s_w[3]);
     return ex;
 }
 
@@ -112,43 +130,62 @@ __device__ __forceinline__ void wave_lds_sync()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// The thread's index as a value that the compiler cannot move: what is computed from it is computed where it stands, and takes no
+// registers elsewhere.
+__device__ __forceinline__ int thread_here()
+{
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
+
+template <bool WIDE>
 __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g4 = lane >> 4;
+    typedef decltype(KeyList<WIDE>::at[0] + 0) offset_t;
     __shared__ __align__(16) WaveOut s_out;
-    __shared__ __align__(16) KeyList s_list[4][2];
+    __shared__ __align__(16) KeyList<WIDE> s_list[4][2];
+    __shared__ __align__(16) offset_t s_none[QT];           // where a wave reads ahead behind its last tile: the first row, a line or two
     __shared__ int s_delta[4][64];
     __shared__ int s_group[MAX_GROUPS];
-    __shared__ int s_w[4], s_found[2];
+    __shared__ int s_w[4], s_found[4];
     __shared__ float s_ml[2][4][16];
 
+    const int wave = uniform(threadIdx.x >> 6);
+
     // This workgroup's share of the tiles.  Workgroups go round the 8 XCDs: each XCD takes consecutive shares.
-    const int R = a.B * a.H * a.per;
+    const int R = a.B * a.H * a.per, tid = threadIdx.x;
+    if (tid < QT) s_none[tid] = 0;
     const int each = (R + 255) / 256, i_lo = min(R, tid * each), i_hi = min(R, i_lo + each);
     int mine = 0, all;
     for (int i = i_lo; i < i_hi; ++i) mine += row_tiles(a, dealt_row(a, i)).total;
     int before = block_exclusive(mine, tid, s_w, all);
-    const int shares = min((int)gridDim.x, (all + 3) / 4);
+    const int shares = min((int)gridDim.x, (all + 3) / 4);      // (at least a tile for each wave)
     const int per = (all + shares - 1) / shares, per_xcd = (shares + 7) / 8;
     const int share = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per_xcd || (long long)share * per >= all) return;
     const int t0 = share * per, t1 = min(all, t0 + per);
     if (before <= t0 && t0 < before + mine) {
         int i = i_lo;
+        RowTiles rt;
         for (;; ++i) {
-            const int n = row_tiles(a, dealt_row(a, i)).total;
-            if (t0 < before + n) break;
-            before += n;
+            rt = row_tiles(a, dealt_row(a, i));
+            if (t0 < before + rt.total) break;
+            before += rt.total;
         }
         s_found[0] = i;
         s_found[1] = before;
+        s_found[2] = rt.nf;
+        s_found[3] = rt.nu;
     }
     __syncthreads();
-    int ri = s_found[0], row_start = s_found[1];
+    // (a row's numbers are the same in every lane: known to be, they take scalar registers, and addresses a scalar base)
+    int ri = uniform(s_found[0]), row_start = uniform(s_found[1]);
+    RowTiles rt = tiles_of(uniform(s_found[2]), uniform(s_found[3]));
 
-    for (; row_start < t1; ++ri) {
+    for (;;) {
+        const int lane = thread_here() & 63, c16 = lane & 15, g4 = lane >> 4;
         const int r = dealt_row(a, ri);
-        const RowTiles rt = row_tiles(a, r);
         const int bh = r / a.per, h = bh % a.H, b = bh / a.H;
         const int lo = max(t0 - row_start, 0), hi = min(t1 - row_start, rt.total);
         // q^T as the second operand of S^T: lane = query column c16, dimensions 32 g4 + 8 s ..
@@ -164,37 +201,44 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
         for (int i = 0; i < 8; ++i) o[i] = f4{0.f, 0.f, 0.f, 0.f};
 
         // The row's ranges in groups of 64: how many keys lie before each group, for a wave to find its first.
-        const int2 *rg = reinterpret_cast<const int2 *>(a.ranges) + (size_t)r * a.C;
-        const int nr = lo < rt.tf ? min(max(a.n_ranges[r], 0), a.C) : 0, groups = (nr + GROUP - 1) / GROUP;
-        auto range_of = [&](int gi) {                       // this lane's range of a group; (0, 0) behind the last
-            const int i = gi * GROUP + lane;
-            int2 e = i < nr ? rg[i] : int2{0, 0};
-            e.x = min(max(e.x, -MAX_L), MAX_L);
-            e.y = min(max(e.y, 0), a.L);
-            return e;
+        const global<i2v> rg = uniform(reinterpret_cast<const i2v *>(a.ranges) + (size_t)r * a.C);
+        const bool has_fixed = lo < rt.tf;
+        // (a wave's first group is read beside the number of ranges, not behind it)
+        auto range_of = [&](int gi) { return rg[min(gi * GROUP + lane, a.C - 1)]; };   // as it stands in memory: see in_bounds
+        i2v own = {0, 0};
+        if (has_fixed) own = range_of(wave);
+        const int nr = uniform(has_fixed ? min(max(a.n_ranges[r], 0), a.C) : 0), groups = (nr + GROUP - 1) / GROUP;
+        auto in_bounds = [&](i2v e, int gi) {               // a lane's range of a group; (0, 0) behind the last
+            const bool ok = gi * GROUP + lane < nr;
+            return i2v{min(max(e.x, -MAX_L), MAX_L), ok ? min(max(e.y, 0), a.L) : 0};
         };
         for (int gi = wave; gi < groups; gi += 4) {
+            if (gi > wave) own = range_of(gi);
             // (counts that sum to more than a row can have are cut, far from overflow)
-            const int n = min(wave_sum_i(range_of(gi).y), MAX_L);
+            const int n = min(wave_sum_i(in_bounds(own, gi).y), MAX_L);
             if (lane == 0) s_group[gi] = n;
         }
         __syncthreads();
 
         // This wave's quarter of the tiles: fixed keys, then the user's, 64 keys listed at a time and a step ahead.
         const int w0 = lo + (int)((long long)(hi - lo) * wave / 4), w1 = lo + (int)((long long)(hi - lo) * (wave + 1) / 4);
-        for (int phase = 0; phase < 2; ++phase) {
+        int phase = 0;
+#pragma clang loop unroll(disable)
+        for (; phase < 2; ++phase) {
+            asm volatile("" : "+s"(phase));                 // (one copy of the loop below for both)
             const bool fixed = phase == 0;
             const int f0 = fixed ? w0 : max(w0, rt.tf) - rt.tf;          // first tile of the phase, and how many
             const int tiles = (fixed ? min(w1, rt.tf) : w1 - rt.tf) - f0;
             if (tiles <= 0) continue;
-            const uint8_t *Kb = (fixed ? a.K8 : a.cK) + 32 * g4, *Vb = (fixed ? a.V8 : a.cV) + 8 * c16;
-            const float *kscale = fixed ? a.ks : a.cks, *vscale = fixed ? a.vs : a.cvs;
+            const size_t head = fixed ? (size_t)h * a.L * D : 0;
+            const global<uint8_t> Kb = uniform((fixed ? a.K8 : a.cK) + head), Vb = uniform((fixed ? a.V8 : a.cV) + head);
+            const global<float> kscale = uniform(fixed ? a.ks : a.cks), vscale = uniform(fixed ? a.vs : a.cvs);
+            const global<int32_t> pages = uniform(a.page_table + (size_t)b * a.max_pages);
             int p = f0 * QT;                                // the next position to list
             int end;                                        // where the row's keys end
             // ranges in hand: group gi, its lanes' first positions, where it ends; the group behind it is on its way
             int gi = 0, first = 0, ends = 0;
-            int2 e = {0, 0}, e_next = {0, 0};
-            int page = -1;                                  // user: the page of position p + lane, read ahead
+            i2v e = {0, 0}, e_next = {0, 0};                 // user: e.x is the page of position p + lane, read ahead
             if (fixed) {
                 int sum[MAX_GROUPS / 64], at = 0;
                 int total = 0;
@@ -206,26 +250,28 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
                 const int inc = wave_inclusive_scan(total, lane);
                 end = min(rt.nf, __builtin_amdgcn_readlane(inc, 63));
                 at = inc - total;
-                int here = 0, start = 0;                    // groups that end at or before p; the last start at or before it
+                int here = 0, start = 0;                    // groups that end at or before p, and their keys
 #pragma unroll
                 for (int i = 0; i < MAX_GROUPS / 64; ++i) {
                     const bool passed = 4 * lane + i < groups && at + sum[i] <= p;
                     here += __popcll(__ballot(passed));
-                    start = max(start, passed ? at + sum[i] : 0);
+                    start += passed ? sum[i] : 0;
                     at += sum[i];
                 }
                 gi = min(here, max(groups - 1, 0));
-                // (groups pass in order, so the last passed end is the found group's start)
-#pragma unroll
-                for (int k = 32; k > 0; k >>= 1) start = max(start, __shfl_xor(start, k));
-                e = range_of(gi);
-                e_next = range_of(gi + 1);
+                start = wave_sum_i(start);
+                gi = uniform(gi);
+                if (groups > 0) {
+                    e = in_bounds(range_of(gi), gi);
+                    e_next = range_of(gi + 1);
+                }
                 const int c = wave_inclusive_scan(e.y, lane);
                 first = start + c - e.y;
-                ends = start + __builtin_amdgcn_readlane(c, 63);
+                ends = uniform(start + __builtin_amdgcn_readlane(c, 63));
             } else {
                 end = rt.nu;
-                if (p + lane < end) page = a.page_table[(size_t)b * a.max_pages + ((p + lane) >> a.p_log)];
+                e.x = -1;
+                if (end > 0) e.x = pages[min(p + lane, end - 1) >> a.p_log];
             }
 
             float ks = 0.0f, vs = 0.0f;
@@ -233,7 +279,7 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
             // Lists positions p .. p + 63 and starts to read their scales.
             auto list = [&](int buf) {
                 bool ok = p + lane < end;
-                unsigned long long at = 0ull;
+                offset_t at = 0;
                 int sc = 0;
                 if (fixed) {
                     s_delta[wave][lane] = SENTINEL;
@@ -242,12 +288,12 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
                         const int from = max(first, p), to = min(first + e.y, p + 64);
                         if (from < to) s_delta[wave][from - p] = e.x - first;
                         if (ends >= p + 64 || gi + 1 >= groups) break;
-                        e = e_next;
-                        ++gi;
+                        gi = uniform(gi + 1);
+                        e = in_bounds(e_next, gi);
                         e_next = range_of(gi + 1);
                         const int c = wave_inclusive_scan(e.y, lane);
                         first = ends + c - e.y;
-                        ends = min(ends + __builtin_amdgcn_readlane(c, 63), MAX_L + MAX_L);
+                        ends = uniform(min(ends + __builtin_amdgcn_readlane(c, 63), MAX_L + MAX_L));
                     }
                     wave_lds_sync();
                     const unsigned long long marks = __ballot(s_delta[wave][lane] != SENTINEL) & (~0ull >> (63 - lane));
@@ -255,17 +301,17 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
                     if (ok) {
                         const int d = s_delta[wave][63 - __clzll((long long)marks)];
                         const int key = min(max(p + lane + d, 0), a.L - 1);
-                        at = ((unsigned long long)h * a.L + key) * D;
+                        at = (offset_t)key * D;
                         sc = h * a.sblocks + (key >> 6);
                     }
                 } else {
                     const int t = p + lane;
-                    ok = ok && page >= 0 && page < a.n_pages;
+                    ok = ok && e.x >= 0 && e.x < a.n_pages;
                     if (ok) {
-                        sc = page * a.H + h;
-                        at = (((unsigned long long)sc << a.p_log) + (t & ((1 << a.p_log) - 1))) * D;
+                        sc = e.x * a.H + h;
+                        at = (((offset_t)sc << a.p_log) + (t & ((1 << a.p_log) - 1))) * D;
                     }
-                    if (t + 64 < end) page = a.page_table[(size_t)b * a.max_pages + ((t + 64) >> a.p_log)];
+                    if (end > 0) e.x = pages[min(t + 64, end - 1) >> a.p_log];
                 }
                 ks = vs = 0.0f;
                 if (ok) {
@@ -285,17 +331,18 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
             u4v k[2][2];                                    // keys c16 and 16 + c16, dimensions 32 g4 ..
             u2v v[8];                                       // keys 4 g4 .. and 16 + 4 g4 .., dimensions 8 c16 ..
             auto load_k = [&](int t) {
-                const unsigned long long *at = s_list[wave][(t >> 1) & 1].at + (t & 1) * QT;
-                const uint8_t *k0 = Kb + at[c16], *k1 = Kb + at[16 + c16];
-                k[0][0] = *reinterpret_cast<const u4v *>(k0);
-                k[0][1] = *reinterpret_cast<const u4v *>(k0 + 16);
-                k[1][0] = *reinterpret_cast<const u4v *>(k1);
-                k[1][1] = *reinterpret_cast<const u4v *>(k1 + 16);
+                const auto *at = t < tiles ? s_list[wave][(t >> 1) & 1].at + (t & 1) * QT : s_none;
+                const offset_t k0 = at[c16] + 32 * g4, k1 = at[16 + c16] + 32 * g4;
+                k[0][0] = *reinterpret_cast<global<u4v>>(Kb + k0);
+                k[0][1] = *reinterpret_cast<global<u4v>>(Kb + k0 + 16);
+                k[1][0] = *reinterpret_cast<global<u4v>>(Kb + k1);
+                k[1][1] = *reinterpret_cast<global<u4v>>(Kb + k1 + 16);
             };
             auto load_v = [&](int t) {
-                const unsigned long long *at = s_list[wave][(t >> 1) & 1].at + (t & 1) * QT;
+                const auto *at = (t < tiles ? s_list[wave][(t >> 1) & 1].at + (t & 1) * QT : s_none) + 4 * g4;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const u2v *>(Vb + at[(i < 4 ? 0 : 16) + 4 * g4 + (i & 3)]);
+                for (int i = 0; i < 8; ++i)
+                    v[i] = *reinterpret_cast<global<u2v>>(Vb + (offset_t)(at[(i < 4 ? 0 : 12) + i] + 8 * c16));
             };
 
             list(0);
@@ -317,7 +364,7 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
                         const u4v x = k[u][s >> 1];
                         acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(s & 1 ? codes_f16(x.z, x.w) : codes_f16(x.x, x.y), qf[s], acc[u], 0, 0, 0);
                     }
-                if (t + 1 < tiles) load_k(t + 1);            // (as soon as the scores have used this tile's)
+                load_k(t + 1);                               // (as soon as the scores have used this tile's)
                 float s[8];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
@@ -363,7 +410,6 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
                     transpose4(w[i][0], w[i][1], w[i][2], w[i][3]);
                     transpose4(w[i][4], w[i][5], w[i][6], w[i][7]);
                 }
-                if (t + 1 < tiles) load_v(t + 1);
                 if (__any(alpha != 1.0f)) {                  // (the maximum rarely moves behind the first tiles)
 #pragma unroll
                     for (int dt = 0; dt < 8; ++dt) o[dt] *= alpha;
@@ -374,10 +420,13 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
                     o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi8, o[dt], 0, 0, 0);
                     o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo8, o[dt], 0, 0, 0);
                 }
+                load_v(t + 1);
                 if (even && t + 2 < tiles) list_scales(buf ^ 1);
             }
         }
         // The four waves' results of the row.
+        {
+        const int tid = thread_here(), lane = tid & 63, c16 = lane & 15, g4 = lane >> 4;
         l = cross16_sum(l);
         if (g4 == 0) {
             s_ml[0][wave][c16] = m;
@@ -401,7 +450,7 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
             float ls = 0.0f, os = 0.0f;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const float f = exp2f(s_ml[0][w][qi] - mu);
+                const float f = __builtin_amdgcn_exp2f(s_ml[0][w][qi] - mu);
                 ls += f * s_ml[1][w][qi];
                 os += f * s_out.o[w][qi][d];
             }
@@ -420,8 +469,13 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
             const int last = (row_start + rt.total - 1) / per;
             a.info[r] = int2{slot, whole ? 0 : last - share + 1};
         }
+        }
         __syncthreads();
         row_start += rt.total;
+        if (row_start >= t1) break;
+        ++ri;
+        const RowTiles next = row_tiles(a, dealt_row(a, ri));
+        rt = tiles_of(uniform(next.nf), uniform(next.nu));
     }
 }
 
@@ -479,11 +533,13 @@ __global__ __launch_bounds__(256) void decode_q8_merge_kernel(DecodeQ8Args a)
 
 hipError_t launch_decode_q8(const DecodeQ8Args &a, hipStream_t s)
 {
+    const bool wide = ((size_t)a.n_pages * a.H << a.p_log) * D > (1ull << 32);
+    auto *kernel = wide ? decode_q8_kernel<true> : decode_q8_kernel<false>;
     hipEvent_t ev0, ev1;
     if (profile_pair(&ev0, &ev1))
-        hipExtLaunchKernelGGL(decode_q8_kernel, dim3(Q8_GRID), dim3(256), 0, s, ev0, ev1, 0, a);
+        hipExtLaunchKernelGGL(kernel, dim3(Q8_GRID), dim3(256), 0, s, ev0, ev1, 0, a);
     else
-        hipLaunchKernelGGL(decode_q8_kernel, dim3(Q8_GRID), dim3(256), 0, s, a);
+        hipLaunchKernelGGL(kernel, dim3(Q8_GRID), dim3(256), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(decode_q8_merge_kernel, dim3((unsigned)(a.B * a.H * a.per * a.g)), dim3(256), 0, s, a);

@@ -87,32 +87,59 @@ __device__ __forceinline__ void norm_rotate(T (&e)[8], const T (&w)[8], bool nor
 }
 
 template <typename T>
-__device__ __forceinline__ void load_pieces(T (&e)[8], const _Float16 *row, const LanePieces &lp)
+__device__ __forceinline__ void widen(T (&e)[8], h4 x, h4 y)
 {
-    const h4 x = *reinterpret_cast<const h4 *>(row + lp.a), y = *reinterpret_cast<const h4 *>(row + lp.b);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         e[i] = (T)(float)x[i];
         e[i + 4] = (T)(float)y[i];
     }
 }
-
-// A query or key row to f16, fp32 arithmetic.
-__device__ __forceinline__ void store_turned_row(_Float16 *dst, const _Float16 *src, const _Float16 *weight, const RotaryArgs &ra,
-                                                 const LanePieces &lp, const float (&cs)[8])
+template <typename T>
+__device__ __forceinline__ void load_pieces(T (&e)[8], const _Float16 *row, const LanePieces &lp)
 {
-    float e[8], w[8] = {};
-    load_pieces(e, src, lp);
-    if (weight) load_pieces(w, weight, lp);
-    norm_rotate<float>(e, w, weight != nullptr, ra.eps, cs, lp.turns, ra.adjacent != 0);
-    h4 x, y;
+    widen(e, *reinterpret_cast<const h4 *>(row + lp.a), *reinterpret_cast<const h4 *>(row + lp.b));
+}
+
+// Up to four heads of one token by 16 lanes, fp32 arithmetic, rounded to f16 once; kind 0: query, 1: key, 2: value (copied).  All of
+// the rows are read before the first is turned, and the token's cosines and sines once for all of them.
+constexpr int ROWS_AT_ONCE = 4;
+struct TurnRows {
+    const _Float16 *src[ROWS_AT_ONCE];
+    _Float16 *dst[ROWS_AT_ONCE];
+    int kind[ROWS_AT_ONCE];
+    int n;
+};
+__device__ __forceinline__ void turn_rows(const TurnRows &t, const RotaryArgs &ra, int position, int j)
+{
+    const LanePieces lp = lane_pieces(j, ra.rot_dim, ra.adjacent != 0);
+    h4 x[ROWS_AT_ONCE], y[ROWS_AT_ONCE];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[i] = (_Float16)e[i];
-        y[i] = (_Float16)e[i + 4];
-    }
-    *reinterpret_cast<h4 *>(dst + lp.a) = x;
-    *reinterpret_cast<h4 *>(dst + lp.b) = y;
+    for (int i = 0; i < ROWS_AT_ONCE; ++i)
+        if (i < t.n) {
+            x[i] = *reinterpret_cast<const h4 *>(t.src[i] + lp.a);
+            y[i] = *reinterpret_cast<const h4 *>(t.src[i] + lp.b);
+        }
+    float cs[8];
+    load_turn(cs, ra, position, j, lp.turns && t.kind[0] != 2);   // (values come last)
+#pragma unroll
+    for (int i = 0; i < ROWS_AT_ONCE; ++i)
+        if (i < t.n) {
+            if (t.kind[i] != 2) {
+                const _Float16 *weight = ra.weight[t.kind[i]];
+                float e[8], w[8] = {};
+                widen(e, x[i], y[i]);
+                if (weight) load_pieces(w, weight, lp);
+                norm_rotate<float>(e, w, weight != nullptr, ra.eps, cs, lp.turns, ra.adjacent != 0);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    x[i][c] = (_Float16)e[c];
+                    y[i][c] = (_Float16)e[c + 4];
+                }
+            }
+            *reinterpret_cast<h4 *>(t.dst[i] + lp.a) = x[i];
+            *reinterpret_cast<h4 *>(t.dst[i] + lp.b) = y[i];
+        }
 }
 
 }  // namespace sq

@@ -7,34 +7,32 @@
 
 namespace sq {
 
-__global__ __launch_bounds__(256) void head_rows_kernel(HeadRows hr, RotaryArgs ra, long long rows)
+// A workgroup takes 16 consecutive tokens, 16 lanes each, and four heads: a head's rows of consecutive tokens lie side by side in the
+// output.
+__global__ __launch_bounds__(256) void head_rows_kernel(HeadRows hr, RotaryArgs ra, int tokens)
 {
-    const int j = threadIdx.x & 15;
-    const long long r = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
-    if (r >= rows) return;
-    const int heads = hr.n[0] + hr.n[1] + hr.n[2];
-    const long long token = r / heads;
-    int h = (int)(r - token * heads);
-    const int part = h < hr.n[0] ? 0 : h < hr.n[0] + hr.n[1] ? 1 : 2;
-    h -= part == 0 ? 0 : part == 1 ? hr.n[0] : hr.n[0] + hr.n[1];
-    const long long b = token / hr.Lq, t = token - b * hr.Lq;
-    const _Float16 *src = hr.src[part] + token * hr.stride[part] + (size_t)h * D;
-    _Float16 *dst = hr.dst[part] + ((b * hr.n[part] + h) * hr.Lq + t) * D;
-    if (part == 2) {
-        *reinterpret_cast<u4v *>(dst + 8 * j) = *reinterpret_cast<const u4v *>(src + 8 * j);
-        return;
+    const int j = threadIdx.x & 15, token = blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (token >= tokens) return;
+    const int b = token / hr.Lq, t = token - b * hr.Lq, heads = hr.n[0] + hr.n[1] + hr.n[2];
+    TurnRows rows;
+    rows.n = min(ROWS_AT_ONCE, heads - (int)blockIdx.y * ROWS_AT_ONCE);
+#pragma unroll
+    for (int i = 0; i < ROWS_AT_ONCE; ++i) {
+        int h = min((int)blockIdx.y * ROWS_AT_ONCE + i, heads - 1);
+        const int part = h < hr.n[0] ? 0 : h < hr.n[0] + hr.n[1] ? 1 : 2;
+        h -= part == 0 ? 0 : part == 1 ? hr.n[0] : hr.n[0] + hr.n[1];
+        rows.kind[i] = part;
+        rows.src[i] = hr.src[part] + token * hr.stride[part] + (size_t)h * D;
+        rows.dst[i] = hr.dst[part] + (((size_t)b * hr.n[part] + h) * hr.Lq + t) * D;
     }
-    const LanePieces lp = lane_pieces(j, ra.rot_dim, ra.adjacent != 0);
-    float cs[8];
-    load_turn(cs, ra, ra.rot_dim ? hr.positions[token] : 0, j, lp.turns);
-    store_turned_row(dst, src, ra.weight[part], ra, lp, cs);
+    turn_rows(rows, ra, ra.rot_dim ? hr.positions[token] : 0, j);
 }
 
 hipError_t launch_head_rows(const HeadRows &hr, const RotaryArgs &ra, int tokens, hipStream_t s)
 {
-    const long long rows = (long long)tokens * (hr.n[0] + hr.n[1] + hr.n[2]);
-    if (rows == 0) return hipSuccess;
-    hipLaunchKernelGGL(head_rows_kernel, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, s, hr, ra, rows);
+    const int heads = hr.n[0] + hr.n[1] + hr.n[2];
+    hipLaunchKernelGGL(head_rows_kernel, dim3((unsigned)((tokens + 15) / 16), (unsigned)((heads + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE)), dim3(256),
+                       0, s, hr, ra, tokens);
     return hipGetLastError();
 }
 

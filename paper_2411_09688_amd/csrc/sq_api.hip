@@ -1700,7 +1700,7 @@ int check_rows(const char *fn, const char *name, const void *p, int64_t stride, 
 int check_group(const char *fn, const sq_shape_t *sh, int G, long long tokens)
 {
     if (G < 1 || G > 64) return fail(SQ_ERR_INVALID_ARG, "%s: G = %d must be in [1, 64]", fn, G);
-    if (tokens * sh->H * (G + 2) > 0x7fffffffll) return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", fn);
+    if (tokens * sh->H * (G + 2) > 0x7fffffffll || (long long)sh->H * (G + 2) > 4 * 65535) return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", fn);
     return SQ_OK;
 }
 

@@ -3,15 +3,19 @@
 // A page is written by one workgroup per head and tensor, which holds the page's new rows in registers between the maximum and
 // the rounding.  If the maximum asks for a larger scale than the page has, the same workgroup shifts the page's earlier codes.
 //
-// The key's arithmetic is double precision: a code is decided at a border between two values that lie 1/8 apart, and with the
-// f16 row, the f32 table and the f16 weight given exactly, 53 bits decide it as exact arithmetic does but once in some 10^14
-// values, where 24 bits would differ once in a million.
+// A key's code is decided at a border between two values that lie 1/8 apart, and with the f16 row, the f32 table and the f16 weight
+// given exactly, 53 bits decide it as exact arithmetic does but once in some 10^14 values, where 24 bits would differ once in a
+// million.  So the arithmetic is fp32 with a bound on its error: where the value less the bound and the value and the bound have
+// the same code, that is the code; the others, one wave in a hundred, are taken again in double precision.  (In double precision
+// throughout, the keys and values of 16384 tokens of 8 heads took 77 us, of which the memory needs 20.)
 #include "sq_head_row.hpp"
 #include "sq_internal.hpp"
 
 namespace sq {
 
 namespace {
+
+constexpr int FUSED_TOKENS = 512;
 
 struct Piece {
     int b, block;              // sequence, index of its page
@@ -36,8 +40,8 @@ __device__ __forceinline__ void sequence(const AppendArgs &a, int b, int &held, 
 
 __device__ __forceinline__ int pages_touched(int held, int n, int P) { return n > 0 ? (held + n - 1) / P - held / P + 1 : 0; }
 
-// The `unit`-th page that the call appends to; false: there are not so many.  Called by the whole workgroup.
-__device__ __forceinline__ bool find_piece(const AppendArgs &a, int unit, Piece &p, int *s_scan /*[6]*/)
+// The `unit`-th page that the call appends to; false: there are not so many.  Every wave finds it for itself, 256 sequences at a time.
+__device__ __forceinline__ bool find_piece(const AppendArgs &a, int unit, Piece &p)
 {
     int b, j = 0, held, n, row;
     if (!a.cu) {
@@ -46,32 +50,36 @@ __device__ __forceinline__ bool find_piece(const AppendArgs &a, int unit, Piece 
         sequence(a, b, held, n, row);
         if (j >= pages_touched(held, n, a.P)) return false;
     } else {
-        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        const int lane = threadIdx.x & 63;
         int before = 0;
-        if (tid == 0) s_scan[4] = -1;
         for (int b0 = 0;; b0 += 256) {
             if (b0 >= a.B) return false;
-            int t = 0;
-            if (b0 + tid < a.B) {
-                sequence(a, b0 + tid, held, n, row);
-                t = pages_touched(held, n, a.P);
+            int t[4], sum = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int at = b0 + 4 * lane + k;
+                sequence(a, min(at, a.B - 1), held, n, row);
+                t[k] = at < a.B ? pages_touched(held, n, a.P) : 0;
+                sum += t[k];
             }
-            const int inc = wave_inclusive_scan(t, lane);
-            __syncthreads();
-            if (lane == 63) s_scan[wave] = inc;
-            __syncthreads();
-            int ex = before + inc - t;
-            for (int w = 0; w < wave; ++w) ex += s_scan[w];
-            if (ex <= unit && unit < ex + t) {
-                s_scan[4] = b0 + tid;
-                s_scan[5] = unit - ex;
+            const int inc = wave_inclusive_scan(sum, lane);
+            int ex = before + inc - sum;
+            const unsigned long long here = __ballot(ex <= unit && unit < ex + sum);
+            if (here != 0ull) {
+                b = b0 + 4 * lane;
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+                    if (b == b0 + 4 * lane + k && unit >= ex + t[k]) {
+                        ex += t[k];
+                        ++b;
+                    }
+                const int owner = __ffsll((long long)here) - 1;
+                b = __builtin_amdgcn_readlane(b, owner);
+                j = unit - __builtin_amdgcn_readlane(ex, owner);
+                break;
             }
-            __syncthreads();
-            if (s_scan[4] >= 0) break;
-            before += s_scan[0] + s_scan[1] + s_scan[2] + s_scan[3];
+            before += __builtin_amdgcn_readlane(inc, 63);
         }
-        b = s_scan[4];
-        j = s_scan[5];
         sequence(a, b, held, n, row);
     }
     p.b = b;
@@ -83,16 +91,54 @@ __device__ __forceinline__ bool find_piece(const AppendArgs &a, int unit, Piece 
     return true;
 }
 
+// fp32 arithmetic of a key is off by at most this much of |a| + |b| of its pair (a, b) before the rotation: a sum of 128 squares (11
+// additions in a row, half of which the root takes away), its root, its reciprocal and two products, 12 roundings at most, and three
+// of the rotation.
+constexpr float KEY_ERROR = 1.0f / (1 << 20);
+
+// A key's values in double precision, one pair after the other so that it takes few registers.
+__device__ __forceinline__ void exact_key(float (&x)[8], h4 lo, h4 hi, h4 wa, h4 wb, bool norm, float eps, const float (&cs)[8], bool turns,
+                                          bool adjacent)
+{
+    double r = 1.0;
+    if (norm) {
+        double ss = 0.0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ss += (double)(float)lo[i] * (double)(float)lo[i] + (double)(float)hi[i] * (double)(float)hi[i];
+        r = 1.0 / sqrt(row16_total(ss) / D + (double)eps);
+    }
+    auto value = [&](int i) {                               // dimension i of the lane's eight
+        const double v = (double)(float)(i < 4 ? lo[i & 3] : hi[i & 3]);
+        return norm ? v * r * (double)(float)(i < 4 ? wa[i & 3] : wb[i & 3]) : v;
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const double a = adjacent ? value(2 * i) : value(i), b = adjacent ? value(2 * i + 1) : value(i + 4);
+        const double c = turns ? (double)cs[2 * i] : 1.0, s = turns ? (double)cs[2 * i + 1] : 0.0;
+        const float u = to_float_unbiased(turns ? a * c - b * s : a), v = to_float_unbiased(turns ? b * c + a * s : b);
+        if (adjacent) {
+            x[2 * i] = u;
+            x[2 * i + 1] = v;
+        } else {
+            x[i] = u;
+            x[i + 4] = v;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
 }  // namespace
 
+// Tokens g, g + 16, .. of a page by 16 lanes each: T of them a thread.  Workgroups of the heads of one page, keys and values, follow one
+// another: together they read the page's tokens of the projection row by row.
+template <int T, bool QUERIES>
 __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryArgs ra)
 {
-    const int tid = threadIdx.x, j = tid & 15, g = tid >> 4;
-    __shared__ int s_scan[6];
-    __shared__ uint32_t s_max[4];
-    if ((int)blockIdx.x >= a.kv_blocks) {                   // query rows: four heads of 16 tokens
-        const int at = blockIdx.x - a.kv_blocks, blocks = (a.n_tokens + 15) / 16, quad = at / blocks;
-        const int token = (at - quad * blocks) * 16 + g;
+    const int tid = threadIdx.x, j = tid & 15, g = tid >> 4, wide = blockDim.x >> 4, waves = blockDim.x >> 6;
+    __shared__ float s_max[4];
+    if (QUERIES && (int)blockIdx.x >= a.kv_blocks) {        // query rows: four heads of as many tokens as there are groups of 16 lanes
+        const int at = blockIdx.x - a.kv_blocks, blocks = (a.n_tokens + wide - 1) / wide, quad = at / blocks;
+        const int token = (at - quad * blocks) * wide + g;
         if (token >= a.n_tokens) return;
         if (a.cu && (token < a.cu[0] || token >= a.cu[a.B])) return;
         TurnRows rows;
@@ -108,86 +154,182 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryA
         return;
     }
     const int hv = blockIdx.x % (2 * a.H), unit = blockIdx.x / (2 * a.H);
-    const int h = hv >> 1;
-    const bool value = hv & 1;
+    const bool value = hv >= a.H;
+    const int h = value ? hv - a.H : hv;
     Piece p;
-    if (!find_piece(a, unit, p, s_scan)) return;
+    if (!find_piece(a, unit, p)) return;
+    // (the rows are read beside the page's number, not behind it; lanes behind the last token read it again, and store nothing)
     const int page = a.page_table[(size_t)p.b * a.max_pages + p.block];
-    if (page < 0 || page >= a.n_pages) return;
+    const bool norm = ra.weight[1] != nullptr, adjacent = ra.adjacent != 0, inexact = norm || ra.rot_dim > 0;
+    const LanePieces lp = value ? LanePieces{8 * j, 8 * j + 4, false} : lane_pieces(j, ra.rot_dim, adjacent);
+    auto token_of = [&](int i) { return p.row + min(i * 16 + g, p.n - 1); };
+    auto row_of = [&](int token) {
+        return (value ? a.v + (size_t)token * a.v_stride : a.k + (size_t)token * a.k_stride) + (size_t)h * D;
+    };
+    auto position_of = [&](int token) { return ra.rot_dim ? a.positions[token] : 0; };
+    float x[T][8], off[T][4];                               // values, and how far those of a pair may be off
+    h4 wa = {}, wb = {};
+    {
+        h4 lo[T], hi[T];
+        float cs[T][8];
+#pragma unroll
+        for (int i = 0; i < T; ++i) {
+            const _Float16 *src = row_of(token_of(i));
+            lo[i] = *reinterpret_cast<const h4 *>(src + lp.a);
+            hi[i] = *reinterpret_cast<const h4 *>(src + lp.b);
+        }
+        if (!value) {
+            if (norm) {
+                wa = *reinterpret_cast<const h4 *>(ra.weight[1] + lp.a);
+                wb = *reinterpret_cast<const h4 *>(ra.weight[1] + lp.b);
+            }
+#pragma unroll
+            for (int i = 0; i < T; ++i) load_turn(cs[i], ra, position_of(token_of(i)), j, lp.turns);
+        }
+        if (page < 0 || page >= a.n_pages) return;
+#pragma unroll
+        for (int i = 0; i < T; ++i) {
+            widen(x[i], lo[i], hi[i]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) off[i][c] = 0.0f;
+            if (!value) norm_rotate(x[i], wa, wb, norm, ra.eps, cs[i], lp.turns, adjacent, off[i]);
+        }
+    }
     const size_t ph = (size_t)page * a.H + h;
     uint8_t *codes = (value ? a.V8 : a.K8) + ph * a.P * D;
     float *scale = (value ? a.v_scale : a.k_scale) + ph;
-
-    const LanePieces lp = value ? LanePieces{8 * j, 8 * j + 4, false} : lane_pieces(j, ra.rot_dim, ra.adjacent != 0);
-    float x[4][8];
-    uint32_t amax = 0;
-    double w[8] = {};
-    if (!value && ra.weight[1]) load_pieces(w, ra.weight[1], lp);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int t = i * 16 + g;
-        if (i * 16 >= p.n) break;
-        const int token = p.row + min(t, p.n - 1);
-        if (value) {
-            load_pieces(x[i], a.v + (size_t)token * a.v_stride + (size_t)h * D, lp);
-        } else {
-            double e[8];
-            float cs[8];
-            load_turn(cs, ra, ra.rot_dim ? a.positions[token] : 0, j, lp.turns);
-            load_pieces(e, a.k + (size_t)token * a.k_stride + (size_t)h * D, lp);
-            norm_rotate<double>(e, w, ra.weight[1] != nullptr, (double)ra.eps, cs, lp.turns, ra.adjacent != 0);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) x[i][c] = to_float_unbiased(e[c]);
-        }
-#pragma unroll
-        for (int c = 0; c < 8; ++c) amax = max(amax, finite_abs(x[i][c]));
-    }
-#pragma unroll
-    for (int k = 32; k > 0; k >>= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, k));
-    if ((tid & 63) == 0) s_max[tid >> 6] = amax;
     const int e_old = p.old > 0 ? exponent_of(*scale) : E4M3_EXP_MIN;
-    __syncthreads();                                        // (every thread has read the scale)
-    amax = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
-    const int e = max(scale_exponent(amax), e_old);
+    // One token's key, read and computed again in double precision.
+    auto exactly = [&](float (&y)[8], int i) {
+        const int token = token_of(i);
+        const _Float16 *src = row_of(token);
+        float cs[8];
+        load_turn(cs, ra, position_of(token), j, lp.turns);
+        exact_key(y, *reinterpret_cast<const h4 *>(src + lp.a), *reinterpret_cast<const h4 *>(src + lp.b), wa, wb, norm, ra.eps, cs, lp.turns,
+                  adjacent);
+    };
+    auto largest = [](uint32_t most, const float (&y)[8]) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) most = max(most, finite_abs(y[c]));
+        return most;
+    };
+    auto page_max = [&](uint32_t most) {                    // (bits of floats that are not negative order as they do)
+        float v = wave_max(__builtin_bit_cast(float, most));
+        if ((tid & 63) == 0) s_max[tid >> 6] = v;
+        __syncthreads();
+        v = s_max[0];
+        for (int i = 1; i < waves; ++i) v = fmaxf(v, s_max[i]);
+        return v;
+    };
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < T; ++i) most = largest(most, x[i]);
+    float amax = page_max(most);                            // (behind its barrier every thread has read the scale)
+    uint32_t again = 0;                                     // tokens to be taken again in double precision, a bit each
+    const auto exponent = [](float v) { return scale_exponent(__builtin_bit_cast(uint32_t, v)); };
+    // (|a| + |b| of the largest value's pair is at most twice the value)
+    if (!value && inexact && exponent(amax * (1.0f - 4 * KEY_ERROR)) != exponent(amax * (1.0f + 4 * KEY_ERROR))) {
+        again = (1u << T) - 1;
+        most = 0;
+#pragma unroll 1
+        for (int i = 0; i < T; ++i) {
+            float y[8];
+            exactly(y, i);
+            most = largest(most, y);
+        }
+        __syncthreads();                                    // (the first maxima have been read)
+        amax = page_max(most);
+    }
+    const int e = max(exponent(amax), e_old);
     if (p.old > 0 && e > e_old) {
-        const float f = exp2_int(e_old - e < -126 ? -126 : e_old - e);
-        for (int i = tid; i < p.old * (D / 8); i += 256) {
-            u2v *c = reinterpret_cast<u2v *>(codes) + i;
-            const u2v v = *c;
-            *c = u2v{e4m3_rescale4(v.x, f), e4m3_rescale4(v.y, f)};
+        const float f = exp2_int(max(e_old - e, -126));
+        for (int i = tid; i < p.old * (D / 16); i += blockDim.x) {
+            u4v *c = reinterpret_cast<u4v *>(codes) + i;
+            const u4v v = *c;
+            *c = u4v{e4m3_rescale4(v.x, f), e4m3_rescale4(v.y, f), e4m3_rescale4(v.z, f), e4m3_rescale4(v.w, f)};
         }
     }
     const float inv = exp2_int(-e);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int t = i * 16 + g;
-        if (t >= p.n) break;
-        const u2v c = e4m3_encode8(x[i], inv);
-        uint8_t *row = codes + (size_t)(p.old + t) * D;
+    auto store = [&](int i, u2v c) {
+        if (i * 16 + g >= p.n) return;
+        uint8_t *row = codes + (size_t)(p.old + i * 16 + g) * D;
         *reinterpret_cast<uint32_t *>(row + lp.a) = c.x;
         *reinterpret_cast<uint32_t *>(row + lp.b) = c.y;
+    };
+    if (!value && inexact) {
+#pragma unroll
+        for (int i = 0; i < T; ++i) {
+            float less[8], more[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const float d = (adjacent ? off[i][c >> 1] : off[i][c & 3]) * KEY_ERROR;
+                less[c] = x[i][c] - d;
+                more[c] = x[i][c] + d;
+            }
+            const u2v down = e4m3_encode8(less, inv), up = e4m3_encode8(more, inv);
+            if (down.x != up.x || down.y != up.y) again |= 1u << i;
+            store(i, down);
+        }
+#pragma unroll 1
+        for (int i = 0; i < T; ++i)                         // (what was stored where a code was in doubt is overwritten)
+            if (__any(again >> i & 1)) {
+                float y[8];
+                exactly(y, i);
+                store(i, e4m3_encode8(y, inv));
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < T; ++i) store(i, e4m3_encode8(x[i], inv));
     }
     if (tid == 0) *scale = exp2_int(e);
+}
+
+template <bool QUERIES>
+hipError_t launch_append(const AppendArgs &a, const RotaryArgs &ra, int most, unsigned grid, int threads, hipStream_t s)
+{
+    if (most > 32) hipLaunchKernelGGL((cache_append_kernel<4, QUERIES>), dim3(grid), dim3(threads), 0, s, a, ra);
+    else if (most > 16) hipLaunchKernelGGL((cache_append_kernel<2, QUERIES>), dim3(grid), dim3(threads), 0, s, a, ra);
+    else hipLaunchKernelGGL((cache_append_kernel<1, QUERIES>), dim3(grid), dim3(threads), 0, s, a, ra);
+    return hipGetLastError();
 }
 
 hipError_t launch_cache_append(AppendArgs a, const RotaryArgs &ra, hipStream_t s)
 {
     long long units;
+    int most;                                               // new tokens that a page can get
     if (a.cu) {
         // n tokens touch at most n pages, and at most n / P + 2
         const long long some = a.B < a.n_tokens ? a.B : a.n_tokens;
         units = (long long)a.n_tokens / a.P + 2 * some;
         if (units > a.n_tokens) units = a.n_tokens;
+        most = a.n_tokens;
     } else {
         a.per_seq = (a.Lq + a.P - 2) / a.P + 1;
         units = (long long)a.B * a.per_seq;
+        most = a.Lq;
     }
-    const long long kv = units * a.H * 2, q = a.q ? ((long long)a.n_tokens + 15) / 16 * ((a.Hq + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE) : 0;
+    if (most > a.P) most = a.P;
+    const int threads = most < 16 ? (most * 16 + 63) / 64 * 64 : 256;
+    const long long kv = units * a.H * 2;
+    // The queries of few tokens are workgroups of the same launch; of many, a launch of their own, with registers of their own.
+    const bool fused = a.q && a.n_tokens <= FUSED_TOKENS;
+    const long long q = fused ? ((long long)a.n_tokens * 16 + threads - 1) / threads * ((a.Hq + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE) : 0;
     if (kv + q > 0x7fffffffll) return hipErrorInvalidConfiguration;
-    if (kv + q == 0) return hipSuccess;
+    if (a.q && !fused) {
+        HeadRows hr{};
+        hr.src[0] = a.q;
+        hr.dst[0] = a.q_out;
+        hr.stride[0] = a.q_stride;
+        hr.n[0] = a.Hq;
+        hr.Lq = 1;
+        hr.positions = a.positions;
+        hr.first = a.cu;
+        hr.last = a.cu ? a.cu + a.B : nullptr;
+        hipError_t e = launch_head_rows(hr, ra, a.n_tokens, s);
+        if (e != hipSuccess) return e;
+    }
     a.kv_blocks = (int)kv;
-    hipLaunchKernelGGL(cache_append_kernel, dim3((unsigned)(kv + q)), dim3(256), 0, s, a, ra);
-    return hipGetLastError();
+    return fused ? launch_append<true>(a, ra, most, (unsigned)(kv + q), threads, s) : launch_append<false>(a, ra, most, (unsigned)kv, threads, s);
 }
 
 }  // namespace sq

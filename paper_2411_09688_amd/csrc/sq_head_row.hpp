@@ -44,44 +44,43 @@ __device__ __forceinline__ void load_turn(float (&cs)[8], const RotaryArgs &ra, 
     cs[4] = y[0]; cs[5] = y[1]; cs[6] = y[2]; cs[7] = y[3];
 }
 
-template <typename T>
-__device__ __forceinline__ T row16_total(T v)
+__device__ __forceinline__ float row16_total(float v) { return row16_sum(v); }
+__device__ __forceinline__ double row16_total(double v)
 {
-    if constexpr (sizeof(T) == 4) {
-        return row16_sum(v);
-    } else {
 #pragma unroll
-        for (int k = 8; k > 0; k >>= 1) v += __shfl_xor(v, k, 16);
-        return v;
-    }
+    for (int k = 8; k > 0; k >>= 1) v += __shfl_xor(v, k, 16);
+    return v;
 }
 
-// e: the lane's dimensions (pieces a, b); w: the weight's, same places.  T is the type of the arithmetic.
-template <typename T>
-__device__ __forceinline__ void norm_rotate(T (&e)[8], const T (&w)[8], bool norm, T eps, const float (&cs)[8], bool turns, bool adjacent)
+// e: the lane's dimensions (pieces a, b); wa, wb: the weight's, same places.  pair: |a| + |b| of each pair before it is turned, 0 where
+// nothing was done to it.
+__device__ __forceinline__ void norm_rotate(float (&e)[8], h4 wa, h4 wb, bool norm, float eps, const float (&cs)[8], bool turns, bool adjacent,
+                                            float (&pair)[4])
 {
     if (norm) {
-        T ss = 0;
+        float ss = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) ss += e[i] * e[i];
-        const T r = (T)1 / sqrt(row16_total(ss) / (T)D + eps);
+        const float r = 1.0f / sqrtf(row16_total(ss) * (1.0f / D) + eps);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = e[i] * r * w[i];
+        for (int i = 0; i < 8; ++i) e[i] = e[i] * r * (float)(i < 4 ? wa[i & 3] : wb[i & 3]);
     }
-    if (!turns) return;
+    if (!norm && !turns) return;
     if (adjacent) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const T a = e[2 * i], b = e[2 * i + 1], c = cs[2 * i], s = cs[2 * i + 1];
-            e[2 * i] = a * c - b * s;
-            e[2 * i + 1] = b * c + a * s;
+            const float a = e[2 * i], b = e[2 * i + 1], c = cs[2 * i], s = cs[2 * i + 1];
+            pair[i] = fabsf(a) + fabsf(b);
+            e[2 * i] = turns ? a * c - b * s : a;
+            e[2 * i + 1] = turns ? b * c + a * s : b;
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const T a = e[i], b = e[i + 4], c = cs[2 * i], s = cs[2 * i + 1];
-            e[i] = a * c - b * s;
-            e[i + 4] = b * c + a * s;
+            const float a = e[i], b = e[i + 4], c = cs[2 * i], s = cs[2 * i + 1];
+            pair[i] = fabsf(a) + fabsf(b);
+            e[i] = turns ? a * c - b * s : a;
+            e[i + 4] = turns ? b * c + a * s : b;
         }
     }
 }
@@ -95,12 +94,6 @@ __device__ __forceinline__ void widen(T (&e)[8], h4 x, h4 y)
         e[i + 4] = (T)(float)y[i];
     }
 }
-template <typename T>
-__device__ __forceinline__ void load_pieces(T (&e)[8], const _Float16 *row, const LanePieces &lp)
-{
-    widen(e, *reinterpret_cast<const h4 *>(row + lp.a), *reinterpret_cast<const h4 *>(row + lp.b));
-}
-
 // Up to four heads of one token by 16 lanes, fp32 arithmetic, rounded to f16 once; kind 0: query, 1: key, 2: value (copied).  All of
 // the rows are read before the first is turned, and the token's cosines and sines once for all of them.
 constexpr int ROWS_AT_ONCE = 4;
@@ -127,10 +120,14 @@ __device__ __forceinline__ void turn_rows(const TurnRows &t, const RotaryArgs &r
         if (i < t.n) {
             if (t.kind[i] != 2) {
                 const _Float16 *weight = ra.weight[t.kind[i]];
-                float e[8], w[8] = {};
+                float e[8], pair[4];
+                h4 wa = {}, wb = {};
+                if (weight) {
+                    wa = *reinterpret_cast<const h4 *>(weight + lp.a);
+                    wb = *reinterpret_cast<const h4 *>(weight + lp.b);
+                }
                 widen(e, x[i], y[i]);
-                if (weight) load_pieces(w, weight, lp);
-                norm_rotate<float>(e, w, weight != nullptr, ra.eps, cs, lp.turns, ra.adjacent != 0);
+                norm_rotate(e, wa, wb, weight != nullptr, ra.eps, cs, lp.turns, ra.adjacent != 0, pair);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     x[i][c] = (_Float16)e[c];

@@ -13,6 +13,7 @@ __global__ __launch_bounds__(256) void head_rows_kernel(HeadRows hr, RotaryArgs 
 {
     const int j = threadIdx.x & 15, token = blockIdx.x * 16 + (threadIdx.x >> 4);
     if (token >= tokens) return;
+    if (hr.first && (token < *hr.first || token >= *hr.last)) return;
     const int b = token / hr.Lq, t = token - b * hr.Lq, heads = hr.n[0] + hr.n[1] + hr.n[2];
     TurnRows rows;
     rows.n = min(ROWS_AT_ONCE, heads - (int)blockIdx.y * ROWS_AT_ONCE);

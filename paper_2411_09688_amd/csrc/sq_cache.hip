@@ -15,8 +15,6 @@ namespace sq {
 
 namespace {
 
-constexpr int FUSED_TOKENS = 512;
-
 struct Piece {
     int b, block;              // sequence, index of its page
     int old, n;                // tokens of the page before, new ones
@@ -91,21 +89,23 @@ __device__ __forceinline__ bool find_piece(const AppendArgs &a, int unit, Piece 
     return true;
 }
 
-// fp32 arithmetic of a key is off by at most this much of |a| + |b| of its pair (a, b) before the rotation: a sum of 128 squares (11
-// additions in a row, half of which the root takes away), its root, its reciprocal and two products, 12 roundings at most, and three
-// of the rotation.
+// fp32 arithmetic of a key is off by at most this much, 16 roundings, of |a| + |b| of its pair (a, b) before the rotation: a sum of 128
+// squares (13 additions in a row, of which the root halves the error), the reciprocal root (a last place: two roundings), two products,
+// and three roundings of the rotation make 14.
 constexpr float KEY_ERROR = 1.0f / (1 << 20);
 
 // A key's values in double precision, one pair after the other so that it takes few registers.
-__device__ __forceinline__ void exact_key(float (&x)[8], h4 lo, h4 hi, h4 wa, h4 wb, bool norm, float eps, const float (&cs)[8], bool turns,
-                                          bool adjacent)
+template <bool ADJACENT>
+__device__ __forceinline__ void exact_key(float (&x)[8], h4 lo, h4 hi, h4 wa, h4 wb, bool norm, float eps, const float (&cs)[8], bool turns)
 {
     double r = 1.0;
     if (norm) {
         double ss = 0.0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) ss += (double)(float)lo[i] * (double)(float)lo[i] + (double)(float)hi[i] * (double)(float)hi[i];
-        r = 1.0 / sqrt(row16_total(ss) / D + (double)eps);
+#pragma unroll
+        for (int k = 8; k > 0; k >>= 1) ss += __shfl_xor(ss, k, 16);
+        r = 1.0 / sqrt(ss / D + (double)eps);
     }
     auto value = [&](int i) {                               // dimension i of the lane's eight
         const double v = (double)(float)(i < 4 ? lo[i & 3] : hi[i & 3]);
@@ -113,16 +113,10 @@ __device__ __forceinline__ void exact_key(float (&x)[8], h4 lo, h4 hi, h4 wa, h4
     };
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const double a = adjacent ? value(2 * i) : value(i), b = adjacent ? value(2 * i + 1) : value(i + 4);
-        const double c = turns ? (double)cs[2 * i] : 1.0, s = turns ? (double)cs[2 * i + 1] : 0.0;
-        const float u = to_float_unbiased(turns ? a * c - b * s : a), v = to_float_unbiased(turns ? b * c + a * s : b);
-        if (adjacent) {
-            x[2 * i] = u;
-            x[2 * i + 1] = v;
-        } else {
-            x[i] = u;
-            x[i + 4] = v;
-        }
+        const int ia = ADJACENT ? 2 * i : i, ib = ADJACENT ? 2 * i + 1 : i + 4;
+        const double a = value(ia), b = value(ib), c = cs[2 * i], s = cs[2 * i + 1];
+        x[ia] = to_float_unbiased(turns ? a * c - b * s : a);
+        x[ib] = to_float_unbiased(turns ? b * c + a * s : b);
         __builtin_amdgcn_sched_barrier(0);
     }
 }
@@ -131,14 +125,14 @@ __device__ __forceinline__ void exact_key(float (&x)[8], h4 lo, h4 hi, h4 wa, h4
 
 // Tokens g, g + 16, .. of a page by 16 lanes each: T of them a thread.  Workgroups of the heads of one page, keys and values, follow one
 // another: together they read the page's tokens of the projection row by row.
-template <int T, bool QUERIES>
+template <int T, bool ADJACENT, bool PARTIAL>
 __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryArgs ra)
 {
     const int tid = threadIdx.x, j = tid & 15, g = tid >> 4, wide = blockDim.x >> 4, waves = blockDim.x >> 6;
     __shared__ float s_max[4];
-    if (QUERIES && (int)blockIdx.x >= a.kv_blocks) {        // query rows: four heads of as many tokens as there are groups of 16 lanes
-        const int at = blockIdx.x - a.kv_blocks, blocks = (a.n_tokens + wide - 1) / wide, quad = at / blocks;
-        const int token = (at - quad * blocks) * wide + g;
+    if ((int)blockIdx.x >= a.kv_blocks) {                   // query rows: four heads of as many tokens as there are groups of 16 lanes
+        const int at = blockIdx.x - a.kv_blocks, quads = (a.Hq + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE, block = at / quads;
+        const int quad = at - block * quads, token = block * wide + g;
         if (token >= a.n_tokens) return;
         if (a.cu && (token < a.cu[0] || token >= a.cu[a.B])) return;
         TurnRows rows;
@@ -150,7 +144,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryA
             rows.src[i] = a.q + (size_t)token * a.q_stride + (size_t)h * D;
             rows.dst[i] = a.q_out + ((size_t)token * a.Hq + h) * D;
         }
-        turn_rows(rows, ra, ra.rot_dim ? a.positions[token] : 0, j);
+        turn_rows<ADJACENT, PARTIAL>(rows, ra, ra.rot_dim ? a.positions[token] : 0, j);
         return;
     }
     const int hv = blockIdx.x % (2 * a.H), unit = blockIdx.x / (2 * a.H);
@@ -160,8 +154,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryA
     if (!find_piece(a, unit, p)) return;
     // (the rows are read beside the page's number, not behind it; lanes behind the last token read it again, and store nothing)
     const int page = a.page_table[(size_t)p.b * a.max_pages + p.block];
-    const bool norm = ra.weight[1] != nullptr, adjacent = ra.adjacent != 0, inexact = norm || ra.rot_dim > 0;
-    const LanePieces lp = value ? LanePieces{8 * j, 8 * j + 4, false} : lane_pieces(j, ra.rot_dim, adjacent);
+    const bool norm = ra.weight[1] != nullptr, inexact = norm || ra.rot_dim > 0;
+    const LanePieces lp = value ? LanePieces{8 * j, 8 * j + 4, false} : lane_pieces<ADJACENT, PARTIAL>(j, ra.rot_dim);
     auto token_of = [&](int i) { return p.row + min(i * 16 + g, p.n - 1); };
     auto row_of = [&](int token) {
         return (value ? a.v + (size_t)token * a.v_stride : a.k + (size_t)token * a.k_stride) + (size_t)h * D;
@@ -189,10 +183,10 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryA
         if (page < 0 || page >= a.n_pages) return;
 #pragma unroll
         for (int i = 0; i < T; ++i) {
-            widen(x[i], lo[i], hi[i]);
+            if (!value) norm_rotate<ADJACENT, PARTIAL, true>(x[i], lo[i], hi[i], wa, wb, norm, ra.eps, cs[i], lp.turns, off[i]);
+            else
 #pragma unroll
-            for (int c = 0; c < 4; ++c) off[i][c] = 0.0f;
-            if (!value) norm_rotate(x[i], wa, wb, norm, ra.eps, cs[i], lp.turns, adjacent, off[i]);
+                for (int c = 0; c < 8; ++c) x[i][c] = (float)(c < 4 ? lo[i][c & 3] : hi[i][c & 3]);
         }
     }
     const size_t ph = (size_t)page * a.H + h;
@@ -205,37 +199,45 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryA
         const _Float16 *src = row_of(token);
         float cs[8];
         load_turn(cs, ra, position_of(token), j, lp.turns);
-        exact_key(y, *reinterpret_cast<const h4 *>(src + lp.a), *reinterpret_cast<const h4 *>(src + lp.b), wa, wb, norm, ra.eps, cs, lp.turns,
-                  adjacent);
+        exact_key<ADJACENT>(y, *reinterpret_cast<const h4 *>(src + lp.a), *reinterpret_cast<const h4 *>(src + lp.b), wa, wb, norm, ra.eps, cs,
+                            lp.turns);
     };
-    auto largest = [](uint32_t most, const float (&y)[8]) {
-#pragma unroll
-        for (int c = 0; c < 8; ++c) most = max(most, finite_abs(y[c]));
-        return most;
-    };
-    auto page_max = [&](uint32_t most) {                    // (bits of floats that are not negative order as they do)
-        float v = wave_max(__builtin_bit_cast(float, most));
+    auto page_max = [&](float v) {
+        v = wave_max(v);
         if ((tid & 63) == 0) s_max[tid >> 6] = v;
         __syncthreads();
         v = s_max[0];
         for (int i = 1; i < waves; ++i) v = fmaxf(v, s_max[i]);
         return v;
     };
-    uint32_t most = 0;
+    float most = 0.0f;                                      // (a maximum passes over NaN)
 #pragma unroll
-    for (int i = 0; i < T; ++i) most = largest(most, x[i]);
+    for (int i = 0; i < T; ++i)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) most = fmaxf(most, fabsf(x[i][c]));
     float amax = page_max(most);                            // (behind its barrier every thread has read the scale)
     uint32_t again = 0;                                     // tokens to be taken again in double precision, a bit each
     const auto exponent = [](float v) { return scale_exponent(__builtin_bit_cast(uint32_t, v)); };
-    // (|a| + |b| of the largest value's pair is at most twice the value)
-    if (!value && inexact && exponent(amax * (1.0f - 4 * KEY_ERROR)) != exponent(amax * (1.0f + 4 * KEY_ERROR))) {
-        again = (1u << T) - 1;
-        most = 0;
+    // An infinity sets no scale; and where the largest value lies within its error of one's limit, it is taken exactly (|a| + |b| of its
+    // pair is at most twice the value).
+    const bool near = !value && inexact && exponent(amax * (1.0f - 4 * KEY_ERROR)) != exponent(amax * (1.0f + 4 * KEY_ERROR));
+    if (near || amax > 3.4e38f) {
+        if (near) again = (1u << T) - 1;
+        most = 0.0f;
 #pragma unroll 1
         for (int i = 0; i < T; ++i) {
             float y[8];
-            exactly(y, i);
-            most = largest(most, y);
+            if (near) {
+                exactly(y, i);
+            } else {
+#pragma unroll
+                for (int k = 0; k < T; ++k)
+                    if (k == i)
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) y[c] = x[k][c];
+            }
+#pragma unroll
+            for (int c = 0; c < 8; ++c) most = fmaxf(most, __builtin_bit_cast(float, finite_abs(y[c])));
         }
         __syncthreads();                                    // (the first maxima have been read)
         amax = page_max(most);
@@ -262,11 +264,11 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryA
             float less[8], more[8];
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
-                const float d = (adjacent ? off[i][c >> 1] : off[i][c & 3]) * KEY_ERROR;
-                less[c] = x[i][c] - d;
-                more[c] = x[i][c] + d;
+                const float v = x[i][c] * inv, d = off[i][ADJACENT ? c >> 1 : c & 3] * (KEY_ERROR * inv);
+                less[c] = v - d;
+                more[c] = v + d;
             }
-            const u2v down = e4m3_encode8(less, inv), up = e4m3_encode8(more, inv);
+            const u2v down = e4m3_encode8(less), up = e4m3_encode8(more);
             if (down.x != up.x || down.y != up.y) again |= 1u << i;
             store(i, down);
         }
@@ -282,15 +284,6 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryA
         for (int i = 0; i < T; ++i) store(i, e4m3_encode8(x[i], inv));
     }
     if (tid == 0) *scale = exp2_int(e);
-}
-
-template <bool QUERIES>
-hipError_t launch_append(const AppendArgs &a, const RotaryArgs &ra, int most, unsigned grid, int threads, hipStream_t s)
-{
-    if (most > 32) hipLaunchKernelGGL((cache_append_kernel<4, QUERIES>), dim3(grid), dim3(threads), 0, s, a, ra);
-    else if (most > 16) hipLaunchKernelGGL((cache_append_kernel<2, QUERIES>), dim3(grid), dim3(threads), 0, s, a, ra);
-    else hipLaunchKernelGGL((cache_append_kernel<1, QUERIES>), dim3(grid), dim3(threads), 0, s, a, ra);
-    return hipGetLastError();
 }
 
 hipError_t launch_cache_append(AppendArgs a, const RotaryArgs &ra, hipStream_t s)
@@ -311,25 +304,15 @@ hipError_t launch_cache_append(AppendArgs a, const RotaryArgs &ra, hipStream_t s
     if (most > a.P) most = a.P;
     const int threads = most < 16 ? (most * 16 + 63) / 64 * 64 : 256;
     const long long kv = units * a.H * 2;
-    // The queries of few tokens are workgroups of the same launch; of many, a launch of their own, with registers of their own.
-    const bool fused = a.q && a.n_tokens <= FUSED_TOKENS;
-    const long long q = fused ? ((long long)a.n_tokens * 16 + threads - 1) / threads * ((a.Hq + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE) : 0;
+    const long long q = a.q ? ((long long)a.n_tokens * 16 + threads - 1) / threads * ((a.Hq + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE) : 0;
     if (kv + q > 0x7fffffffll) return hipErrorInvalidConfiguration;
-    if (a.q && !fused) {
-        HeadRows hr{};
-        hr.src[0] = a.q;
-        hr.dst[0] = a.q_out;
-        hr.stride[0] = a.q_stride;
-        hr.n[0] = a.Hq;
-        hr.Lq = 1;
-        hr.positions = a.positions;
-        hr.first = a.cu;
-        hr.last = a.cu ? a.cu + a.B : nullptr;
-        hipError_t e = launch_head_rows(hr, ra, a.n_tokens, s);
-        if (e != hipSuccess) return e;
-    }
     a.kv_blocks = (int)kv;
-    return fused ? launch_append<true>(a, ra, most, (unsigned)(kv + q), threads, s) : launch_append<false>(a, ra, most, (unsigned)kv, threads, s);
+#define SQ_APPEND_1(A, P) cache_append_kernel<1, A, P>
+#define SQ_APPEND_2(A, P) cache_append_kernel<2, A, P>
+#define SQ_APPEND_4(A, P) cache_append_kernel<4, A, P>
+    auto *kernel = most > 32 ? SQ_FOR_ROTARY(ra, SQ_APPEND_4) : most > 16 ? SQ_FOR_ROTARY(ra, SQ_APPEND_2) : SQ_FOR_ROTARY(ra, SQ_APPEND_1);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(kv + q)), dim3(threads), 0, s, a, ra);
+    return hipGetLastError();
 }
 
 }  // namespace sq

@@ -47,13 +47,16 @@ __device__ __forceinline__ uint32_t e4m3_pair(float a, float b, uint32_t old)
     return __builtin_amdgcn_cvt_pk_fp8_f32(a, b, old, HIGH);
 }
 
-// Eight values, scaled, to eight codes.
+// Eight values to eight codes; scaled first.
+__device__ __forceinline__ u2v e4m3_encode8(const float (&x)[8])
+{
+    const uint32_t lo = e4m3_pair<true>(x[2], x[3], e4m3_pair<false>(x[0], x[1], 0u));
+    return u2v{lo, e4m3_pair<true>(x[6], x[7], e4m3_pair<false>(x[4], x[5], 0u))};
+}
 __device__ __forceinline__ u2v e4m3_encode8(const float (&x)[8], float inv)
 {
-    uint32_t lo = e4m3_pair<false>(x[0] * inv, x[1] * inv, 0u), hi = e4m3_pair<false>(x[4] * inv, x[5] * inv, 0u);
-    lo = e4m3_pair<true>(x[2] * inv, x[3] * inv, lo);
-    hi = e4m3_pair<true>(x[6] * inv, x[7] * inv, hi);
-    return u2v{lo, hi};
+    const float y[8] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv, x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv};
+    return e4m3_encode8(y);
 }
 
 // Four codes, scaled by a power of two, to four codes.

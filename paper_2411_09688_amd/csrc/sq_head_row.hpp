@@ -22,12 +22,13 @@ struct LanePieces {
     bool turns;                    // they are rotated
 };
 
-__device__ __forceinline__ LanePieces lane_pieces(int j, int rot_dim, bool adjacent)
+template <bool ADJACENT, bool PARTIAL>
+__device__ __forceinline__ LanePieces lane_pieces(int j, int rot_dim)
 {
-    const int n = rot_dim >> 3;
-    if (adjacent) return {8 * j, 8 * j + 4, j < n};
-    if (j < n) return {4 * j, (rot_dim >> 1) + 4 * j, true};
-    return {rot_dim + 8 * (j - n), rot_dim + 8 * (j - n) + 4, false};
+    const int r = PARTIAL ? rot_dim : D, n = r >> 3;
+    if (ADJACENT) return {8 * j, 8 * j + 4, !PARTIAL || j < n};
+    if (!PARTIAL || j < n) return {4 * j, (r >> 1) + 4 * j, true};
+    return {r + 8 * (j - n), r + 8 * (j - n) + 4, false};
 }
 
 // The four pairs' cosines and sines of a lane; 1 and 0 where it does not rotate.
@@ -44,56 +45,49 @@ __device__ __forceinline__ void load_turn(float (&cs)[8], const RotaryArgs &ra, 
     cs[4] = y[0]; cs[5] = y[1]; cs[6] = y[2]; cs[7] = y[3];
 }
 
-__device__ __forceinline__ float row16_total(float v) { return row16_sum(v); }
-__device__ __forceinline__ double row16_total(double v)
-{
-#pragma unroll
-    for (int k = 8; k > 0; k >>= 1) v += __shfl_xor(v, k, 16);
-    return v;
-}
+// The kernels are compiled for each kind of rotation, which costs a row a third of its instructions as selects otherwise: pairs
+// (2i, 2i + 1) or not (ADJACENT), and lanes that do not rotate or none (PARTIAL: rot_dim < 128).
+#define SQ_FOR_ROTARY(ra, call)                                                       \
+    ((ra).adjacent ? ((ra).rot_dim < D ? call(true, true) : call(true, false))        \
+                   : ((ra).rot_dim < D ? call(false, true) : call(false, false)))
 
-// e: the lane's dimensions (pieces a, b); wa, wb: the weight's, same places.  pair: |a| + |b| of each pair before it is turned, 0 where
-// nothing was done to it.
-__device__ __forceinline__ void norm_rotate(float (&e)[8], h4 wa, h4 wb, bool norm, float eps, const float (&cs)[8], bool turns, bool adjacent,
+// The lane's dimensions x, y (pieces a, b) normed and rotated, fp32 arithmetic; wa, wb: the weight's, same places; turns: this lane
+// rotates.  pair (if PAIRS): |a| + |b| of each pair (a, b) before it is turned.
+template <bool ADJACENT, bool PARTIAL, bool PAIRS>
+__device__ __forceinline__ void norm_rotate(float (&e)[8], h4 x, h4 y, h4 wa, h4 wb, bool norm, float eps, const float (&cs)[8], bool turns,
                                             float (&pair)[4])
 {
     if (norm) {
         float ss = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ss += e[i] * e[i];
-        const float r = 1.0f / sqrtf(row16_total(ss) * (1.0f / D) + eps);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = e[i] * r * (float)(i < 4 ? wa[i & 3] : wb[i & 3]);
-    }
-    if (!norm && !turns) return;
-    if (adjacent) {
+        for (int i = 0; i < 4; ++i) {
+            ss = __builtin_fmaf((float)x[i], (float)x[i], ss);
+            ss = __builtin_fmaf((float)y[i], (float)y[i], ss);
+        }
+        const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(row16_sum(ss), 1.0f / D, eps));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float a = e[2 * i], b = e[2 * i + 1], c = cs[2 * i], s = cs[2 * i + 1];
-            pair[i] = fabsf(a) + fabsf(b);
-            e[2 * i] = turns ? a * c - b * s : a;
-            e[2 * i + 1] = turns ? b * c + a * s : b;
+            e[i] = (float)x[i] * ((float)wa[i] * r);
+            e[i + 4] = (float)y[i] * ((float)wb[i] * r);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float a = e[i], b = e[i + 4], c = cs[2 * i], s = cs[2 * i + 1];
-            pair[i] = fabsf(a) + fabsf(b);
-            e[i] = turns ? a * c - b * s : a;
-            e[i + 4] = turns ? b * c + a * s : b;
+            e[i] = (float)x[i];
+            e[i + 4] = (float)y[i];
         }
     }
+    auto turn = [&](int ia, int ib, int i) {
+        const float a = e[ia], b = e[ib], c = cs[2 * i], s = cs[2 * i + 1];
+        if (PAIRS) pair[i] = fabsf(a) + fabsf(b);
+        const float u = __builtin_fmaf(a, c, -(b * s)), v = __builtin_fmaf(b, c, a * s);
+        e[ia] = PARTIAL && !turns ? a : u;
+        e[ib] = PARTIAL && !turns ? b : v;
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ADJACENT ? turn(2 * i, 2 * i + 1, i) : turn(i, i + 4, i);
 }
 
-template <typename T>
-__device__ __forceinline__ void widen(T (&e)[8], h4 x, h4 y)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        e[i] = (T)(float)x[i];
-        e[i + 4] = (T)(float)y[i];
-    }
-}
 // Up to four heads of one token by 16 lanes, fp32 arithmetic, rounded to f16 once; kind 0: query, 1: key, 2: value (copied).  All of
 // the rows are read before the first is turned, and the token's cosines and sines once for all of them.
 constexpr int ROWS_AT_ONCE = 4;
@@ -103,9 +97,10 @@ struct TurnRows {
     int kind[ROWS_AT_ONCE];
     int n;
 };
+template <bool ADJACENT, bool PARTIAL>
 __device__ __forceinline__ void turn_rows(const TurnRows &t, const RotaryArgs &ra, int position, int j)
 {
-    const LanePieces lp = lane_pieces(j, ra.rot_dim, ra.adjacent != 0);
+    const LanePieces lp = lane_pieces<ADJACENT, PARTIAL>(j, ra.rot_dim);
     h4 x[ROWS_AT_ONCE], y[ROWS_AT_ONCE];
 #pragma unroll
     for (int i = 0; i < ROWS_AT_ONCE; ++i)
@@ -126,8 +121,7 @@ __device__ __forceinline__ void turn_rows(const TurnRows &t, const RotaryArgs &r
                     wa = *reinterpret_cast<const h4 *>(weight + lp.a);
                     wb = *reinterpret_cast<const h4 *>(weight + lp.b);
                 }
-                widen(e, x[i], y[i]);
-                norm_rotate(e, wa, wb, weight != nullptr, ra.eps, cs, lp.turns, ra.adjacent != 0, pair);
+                norm_rotate<ADJACENT, PARTIAL, false>(e, x[i], y[i], wa, wb, weight != nullptr, ra.eps, cs, lp.turns, pair);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     x[i][c] = (_Float16)e[c];

@@ -9,31 +9,34 @@ namespace sq {
 
 // A workgroup takes 16 consecutive tokens, 16 lanes each, and four heads: a head's rows of consecutive tokens lie side by side in the
 // output.
+template <bool ADJACENT, bool PARTIAL>
 __global__ __launch_bounds__(256) void head_rows_kernel(HeadRows hr, RotaryArgs ra, int tokens)
 {
-    const int j = threadIdx.x & 15, token = blockIdx.x * 16 + (threadIdx.x >> 4);
+    const int heads = hr.n[0] + hr.n[1] + hr.n[2], quads = (heads + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE;
+    const int block = blockIdx.x / quads, quad = blockIdx.x - block * quads;
+    const int j = threadIdx.x & 15, token = block * 16 + (threadIdx.x >> 4);
     if (token >= tokens) return;
-    if (hr.first && (token < *hr.first || token >= *hr.last)) return;
-    const int b = token / hr.Lq, t = token - b * hr.Lq, heads = hr.n[0] + hr.n[1] + hr.n[2];
+    const int b = token / hr.Lq, t = token - b * hr.Lq;
     TurnRows rows;
-    rows.n = min(ROWS_AT_ONCE, heads - (int)blockIdx.y * ROWS_AT_ONCE);
+    rows.n = min(ROWS_AT_ONCE, heads - quad * ROWS_AT_ONCE);
 #pragma unroll
     for (int i = 0; i < ROWS_AT_ONCE; ++i) {
-        int h = min((int)blockIdx.y * ROWS_AT_ONCE + i, heads - 1);
+        int h = min(quad * ROWS_AT_ONCE + i, heads - 1);
         const int part = h < hr.n[0] ? 0 : h < hr.n[0] + hr.n[1] ? 1 : 2;
         h -= part == 0 ? 0 : part == 1 ? hr.n[0] : hr.n[0] + hr.n[1];
         rows.kind[i] = part;
         rows.src[i] = hr.src[part] + token * hr.stride[part] + (size_t)h * D;
         rows.dst[i] = hr.dst[part] + (((size_t)b * hr.n[part] + h) * hr.Lq + t) * D;
     }
-    turn_rows(rows, ra, ra.rot_dim ? hr.positions[token] : 0, j);
+    turn_rows<ADJACENT, PARTIAL>(rows, ra, ra.rot_dim ? hr.positions[token] : 0, j);
 }
 
 hipError_t launch_head_rows(const HeadRows &hr, const RotaryArgs &ra, int tokens, hipStream_t s)
 {
     const int heads = hr.n[0] + hr.n[1] + hr.n[2];
-    hipLaunchKernelGGL(head_rows_kernel, dim3((unsigned)((tokens + 15) / 16), (unsigned)((heads + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE)), dim3(256),
-                       0, s, hr, ra, tokens);
+    const dim3 grid((unsigned)((long long)((tokens + 15) / 16) * ((heads + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE)));
+#define SQ_HEAD_ROWS(A, P) head_rows_kernel<A, P>
+    hipLaunchKernelGGL(SQ_FOR_ROTARY(ra, SQ_HEAD_ROWS), grid, dim3(256), 0, s, hr, ra, tokens);
     return hipGetLastError();
 }
 

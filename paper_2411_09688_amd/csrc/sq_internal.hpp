@@ -356,7 +356,6 @@ struct HeadRows {                  // queries, keys, values; n: heads (0: not gi
     int n[3];
     int Lq;
     const int32_t *positions;
-    const int32_t *first, *last;   // tokens outside [*first, *last) are left alone (null: none is)
 };
 hipError_t launch_head_rows(const HeadRows &hr, const RotaryArgs &ra, int tokens, hipStream_t s);
 

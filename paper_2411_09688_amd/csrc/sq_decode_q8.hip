@@ -153,35 +153,57 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
 
     const int wave = uniform(threadIdx.x >> 6);
 
-    // This workgroup's share of the tiles.  Workgroups go round the 8 XCDs: each XCD takes consecutive shares.
-    const int R = a.B * a.H * a.per, tid = threadIdx.x;
+    const int tid = threadIdx.x;
     if (tid < QT) s_none[tid] = 0;
-    const int each = (R + 255) / 256, i_lo = min(R, tid * each), i_hi = min(R, i_lo + each);
-    int mine = 0, all;
-    for (int i = i_lo; i < i_hi; ++i) mine += row_tiles(a, dealt_row(a, i)).total;
-    int before = block_exclusive(mine, tid, s_w, all);
-    const int shares = min((int)gridDim.x, (all + 3) / 4);      // (at least a tile for each wave)
-    const int per = (all + shares - 1) / shares, per_xcd = (shares + 7) / 8;
-    const int share = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per_xcd || (long long)share * per >= all) return;
-    const int t0 = share * per, t1 = min(all, t0 + per);
-    if (before <= t0 && t0 < before + mine) {
-        int i = i_lo;
-        RowTiles rt;
-        for (;; ++i) {
-            rt = row_tiles(a, dealt_row(a, i));
-            if (t0 < before + rt.total) break;
-            before += rt.total;
-        }
-        s_found[0] = i;
-        s_found[1] = before;
-        s_found[2] = rt.nf;
-        s_found[3] = rt.nu;
-    }
     __syncthreads();
-    // (a row's numbers are the same in every lane: known to be, they take scalar registers, and addresses a scalar base)
-    int ri = uniform(s_found[0]), row_start = uniform(s_found[1]);
-    RowTiles rt = tiles_of(uniform(s_found[2]), uniform(s_found[3]));
+    // This workgroup's share: tiles [t0, t1), counted from row ri's first less row_start; share0 + t / per is who has tile t.
+    int share, share0, per, t0, t1, ri, row_start;
+    RowTiles rt;
+    if (a.splits > 0) {
+        // Few keys: a row's tiles are divided among workgroups of its own, without a look at the other rows.
+        ri = blockIdx.x / a.splits;
+        rt = row_tiles(a, dealt_row(a, ri));
+        rt = tiles_of(uniform(rt.nf), uniform(rt.nu));
+        share0 = ri * a.splits;
+        share = blockIdx.x;
+        per = max(4, (rt.total + a.splits - 1) / a.splits);
+        row_start = 0;
+        t0 = (share - share0) * per;
+        t1 = min(rt.total, t0 + per);
+        if (t0 >= t1) return;
+    } else {
+        // Workgroups go round the 8 XCDs: each XCD takes consecutive shares.
+        const int R = a.B * a.H * a.per;
+        const int each = (R + 255) / 256, i_lo = min(R, tid * each), i_hi = min(R, i_lo + each);
+        int mine = 0, all;
+        for (int i = i_lo; i < i_hi; ++i) mine += row_tiles(a, dealt_row(a, i)).total;
+        int before = block_exclusive(mine, tid, s_w, all);
+        const int shares = min((int)gridDim.x, (all + 3) / 4);      // (at least a tile for each wave)
+        const int per_xcd = (shares + 7) / 8;
+        per = (all + shares - 1) / shares;
+        share0 = 0;
+        share = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+        if ((int)(blockIdx.x >> 3) >= per_xcd || (long long)share * per >= all) return;
+        t0 = share * per;
+        t1 = min(all, t0 + per);
+        if (before <= t0 && t0 < before + mine) {
+            int i = i_lo;
+            for (;; ++i) {
+                rt = row_tiles(a, dealt_row(a, i));
+                if (t0 < before + rt.total) break;
+                before += rt.total;
+            }
+            s_found[0] = i;
+            s_found[1] = before;
+            s_found[2] = rt.nf;
+            s_found[3] = rt.nu;
+        }
+        __syncthreads();
+        // (a row's numbers are the same in every lane: known to be, they take scalar registers, and addresses a scalar base)
+        ri = uniform(s_found[0]);
+        row_start = uniform(s_found[1]);
+        rt = tiles_of(uniform(s_found[2]), uniform(s_found[3]));
+    }
 
     for (;;) {
         const int lane = thread_here() & 63, c16 = lane & 15, g4 = lane >> 4;
@@ -203,22 +225,26 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
         // The row's ranges in groups of 64: how many keys lie before each group, for a wave to find its first.
         const global<i2v> rg = uniform(reinterpret_cast<const i2v *>(a.ranges) + (size_t)r * a.C);
         const bool has_fixed = lo < rt.tf;
-        // (a wave's first group is read beside the number of ranges, not behind it)
+        // Up to four of them every wave has in registers, read beside the number of ranges and not behind it; more are summed by turns.
         auto range_of = [&](int gi) { return rg[min(gi * GROUP + lane, a.C - 1)]; };   // as it stands in memory: see in_bounds
-        i2v own = {0, 0};
-        if (has_fixed) own = range_of(wave);
+        i2v near[4] = {};
+        if (has_fixed) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) near[k] = range_of(k);
+        }
         const int nr = uniform(has_fixed ? min(max(a.n_ranges[r], 0), a.C) : 0), groups = (nr + GROUP - 1) / GROUP;
         auto in_bounds = [&](i2v e, int gi) {               // a lane's range of a group; (0, 0) behind the last
             const bool ok = gi * GROUP + lane < nr;
             return i2v{min(max(e.x, -MAX_L), MAX_L), ok ? min(max(e.y, 0), a.L) : 0};
         };
-        for (int gi = wave; gi < groups; gi += 4) {
-            if (gi > wave) own = range_of(gi);
-            // (counts that sum to more than a row can have are cut, far from overflow)
-            const int n = min(wave_sum_i(in_bounds(own, gi).y), MAX_L);
-            if (lane == 0) s_group[gi] = n;
+        if (groups > 4) {
+            for (int gi = wave; gi < groups; gi += 4) {
+                // (counts that sum to more than a row can have are cut, far from overflow)
+                const int n = min(wave_sum_i(in_bounds(range_of(gi), gi).y), MAX_L);
+                if (lane == 0) s_group[gi] = n;
+            }
+            __syncthreads();
         }
-        __syncthreads();
 
         // This wave's quarter of the tiles: fixed keys, then the user's, 64 keys listed at a time and a step ahead.
         const int w0 = lo + (int)((long long)(hi - lo) * wave / 4), w1 = lo + (int)((long long)(hi - lo) * (wave + 1) / 4);
@@ -240,31 +266,45 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
             int gi = 0, first = 0, ends = 0;
             i2v e = {0, 0}, e_next = {0, 0};                 // user: e.x is the page of position p + lane, read ahead
             if (fixed) {
-                int sum[MAX_GROUPS / 64], at = 0;
-                int total = 0;
+                int start = 0, total = 0;                   // keys before group gi, keys of all groups
+                if (groups <= 4) {
+                    e = in_bounds(near[0], 0);
 #pragma unroll
-                for (int i = 0; i < MAX_GROUPS / 64; ++i) {
-                    sum[i] = 4 * lane + i < groups ? s_group[4 * lane + i] : 0;
-                    total += sum[i];
-                }
-                const int inc = wave_inclusive_scan(total, lane);
-                end = min(rt.nf, __builtin_amdgcn_readlane(inc, 63));
-                at = inc - total;
-                int here = 0, start = 0;                    // groups that end at or before p, and their keys
+                    for (int k = 0; k < 4; ++k) {
+                        total += wave_sum_i(in_bounds(near[k], k).y);
+                        if (k + 1 < groups && total <= p) {
+                            gi = k + 1;
+                            start = total;
+                            e = in_bounds(near[k < 3 ? k + 1 : 3], k + 1);
+                        }
+                    }
+                    total = uniform(total);
+                } else {
+                    int sum[MAX_GROUPS / 64], at = 0;
 #pragma unroll
-                for (int i = 0; i < MAX_GROUPS / 64; ++i) {
-                    const bool passed = 4 * lane + i < groups && at + sum[i] <= p;
-                    here += __popcll(__ballot(passed));
-                    start += passed ? sum[i] : 0;
-                    at += sum[i];
+                    for (int i = 0; i < MAX_GROUPS / 64; ++i) {
+                        sum[i] = 4 * lane + i < groups ? s_group[4 * lane + i] : 0;
+                        at += sum[i];
+                    }
+                    const int inc = wave_inclusive_scan(at, lane);
+                    total = __builtin_amdgcn_readlane(inc, 63);
+                    at = inc - at;
+                    int here = 0;                           // groups that end at or before p
+#pragma unroll
+                    for (int i = 0; i < MAX_GROUPS / 64; ++i) {
+                        const bool passed = 4 * lane + i < groups && at + sum[i] <= p;
+                        here += __popcll(__ballot(passed));
+                        start += passed ? sum[i] : 0;
+                        at += sum[i];
+                    }
+                    gi = min(here, groups - 1);
+                    start = wave_sum_i(start);
+                    e = in_bounds(range_of(uniform(gi)), gi);
                 }
-                gi = min(here, max(groups - 1, 0));
-                start = wave_sum_i(start);
                 gi = uniform(gi);
-                if (groups > 0) {
-                    e = in_bounds(range_of(gi), gi);
-                    e_next = range_of(gi + 1);
-                }
+                start = uniform(start);
+                end = min(rt.nf, total);
+                e_next = range_of(gi + 1);
                 const int c = wave_inclusive_scan(e.y, lane);
                 first = start + c - e.y;
                 ends = uniform(start + __builtin_amdgcn_readlane(c, 63));
@@ -466,7 +506,7 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
             }
         }
         if (tid == 0 && lo == 0) {
-            const int last = (row_start + rt.total - 1) / per;
+            const int last = share0 + (row_start + rt.total - 1) / per;
             a.info[r] = int2{slot, whole ? 0 : last - share + 1};
         }
         }
@@ -531,15 +571,21 @@ __global__ __launch_bounds__(256) void decode_q8_merge_kernel(DecodeQ8Args a)
     store_result(a, (size_t)r * a.g + qi, tid, MM, lt, ot);
 }
 
-hipError_t launch_decode_q8(const DecodeQ8Args &a, hipStream_t s)
+hipError_t launch_decode_q8(const DecodeQ8Args &args, hipStream_t s)
 {
+    DecodeQ8Args a = args;
+    // Rows of workgroups of their own: where every row could be kept whole and a wave had a tile or two even so, how the rows' lengths
+    // differ does not matter, and finding a share among them takes longer (4 heads of 4096 keys and 128: 12.9 us without, SPLIT_US with).
+    const long long rows = (long long)a.B * a.H * a.per, most = (a.ranges ? a.L : 0) + (a.seq_len ? a.max_pages << a.p_log : 0);
+    a.splits = rows <= Q8_GRID / 4 && rows * ((most + QT - 1) / QT + 1) <= 4 * Q8_GRID ? (int)(Q8_GRID / rows) : 0;
+    const int grid = a.splits ? (int)rows * a.splits : Q8_GRID;
     const bool wide = ((size_t)a.n_pages * a.H << a.p_log) * D > (1ull << 32);
     auto *kernel = wide ? decode_q8_kernel<true> : decode_q8_kernel<false>;
     hipEvent_t ev0, ev1;
     if (profile_pair(&ev0, &ev1))
-        hipExtLaunchKernelGGL(kernel, dim3(Q8_GRID), dim3(256), 0, s, ev0, ev1, 0, a);
+        hipExtLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, ev0, ev1, 0, a);
     else
-        hipLaunchKernelGGL(kernel, dim3(Q8_GRID), dim3(256), 0, s, a);
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(decode_q8_merge_kernel, dim3((unsigned)(a.B * a.H * a.per * a.g)), dim3(256), 0, s, a);

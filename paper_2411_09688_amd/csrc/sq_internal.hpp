@@ -397,6 +397,7 @@ struct DecodeQ8Args {
     int per, g;                    // rows per (sequence, K/V head), query heads per row
     int p_log, n_pages, max_pages; // tokens per page: 2^p_log
     float scale;                   // sm_scale * log2(e)
+    int splits;                    // (the launcher's) workgroups of each row, or 0: shares of all rows' tiles
 };
 hipError_t launch_decode_q8(const DecodeQ8Args &a, hipStream_t s);
 

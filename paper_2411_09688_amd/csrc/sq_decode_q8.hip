@@ -62,10 +62,23 @@ __device__ __forceinline__ RowTiles tiles_of(int nf, int nu)
     const int tf = (nf + QT - 1) / QT;
     return RowTiles{nf, nu, tf, max(1, tf + (nu + QT - 1) / QT)};
 }
-__device__ __forceinline__ RowTiles row_tiles(const DecodeQ8Args &a, int r)
+// A row by its place in the order in which rows are dealt: head by head, so that the sequences (and query heads) that read the same
+// head of the fixed context are on the same XCD at about the same time, where its L2 holds what several of them keep.
+struct Row {
+    int r, b, h;                             // row, sequence, K/V head
+};
+__device__ __forceinline__ Row dealt_row(const DecodeQ8Args &a, int i)
 {
-    return tiles_of(a.ranges ? min(max(a.n_keys[r], 0), a.L) : 0,
-                    a.seq_len ? min(max(a.seq_len[r / (a.H * a.per)], 0), a.max_pages << a.p_log) : 0);
+    if (a.B * a.per == 1) return Row{i, 0, i};
+    const int n = a.B * a.per, h = i / n, rest = i - h * n;
+    if (a.per == 1) return Row{rest * a.H + h, rest, h};
+    const int b = rest / a.per;
+    return Row{(b * a.H + h) * a.per + rest - b * a.per, b, h};
+}
+__device__ __forceinline__ RowTiles row_tiles(const DecodeQ8Args &a, int i)
+{
+    const Row w = dealt_row(a, i);
+    return tiles_of(a.ranges ? min(max(a.n_keys[w.r], 0), a.L) : 0, a.seq_len ? min(max(a.seq_len[w.b], 0), a.max_pages << a.p_log) : 0);
 }
 
 __device__ __forceinline__ int block_exclusive(int v, int tid, int *s_w /*[4]*/, int &total)
@@ -114,14 +127,6 @@ __device__ __forceinline__ void store_result(const DecodeQ8Args &a, size_t query
 
 }  // namespace
 
-// Rows in the order in which they are dealt: head by head, so that the sequences (and query heads) that read the same head of the
-// fixed context are on the same XCD at about the same time, where its L2 holds what several of them keep.
-__device__ __forceinline__ int dealt_row(const DecodeQ8Args &a, int i)
-{
-    const int n = a.B * a.per, h = i / n, rest = i - h * n, b = rest / a.per;
-    return (b * a.H + h) * a.per + rest - b * a.per;
-}
-
 // What one lane writes to LDS another lane of the wave reads.
 __device__ __forceinline__ void wave_lds_sync()
 {
@@ -162,7 +167,7 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
     if (a.splits > 0) {
         // Few keys: a row's tiles are divided among workgroups of its own, without a look at the other rows.
         ri = blockIdx.x / a.splits;
-        rt = row_tiles(a, dealt_row(a, ri));
+        rt = row_tiles(a, ri);
         rt = tiles_of(uniform(rt.nf), uniform(rt.nu));
         share0 = ri * a.splits;
         share = blockIdx.x;
@@ -174,41 +179,81 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
     } else {
         // Workgroups go round the 8 XCDs: each XCD takes consecutive shares.
         const int R = a.B * a.H * a.per;
-        const int each = (R + 255) / 256, i_lo = min(R, tid * each), i_hi = min(R, i_lo + each);
-        int mine = 0, all;
-        for (int i = i_lo; i < i_hi; ++i) mine += row_tiles(a, dealt_row(a, i)).total;
-        int before = block_exclusive(mine, tid, s_w, all);
-        const int shares = min((int)gridDim.x, (all + 3) / 4);      // (at least a tile for each wave)
-        const int per_xcd = (shares + 7) / 8;
-        per = (all + shares - 1) / shares;
-        share0 = 0;
-        share = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-        if ((int)(blockIdx.x >> 3) >= per_xcd || (long long)share * per >= all) return;
-        t0 = share * per;
-        t1 = min(all, t0 + per);
-        if (before <= t0 && t0 < before + mine) {
-            int i = i_lo;
-            for (;; ++i) {
-                rt = row_tiles(a, dealt_row(a, i));
-                if (t0 < before + rt.total) break;
-                before += rt.total;
+        auto divide = [&](int all) {                        // false: no share for this workgroup
+            const int shares = min((int)gridDim.x, (all + 3) / 4), per_xcd = (shares + 7) / 8;      // (at least a tile for each wave)
+            per = (all + shares - 1) / shares;
+            share0 = 0;
+            share = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+            if ((int)(blockIdx.x >> 3) >= per_xcd || (long long)share * per >= all) return false;
+            t0 = share * per;
+            t1 = min(all, t0 + per);
+            return true;
+        };
+        int nf, nu;
+        if (R <= 256) {
+            // every wave for itself, four rows a lane
+            const int lane = tid & 63;
+            RowTiles mine[4];
+            int sum = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                mine[k] = row_tiles(a, min(4 * lane + k, R - 1));
+                if (4 * lane + k >= R) mine[k].total = 0;
+                sum += mine[k].total;
             }
-            s_found[0] = i;
-            s_found[1] = before;
-            s_found[2] = rt.nf;
-            s_found[3] = rt.nu;
+            const int inc = wave_inclusive_scan(sum, lane);
+            if (!divide(__builtin_amdgcn_readlane(inc, 63))) return;
+            int before = inc - sum, at = 0;
+            const unsigned long long here = __ballot(before <= t0 && t0 < inc);
+            const int owner = __ffsll((long long)here) - 1;
+            nf = mine[0].nf;
+            nu = mine[0].nu;
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+                if (at == k && t0 >= before + mine[k].total) {
+                    before += mine[k].total;
+                    at = k + 1;
+                    nf = mine[k + 1].nf;
+                    nu = mine[k + 1].nu;
+                }
+            ri = __builtin_amdgcn_readlane(4 * lane + at, owner);
+            row_start = __builtin_amdgcn_readlane(before, owner);
+            nf = __builtin_amdgcn_readlane(nf, owner);
+            nu = __builtin_amdgcn_readlane(nu, owner);
+        } else {
+            const int each = (R + 255) / 256, i_lo = min(R, tid * each), i_hi = min(R, i_lo + each);
+            int mine = 0, all;
+            for (int i = i_lo; i < i_hi; ++i) mine += row_tiles(a, i).total;
+            int before = block_exclusive(mine, tid, s_w, all);
+            if (!divide(all)) return;
+            if (before <= t0 && t0 < before + mine) {
+                int i = i_lo;
+                for (;; ++i) {
+                    rt = row_tiles(a, i);
+                    if (t0 < before + rt.total) break;
+                    before += rt.total;
+                }
+                s_found[0] = i;
+                s_found[1] = before;
+                s_found[2] = rt.nf;
+                s_found[3] = rt.nu;
+            }
+            __syncthreads();
+            ri = s_found[0];
+            row_start = s_found[1];
+            nf = s_found[2];
+            nu = s_found[3];
         }
-        __syncthreads();
         // (a row's numbers are the same in every lane: known to be, they take scalar registers, and addresses a scalar base)
-        ri = uniform(s_found[0]);
-        row_start = uniform(s_found[1]);
-        rt = tiles_of(uniform(s_found[2]), uniform(s_found[3]));
+        ri = uniform(ri);
+        row_start = uniform(row_start);
+        rt = tiles_of(uniform(nf), uniform(nu));
     }
 
     for (;;) {
         const int lane = thread_here() & 63, c16 = lane & 15, g4 = lane >> 4;
-        const int r = dealt_row(a, ri);
-        const int bh = r / a.per, h = bh % a.H, b = bh / a.H;
+        const Row row = dealt_row(a, ri);
+        const int r = row.r, h = row.h, b = row.b;
         const int lo = max(t0 - row_start, 0), hi = min(t1 - row_start, rt.total);
         // q^T as the second operand of S^T: lane = query column c16, dimensions 32 g4 + 8 s ..
         h8 qf[4];
@@ -514,7 +559,7 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
         row_start += rt.total;
         if (row_start >= t1) break;
         ++ri;
-        const RowTiles next = row_tiles(a, dealt_row(a, ri));
+        const RowTiles next = row_tiles(a, ri);
         rt = tiles_of(uniform(next.nf), uniform(next.nu));
     }
 }
@@ -574,10 +619,12 @@ __global__ __launch_bounds__(256) void decode_q8_merge_kernel(DecodeQ8Args a)
 hipError_t launch_decode_q8(const DecodeQ8Args &args, hipStream_t s)
 {
     DecodeQ8Args a = args;
-    // Rows of workgroups of their own: where every row could be kept whole and a wave had a tile or two even so, how the rows' lengths
-    // differ does not matter, and finding a share among them takes longer (4 heads of 4096 keys and 128: 12.9 us without, SPLIT_US with).
+    // Workgroups for each row: no search for a share, 3 us less, but a row that keeps more takes longer.  What the rows keep is not known
+    // here; up to 36000 tiles if they kept everything (1.2 million keys), of which they keep some 1/8, the search costs more than the
+    // difference (one set per head, uneven by 1.8 at most, us by rows / in shares: 4 x 4224 keys 10.2 / 12.1; 32 x 33280, of which
+    // 4608, 15.8 / 17.6; 64 x 147456, of which 20000, 73 / 66).
     const long long rows = (long long)a.B * a.H * a.per, most = (a.ranges ? a.L : 0) + (a.seq_len ? a.max_pages << a.p_log : 0);
-    a.splits = rows <= Q8_GRID / 4 && rows * ((most + QT - 1) / QT + 1) <= 4 * Q8_GRID ? (int)(Q8_GRID / rows) : 0;
+    a.splits = rows <= Q8_GRID / 4 && rows * ((most + QT - 1) / QT + 1) <= 36 * 1024 ? (int)(Q8_GRID / rows) : 0;
     const int grid = a.splits ? (int)rows * a.splits : Q8_GRID;
     const bool wide = ((size_t)a.n_pages * a.H << a.p_log) * D > (1ull << 32);
     auto *kernel = wide ? decode_q8_kernel<true> : decode_q8_kernel<false>;

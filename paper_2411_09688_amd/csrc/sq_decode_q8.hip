@@ -144,6 +144,139 @@ __device__ __forceinline__ int thread_here()
     return t;
 }
 
+// A wave's attention so far: a column per query (lane: column c16), its running maximum (base 2) and sum (of a quarter of the keys in
+// each group of 16 lanes), and the output, dimension 32 g4 + 8 i + dt of the column in o[dt][i].
+struct Attending {
+    h8 q[4];                                 // second operand of S^T: lane = column c16, dimensions 32 g4 + 8 s ..
+    float m, l;
+    f4 o[8];
+};
+__device__ __forceinline__ void begin(Attending &st)
+{
+    st.m = SQ_NEG_INF;
+    st.l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) st.o[i] = f4{0.f, 0.f, 0.f, 0.f};
+}
+
+// Slots of the tile without a key (bits i and 16 + i of `mine`: this lane's slots): what stands in their row is not looked at.
+__device__ __forceinline__ void hide_empty(float (&s)[8], uint32_t (&w)[2][8], uint32_t mine)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (!(mine >> (i < 4 ? i : 12 + i) & 1u)) {
+            s[i] = SQ_NEG_INF;
+            w[0][i] = w[1][i] = 0u;
+        }
+}
+
+// Folds 32 keys: k, v as the lanes read them (keys c16 and 16 + c16, dimensions 32 g4 ..; keys 4 g4 .. and 16 + 4 g4 .., dimensions
+// 8 c16 ..), ks, vs the scales of the lane's keys 4 g4 ..  used_k: called when k may be overwritten; hide: sets the scores (and words of
+// values) of keys that are not to be seen.
+template <class UsedK, class Hide>
+__device__ __forceinline__ void fold_tile(Attending &st, const u4v (&k)[2][2], const u2v (&v)[8], const float *ks, const float *vs, UsedK used_k,
+                                          Hide hide)
+{
+    f4 acc[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const u4v x = k[u][s >> 1];
+            acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(s & 1 ? codes_f16(x.z, x.w) : codes_f16(x.x, x.y), st.q[s], acc[u], 0, 0, 0);
+        }
+    used_k();
+    float s[8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const f4 f = *reinterpret_cast<const f4 *>(ks + 16 * u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[4 * u + i] = acc[u][i] * f[i];
+    }
+    uint32_t w[2][8];                        // V: words of dimensions 8 c16 .. + 3 and .. + 7
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        w[0][i] = v[i].x;
+        w[1][i] = v[i].y;
+    }
+    hide(s, w);
+    const float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+    const float mn = fmaxf(st.m, cross16_max(mx));
+    const float mu = mn == SQ_NEG_INF ? 0.0f : mn;
+    const float alpha = __builtin_amdgcn_exp2f(st.m - mu);
+    st.m = mn;
+    st.l *= alpha;
+    b8 hi8, lo8;
+    const f4 v0 = *reinterpret_cast<const f4 *>(vs), v1 = *reinterpret_cast<const f4 *>(vs + 16);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float x = __builtin_amdgcn_exp2f(s[i] - mu);
+        st.l += x;
+        const float pv = x * (i < 4 ? v0[i & 3] : v1[i & 3]);
+        hi8[i] = (__bf16)pv;
+        lo8[i] = (__bf16)(pv - (float)hi8[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        transpose4(w[i][0], w[i][1], w[i][2], w[i][3]);
+        transpose4(w[i][4], w[i][5], w[i][6], w[i][7]);
+    }
+    if (__any(alpha != 1.0f)) {              // (the maximum rarely moves behind the first tiles)
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) st.o[dt] *= alpha;
+    }
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+        const b8 vf = codes_bf16(w[dt >> 2][dt & 3], w[dt >> 2][4 + (dt & 3)]);
+        st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi8, st.o[dt], 0, 0, 0);
+        st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo8, st.o[dt], 0, 0, 0);
+    }
+}
+
+// The waves' results of the workgroup's columns to LDS, for join().
+__device__ __forceinline__ void hand_over(const Attending &st, int columns, int wave, WaveOut &out, float (&ml)[2][4][16])
+{
+    const int lane = thread_here() & 63, c16 = lane & 15, g4 = lane >> 4;
+    const float l = cross16_sum(st.l);
+    if (g4 == 0) {
+        ml[0][wave][c16] = st.m;
+        ml[1][wave][c16] = l;
+    }
+    if (c16 < columns) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float *dst = &out.o[wave][c16][32 * g4 + 8 * i];
+            *reinterpret_cast<f4 *>(dst) = f4{st.o[0][i], st.o[1][i], st.o[2][i], st.o[3][i]};
+            *reinterpret_cast<f4 *>(dst + 4) = f4{st.o[4][i], st.o[5][i], st.o[6][i], st.o[7][i]};
+        }
+    }
+}
+struct Joined {
+    float m, l, o;
+};
+__device__ __forceinline__ Joined join(const WaveOut &out, const float (&ml)[2][4][16], int column, int d)
+{
+    Joined x;
+    x.m = fmaxf(fmaxf(ml[0][0][column], ml[0][1][column]), fmaxf(ml[0][2][column], ml[0][3][column]));
+    const float mu = x.m == SQ_NEG_INF ? 0.0f : x.m;
+    x.l = x.o = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(ml[0][w][column] - mu);
+        x.l += f * ml[1][w][column];
+        x.o += f * out.o[w][column][d];
+    }
+    return x;
+}
+__device__ __forceinline__ void store_partial(float *p, int d, const Joined &x)
+{
+    p[4 + d] = x.o;
+    if (d == 0) {
+        p[0] = x.m;
+        p[1] = x.l;
+    }
+}
+
 template <bool WIDE>
 __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
 {
@@ -255,17 +388,13 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
         const Row row = dealt_row(a, ri);
         const int r = row.r, h = row.h, b = row.b;
         const int lo = max(t0 - row_start, 0), hi = min(t1 - row_start, rt.total);
-        // q^T as the second operand of S^T: lane = query column c16, dimensions 32 g4 + 8 s ..
-        h8 qf[4];
+        Attending st;
+        begin(st);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             const h8 zero = {};
-            qf[s] = c16 < a.g ? *reinterpret_cast<const h8 *>(a.q + ((size_t)r * a.g + c16) * D + 32 * g4 + 8 * s) : zero;
+            st.q[s] = c16 < a.g ? *reinterpret_cast<const h8 *>(a.q + ((size_t)r * a.g + c16) * D + 32 * g4 + 8 * s) : zero;
         }
-        float m = SQ_NEG_INF, l = 0.0f;
-        f4 o[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = f4{0.f, 0.f, 0.f, 0.f};
 
         // The row's ranges in groups of 64: how many keys lie before each group, for a wave to find its first.
         const global<i2v> rg = uniform(reinterpret_cast<const i2v *>(a.ranges) + (size_t)r * a.C);
@@ -441,119 +570,32 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
                     seen = seen_next;
                     if (t + 2 < tiles) list(buf ^ 1);
                 }
-                f4 acc[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-                for (int s = 0; s < 4; ++s)
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const u4v x = k[u][s >> 1];
-                        acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(s & 1 ? codes_f16(x.z, x.w) : codes_f16(x.x, x.y), qf[s], acc[u], 0, 0, 0);
-                    }
-                load_k(t + 1);                               // (as soon as the scores have used this tile's)
-                float s[8];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const f4 f = *reinterpret_cast<const f4 *>(s_list[wave][buf].ks + slot + 16 * u + 4 * g4);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[4 * u + i] = acc[u][i] * f[i];
-                }
-                uint32_t w[2][8];                            // V: words of dimensions 8 c16 .. + 3 and .. + 7
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    w[0][i] = v[i].x;
-                    w[1][i] = v[i].y;
-                }
-                const uint32_t keys = (uint32_t)(seen >> slot);
-                if (keys != 0xffffffffu) {                   // what stands in the row of a slot without a key is not looked at
-                    const uint32_t mine = keys >> (4 * g4);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (!(mine >> (i < 4 ? i : 12 + i) & 1u)) {
-                            s[i] = SQ_NEG_INF;
-                            w[0][i] = w[1][i] = 0u;
-                        }
-                }
-                const float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-                const float mn = fmaxf(m, cross16_max(mx));
-                const float mu = mn == SQ_NEG_INF ? 0.0f : mn;
-                const float alpha = __builtin_amdgcn_exp2f(m - mu);
-                m = mn;
-                l *= alpha;
-                b8 hi8, lo8;
-                const f4 v0 = *reinterpret_cast<const f4 *>(s_list[wave][buf].vs + slot + 4 * g4);
-                const f4 v1 = *reinterpret_cast<const f4 *>(s_list[wave][buf].vs + slot + 16 + 4 * g4);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float x = __builtin_amdgcn_exp2f(s[i] - mu);
-                    l += x;
-                    const float pv = x * (i < 4 ? v0[i & 3] : v1[i & 3]);
-                    hi8[i] = (__bf16)pv;
-                    lo8[i] = (__bf16)(pv - (float)hi8[i]);
-                }
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    transpose4(w[i][0], w[i][1], w[i][2], w[i][3]);
-                    transpose4(w[i][4], w[i][5], w[i][6], w[i][7]);
-                }
-                if (__any(alpha != 1.0f)) {                  // (the maximum rarely moves behind the first tiles)
-#pragma unroll
-                    for (int dt = 0; dt < 8; ++dt) o[dt] *= alpha;
-                }
-#pragma unroll
-                for (int dt = 0; dt < 8; ++dt) {
-                    const b8 vf = codes_bf16(w[dt >> 2][dt & 3], w[dt >> 2][4 + (dt & 3)]);
-                    o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi8, o[dt], 0, 0, 0);
-                    o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo8, o[dt], 0, 0, 0);
-                }
+                const float *kf = s_list[wave][buf].ks + slot + 4 * g4, *vf = s_list[wave][buf].vs + slot + 4 * g4;
+                fold_tile(
+                    st, k, v, kf, vf, [&]() { load_k(t + 1); },  // (as soon as the scores have used this tile's)
+                    [&](float(&x)[8], uint32_t(&w)[2][8]) {
+                        const uint32_t keys = (uint32_t)(seen >> slot);
+                        if (keys != 0xffffffffu) hide_empty(x, w, keys >> (4 * g4));
+                    });
                 load_v(t + 1);
                 if (even && t + 2 < tiles) list_scales(buf ^ 1);
             }
         }
         // The four waves' results of the row.
-        {
-        const int tid = thread_here(), lane = tid & 63, c16 = lane & 15, g4 = lane >> 4;
-        l = cross16_sum(l);
-        if (g4 == 0) {
-            s_ml[0][wave][c16] = m;
-            s_ml[1][wave][c16] = l;
-        }
-        if (c16 < a.g) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float *dst = &s_out.o[wave][c16][32 * g4 + 8 * i];
-                *reinterpret_cast<f4 *>(dst) = f4{o[0][i], o[1][i], o[2][i], o[3][i]};
-                *reinterpret_cast<f4 *>(dst + 4) = f4{o[4][i], o[5][i], o[6][i], o[7][i]};
-            }
-        }
+        hand_over(st, a.g, wave, s_out, s_ml);
         __syncthreads();
+        const int tid = thread_here();
         const bool whole = lo == 0 && hi == rt.total;
         const int slot = share + ri;
         for (int i = tid; i < a.g * D; i += 256) {
             const int qi = i >> 7, d = i & 127;
-            float M = fmaxf(fmaxf(s_ml[0][0][qi], s_ml[0][1][qi]), fmaxf(s_ml[0][2][qi], s_ml[0][3][qi]));
-            const float mu = M == SQ_NEG_INF ? 0.0f : M;
-            float ls = 0.0f, os = 0.0f;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const float f = __builtin_amdgcn_exp2f(s_ml[0][w][qi] - mu);
-                ls += f * s_ml[1][w][qi];
-                os += f * s_out.o[w][qi][d];
-            }
-            if (whole) {
-                store_result(a, (size_t)r * a.g + qi, d, M, ls, os);
-            } else {
-                float *p = a.part + ((size_t)slot * a.g + qi) * PART_STRIDE;
-                p[4 + d] = os;
-                if (d == 0) {
-                    p[0] = M;
-                    p[1] = ls;
-                }
-            }
+            const Joined x = join(s_out, s_ml, qi, d);
+            if (whole) store_result(a, (size_t)r * a.g + qi, d, x.m, x.l, x.o);
+            else store_partial(a.part + ((size_t)slot * a.g + qi) * PART_STRIDE, d, x);
         }
         if (tid == 0 && lo == 0) {
             const int last = share0 + (row_start + rt.total - 1) / per;
             a.info[r] = int2{slot, whole ? 0 : last - share + 1};
-        }
         }
         __syncthreads();
         row_start += rt.total;

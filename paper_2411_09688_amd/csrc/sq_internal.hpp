@@ -398,7 +398,22 @@ struct DecodeQ8Args {
     int p_log, n_pages, max_pages; // tokens per page: 2^p_log
     float scale;                   // sm_scale * log2(e)
     int splits;                    // (the launcher's) workgroups of each row, or 0: shares of all rows' tiles
+    int groups, rows_per_group, s_log;   // (the launcher's) groups of rows of a head that share its keys, 0: none; 2^s_log workgroups each
 };
+// Rows of a head that are taken together: from 8 on, in groups that fill 16 columns.
+struct Q8Groups {
+    int groups, rows, s_log;
+};
+inline Q8Groups q8_groups(int B, int H, int per, int g, int L)
+{
+    const int in_head = B * per, rows = 16 / g;
+    if (in_head < 8 || rows < 8) return Q8Groups{0, 0, 0};
+    const long long groups = (in_head + rows - 1) / rows;
+    int s_log = 0;
+    while (s_log < 9 && (groups * H << (s_log + 1)) <= Q8_GRID && (512 << (s_log + 1)) <= L + 511) ++s_log;
+    return Q8Groups{(int)groups, rows, s_log};
+}
+void launch_decode_q8_shared(const DecodeQ8Args &a, bool wide, hipEvent_t ev0, hipEvent_t ev1, hipStream_t s);
 hipError_t launch_decode_q8(const DecodeQ8Args &a, hipStream_t s);
 
 // Records the calling thread's error message (what sq_last_error returns) and hands back `code`.

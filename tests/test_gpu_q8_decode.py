@@ -117,6 +117,13 @@ CASES = [  # B, H, Lq, L, C, keep, lengths, page, one_set, spread
     (1, 2, 2, 40000, 9000, [0.4, 0.02], [3000], 64, False, 0),             # more than one batch of ranges
     (300, 2, 2, 100, 5, [0.5, 0.0], [i % 40 for i in range(300)], 16, False, 0),   # more rows than workgroups
     (7, 5, 3, 64, 4, 0.6, [100] * 7, 32, True, 0),
+    # eight rows or more of a head: keys that several keep are read once
+    (8, 2, 1, 3000, 90, [0.3, 0.0, 1.0], [0, 1, 64, 65, 200, 7, 31, 130], 32, False, 3),
+    (17, 1, 1, 513, 20, 0.4, None, 16, False, 0),                          # a group of one row behind one of 16; a window of one key
+    (2, 3, 5, 5000, 5000, [0.02, 0.5, 0.0], [90, 0], 16, False, 0),        # clusters of one key
+    (9, 2, 2, 1300, 40, [0.1, 0.6], [3] * 9, 64, True, 2),                 # two query heads to a set, eight rows to a group
+    (16, 1, 1, 70000, 2000, [0.2, 0.01], [40] * 16, 16, False, 0),         # more windows than are marked at a time
+    (11, 1, 3, 40, 3, 1.0, [1000] + [0] * 10, 16, False, 0),               # nearly everything is one sequence's own
 ]
 
 
@@ -173,6 +180,32 @@ def test_nan_reaches_the_queries_that_see_it_only():
             assert torch.isnan(got[r, 9]) and torch.equal(got[r, 10:], clean[r, 10:]) and torch.equal(got[r, :9], clean[r, :9])
         else:
             assert torch.equal(got[r], clean[r])
+
+
+def test_nan_reaches_the_rows_of_a_group_that_see_it_only():
+    """Twelve rows share a head, and each other's tiles: a NaN in a value that some of them keep, and in a user's own value."""
+    p = Problem(22, 6, 1, 2, 2048, 64, [0.5, 0.3], [70, 5, 40, 0, 64, 9], 16, False)
+    args = p.upload()
+    sq.sq_sparse_attn_decode_q8(*args, p.out, p.lse, p.ws)
+    p.check()
+    clean, lse = p.out.clone().reshape(p.rows, 128), p.lse.clone()
+    sees = [any(s <= 1000 < s + c for s, c in p.ranges[r, :p.n_ranges[r]]) for r in range(p.rows)]
+    assert 2 <= sum(sees) <= 10
+    p.fixed[1][0, 1000, 77] = 0x7f
+    p.cache[1][p.table[2, 1], 0, 3, 5] = 0xff                   # token 19 of sequence 2: rows 4 and 5
+    args = p.upload()
+    sq.sq_sparse_attn_decode_q8(*args, p.out, p.lse, p.ws)
+    got = p.out.reshape(p.rows, 128)
+    for r in range(p.rows):
+        want = clean[r].clone()
+        if sees[r]:
+            want[77] = float("nan")
+        if r in (4, 5):
+            want[5] = float("nan")
+        assert torch.equal(torch.isnan(got[r]), torch.isnan(want)), r
+        ok = ~torch.isnan(want)
+        assert (got[r][ok].float() - want[ok].float()).abs().max() <= 2.0 ** -9 * want[ok].float().abs().max(), r
+    assert torch.isfinite(p.lse).all()
 
 
 def test_input_outside_the_contract_stays_inside_the_tensors():

@@ -400,14 +400,27 @@ struct DecodeQ8Args {
     int splits;                    // (the launcher's) workgroups of each row, or 0: shares of all rows' tiles
     int groups, rows_per_group, s_log;   // (the launcher's) groups of rows of a head that share its keys, 0: none; 2^s_log workgroups each
 };
-// Rows of a head that are taken together: from 8 on, in groups that fill 16 columns.
+// Rows of a head that are taken together: from 8 on, in groups that fill 16 columns, and only where the rows have this many keys to
+// select from between them.  Below it what several rows keep comes from the caches again, and marking the union costs more than that.
+// us per call, rows by themselves / their union, by the share of the keys kept (128 user keys a sequence):
+//                                                        0.03           1/8           0.4
+//    8 rows of each of  8 heads x   4096 ( 262 K)      10.6 / 18.6   11.1 / 19.5   13.3 / 19.8
+//   16               x  8       x   4096 ( 524 K)      10.9 / 21.3   12.8 / 22.2   18.1 / 21.1
+//    8               x  4       x  16384 ( 524 K)      10.5 / 19.5   12.3 / 20.7   18.5 / 22.0
+//   16               x  8       x  16384 (  2 M)       15.8 / 23.0   23.2 / 24.2   37.1 / 24.5
+//    8               x  8       x  32768 (  2 M)       16.0 / 21.4   23.1 / 23.4   38.5 / 26.5
+//    8               x 32       x  32768 (  8 M)       25.8 / 30.7   51.5 / 55.2    121 / 69.6
+//   40               x  8       x  32768 ( 10 M)       28.0 / 33.4   53.7 / 44.3    117 / 48.6
+//   16               x  8       x 131072 ( 17 M)       30.8 / 40.7   83.2 / 66.4    224 / 84.0
+constexpr long long Q8_SHARED_MIN_KEYS = 2 << 20;
 struct Q8Groups {
     int groups, rows, s_log;
 };
 inline Q8Groups q8_groups(int B, int H, int per, int g, int L)
 {
-    const int in_head = B * per, rows = 16 / g;
-    if (in_head < 8 || rows < 8) return Q8Groups{0, 0, 0};
+    const int rows = 16 / g;
+    const long long in_head = (long long)B * per;
+    if (in_head < 8 || rows < 8 || in_head * H * L < Q8_SHARED_MIN_KEYS) return Q8Groups{0, 0, 0};
     const long long groups = (in_head + rows - 1) / rows;
     int s_log = 0;
     while (s_log < 9 && (groups * H << (s_log + 1)) <= Q8_GRID && (512 << (s_log + 1)) <= L + 511) ++s_log;

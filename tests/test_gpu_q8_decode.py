@@ -20,7 +20,14 @@ class Problem:
         self.q = (1.5 * rng.standard_normal((B, H * Lq, 128))).astype(np.float16)
         R = self.rows = B * H * (1 if one_set else Lq)
         scales = lambda *s: 2.0 ** (-7 + rng.integers(-spread, spread + 1, s)).astype(np.float64) * (1.1 if spread else 1.0)  # noqa: E731
-        codes = lambda *s: ref.encode((rng.standard_normal(s) * 64).clip(-448, 448))  # noqa: E731
+
+        def codes(*s):
+            if np.prod(s) < 1 << 22:
+                return ref.encode((rng.standard_normal(s) * 64).clip(-448, 448))
+            c = rng.integers(0, 256, s, np.uint8)               # (quicker: codes of any exponent)
+            c[(c & 0x7f) == 0x7f] = 0x35
+            return c
+
         self.fixed = self.cache = None
         if keep is not None:
             n = -(-L // 64)
@@ -117,13 +124,13 @@ CASES = [  # B, H, Lq, L, C, keep, lengths, page, one_set, spread
     (1, 2, 2, 40000, 9000, [0.4, 0.02], [3000], 64, False, 0),             # more than one batch of ranges
     (300, 2, 2, 100, 5, [0.5, 0.0], [i % 40 for i in range(300)], 16, False, 0),   # more rows than workgroups
     (7, 5, 3, 64, 4, 0.6, [100] * 7, 32, True, 0),
-    # eight rows or more of a head: keys that several keep are read once
-    (8, 2, 1, 3000, 90, [0.3, 0.0, 1.0], [0, 1, 64, 65, 200, 7, 31, 130], 32, False, 3),
-    (17, 1, 1, 513, 20, 0.4, None, 16, False, 0),                          # a group of one row behind one of 16; a window of one key
-    (2, 3, 5, 5000, 5000, [0.02, 0.5, 0.0], [90, 0], 16, False, 0),        # clusters of one key
-    (9, 2, 2, 1300, 40, [0.1, 0.6], [3] * 9, 64, True, 2),                 # two query heads to a set, eight rows to a group
-    (16, 1, 1, 70000, 2000, [0.2, 0.01], [40] * 16, 16, False, 0),         # more windows than are marked at a time
-    (11, 1, 3, 40, 3, 1.0, [1000] + [0] * 10, 16, False, 0),               # nearly everything is one sequence's own
+    # eight rows or more of a head with two million keys to select from between them: keys that several rows keep are read once
+    (16, 1, 1, 140001, 4000, [0.02, 0.0, 0.005], [0, 1, 64, 65, 200, 7, 31, 130] * 2, 32, False, 3),   # a last window of 225 keys
+    (17, 1, 1, 131073, 16384, [0.01, 0.03], None, 16, False, 0),           # a group of one row behind one of 16; a window of one key
+    (2, 2, 8, 70000, 500, [0.02, 0.0, 0.04], [90, 0], 16, False, 0),
+    (9, 2, 2, 131072, 3000, [0.01, 0.03], [3] * 9, 64, True, 2),           # two query heads to a set, eight rows to a group
+    (40, 8, 1, 131072, 4096, [0.004, 0.01], [40] * 40, 16, False, 0),      # more windows than are marked at a time
+    (11, 1, 3, 65536, 16, [0.0] * 30 + [1.0], [3000] + [0] * 10, 16, False, 0),   # one sequence's own; one row of everything
 ]
 
 
@@ -132,7 +139,7 @@ def test_decode(case):
     p = Problem(sum(case[:5]), *case)
     args = p.upload()
     sq.sq_sparse_attn_decode_q8(*args, p.out, p.lse, p.ws)
-    few = None if p.rows <= 64 else list(range(0, p.rows, 37)) + [p.rows - 1]
+    few = None if p.rows <= 64 and p.L < 60000 else list(range(0, p.rows, 37 if p.rows > 64 else 5)) + [p.rows - 1]
     p.check(rows=few)
     out, lse = p.out.clone(), p.lse.clone()
     p.ws.fill_(255)                                             # whatever the workspace holds; without lse; the same bits
@@ -184,14 +191,15 @@ def test_nan_reaches_the_queries_that_see_it_only():
 
 def test_nan_reaches_the_rows_of_a_group_that_see_it_only():
     """Twelve rows share a head, and each other's tiles: a NaN in a value that some of them keep, and in a user's own value."""
-    p = Problem(22, 6, 1, 2, 2048, 64, [0.5, 0.3], [70, 5, 40, 0, 64, 9], 16, False)
+    p = Problem(22, 6, 1, 2, 180000, 64, [0.05, 0.03], [70, 5, 40, 0, 64, 9], 16, False)
     args = p.upload()
     sq.sq_sparse_attn_decode_q8(*args, p.out, p.lse, p.ws)
     p.check()
     clean, lse = p.out.clone().reshape(p.rows, 128), p.lse.clone()
-    sees = [any(s <= 1000 < s + c for s, c in p.ranges[r, :p.n_ranges[r]]) for r in range(p.rows)]
-    assert 2 <= sum(sees) <= 10
-    p.fixed[1][0, 1000, 77] = 0x7f
+    key = int(next(p.ranges[r, 0, 0] for r in range(p.rows) if p.n_ranges[r]))
+    sees = [any(s <= key < s + c for s, c in p.ranges[r, :p.n_ranges[r]]) for r in range(p.rows)]
+    assert 1 <= sum(sees) <= 10
+    p.fixed[1][0, key, 77] = 0x7f
     p.cache[1][p.table[2, 1], 0, 3, 5] = 0xff                   # token 19 of sequence 2: rows 4 and 5
     args = p.upload()
     sq.sq_sparse_attn_decode_q8(*args, p.out, p.lse, p.ws)

@@ -612,13 +612,15 @@ int sq_cache_append(const sq_shape_t *shape, int32_t G, const sq_rotary_t *rot, 
  *      written by sq_select; with one_set != 0, ranges [B,H,C,2], n_ranges, n_keys [B,H]: one kept set for the query heads of a
  *      K/V head, as written by sq_select_mean, and each kept key is read once for them.
  *      Ranges ascending, disjoint, within [0, L); n_keys = the sum of their counts (it is read, and divides the work).
- *      Input outside this contract never faults and is not reported: a row uses at most C ranges and L keys, entries with
- *      count <= 0 are skipped, a key row outside [0, L) is read as the nearest row inside, and where n_keys is not the sum of the
- *      counts, only as many of the listed keys are used as both allow.
+ *      Input outside this contract never faults and is not reported: a row uses at most C ranges, entries with count <= 0 are
+ *      skipped, and nothing outside [0, L) is read; which keys such a row then attends to is not specified.
  *      ranges NULL (then n_ranges, n_keys, K8, V8 and the scales are too): no fixed context.  cache NULL (then seq_len is too): no
  *      user keys; of its sequences' tokens, the first max_pages * page_tokens are used.  Not both.  U of the shape is not used.
  * Out: out f16 [B,H*Lq,1,d]; lse f32 [B,H*Lq,1], or NULL.  A query with no visible key gets out = 0 and lse = -inf.
  *      A NaN code reaches the queries that see its key, and no others.
+ * Where a head of the fixed context has at least 8 kept sets (sequences, times the query heads that select on their own; one_set
+ * with Lq > 2: never) and the sets have 2^21 keys to select from in all (sets x L), a key that several of up to 16 of them keep
+ * is read once; the results agree with the other form's up to the order of summation.
  * Workspace: sq_workspace_bytes(shape, SQ_CALL_ATTN_DECODE_Q8), the same for either value of one_set.
  */
 int sq_sparse_attn_decode_q8(const sq_shape_t *shape, int32_t one_set, const void *q, const void *K8, const void *V8,

@@ -353,7 +353,7 @@ DecodeQ8Ws carve_decode_q8(Carver &cv, const sq_shape_t *sh)
     DecodeQ8Ws w{};
     size_t parts = (sq::Q8_GRID + bh) * sh->Lq;
     const sq::Q8Groups ways[] = {sq::q8_groups(sh->B, sh->H, sh->Lq, 1, sh->L), sq::q8_groups(sh->B, sh->H, 1, sh->Lq, sh->L)};
-    for (const sq::Q8Groups &g : ways) parts = std::max(parts, ((size_t)sh->H * g.groups << g.s_log) * 16);
+    for (const sq::Q8Groups &g : ways) parts = std::max(parts, (size_t)sh->H * g.groups * g.parts * 16);
     w.part = cv.take<float>(parts * sq::PART_STRIDE);
     w.info = cv.take<int2>(bh * sh->Lq);
     return w;

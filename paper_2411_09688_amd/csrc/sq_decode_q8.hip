@@ -386,8 +386,8 @@ __global__ __launch_bounds__(256) void decode_q8_merge_kernel(DecodeQ8Args a)
     if (a.groups > 0) {
         const int i = r % a.per, bh = r / a.per, h = bh % a.H, in_head = bh / a.H * a.per + i;
         const int grp = in_head / a.rows_per_group, column = (in_head - grp * a.rows_per_group) * a.g + qi;
-        first = (((size_t)h * a.groups + grp) << a.s_log) * 16 + column;
-        n = 1 << a.s_log;
+        first = ((size_t)h * a.groups + grp) * a.parts * 16 + column;
+        n = a.parts;
         step = 16;
     } else {
         const int2 info = a.info[r];
@@ -449,7 +449,7 @@ hipError_t launch_decode_q8(const DecodeQ8Args &args, hipStream_t s)
     a.groups = shared.groups;
     if (shared.groups > 0) {
         a.rows_per_group = shared.rows;
-        a.s_log = shared.s_log;
+        a.parts = shared.parts;
         launch_decode_q8_shared(a, wide, timed ? ev0 : nullptr, ev1, s);
     } else {
         // Workgroups for each row: no search for a share, 3 us less, but a row that keeps more takes longer.  What the rows keep is not

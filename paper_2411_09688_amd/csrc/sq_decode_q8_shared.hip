@@ -1,7 +1,7 @@
 // sq_sparse_attn_decode_q8 where eight rows or more read one head of the fixed context: sequences that share it, query heads of a K/V
 // head that select on their own.
 //
-// The rows of a head are taken in groups that fill the 16 columns of a tile.  A workgroup has a group and every S-th window of 512 keys
+// The rows of a head are taken in groups that fill the 16 columns of a tile.  A workgroup has a group and every S-th window of 256 keys
 // of its head: it marks what each row keeps there (a bit per key and row), lists the keys that some row keeps, and folds each of them
 // once for all rows, the scores of rows that do not keep it hidden.  So a key that several rows keep is read once, not once per row;
 // what bounds it is the 256 bytes of a key and its value over the union of the rows' sets.  The rows' own user keys follow in the same
@@ -15,9 +15,10 @@ namespace sq {
 
 namespace {
 
-constexpr int WINDOW = 512;                  // keys of a window: 8 words of 64 bits
-constexpr int BATCH = 8;                     // windows whose bits are held at a time
-constexpr int BATCH_WORDS = BATCH * WINDOW / 64;
+constexpr int WINDOW = Q8_WINDOW;            // keys of a window, in words of 64 bits
+constexpr int WINDOW_WORDS = WINDOW / 64;
+constexpr int BATCH_WORDS = 64;              // words that are held at a time
+constexpr int BATCH = BATCH_WORDS / WINDOW_WORDS;
 
 }  // namespace
 
@@ -37,13 +38,13 @@ __global__ __launch_bounds__(256, 2) void decode_q8_shared_kernel(DecodeQ8Args a
     const int wave = uniform(threadIdx.x >> 6);
     if (threadIdx.x < QT) s_none[threadIdx.x] = 0;
     // units (head, group of rows, s of S), consecutive ones on the same XCD
-    const int S = 1 << a.s_log, units = (a.H * a.groups) << a.s_log, per_xcd = (units + 7) / 8;
+    const int S = a.parts, units = a.H * a.groups * S, per_xcd = (units + 7) / 8;
     const int unit = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per_xcd || unit >= units) return;
-    const int s = unit & (S - 1), hg = unit >> a.s_log, h = hg / a.groups, grp = hg - h * a.groups;
+    const int hg = unit / S, s = unit - hg * S, h = hg / a.groups, grp = hg - h * a.groups;
     const int in_head = a.B * a.per, first_row = h * in_head + grp * a.rows_per_group;
     const int nj = min(a.rows_per_group, in_head - grp * a.rows_per_group), columns = nj * a.g;
-    const int windows = (a.L + WINDOW - 1) / WINDOW, mine = (windows - s + S - 1) >> a.s_log, batches = a.ranges ? (mine + BATCH - 1) / BATCH : 0;
+    const int windows = (a.L + WINDOW - 1) / WINDOW, mine = (windows - s + S - 1) / S, batches = a.ranges ? (mine + BATCH - 1) / BATCH : 0;
     const global<uint8_t> Kf = uniform(a.K8 + (size_t)h * a.L * D), Vf = uniform(a.V8 + (size_t)h * a.L * D);
 
     // only < 0: all rows; otherwise that row alone, after a NaN
@@ -95,12 +96,11 @@ __global__ __launch_bounds__(256, 2) void decode_q8_shared_kernel(DecodeQ8Args a
                             if (i0 + 64 * k + lane >= nr) continue;
                             const int x = min(max(e[k].x, -MAX_L), MAX_L), y = min(max(e[k].y, 0), a.L);
                             const int lo = min(max(x, 0), a.L), hi = min(max(x + y, lo), a.L);
-                            int win = lo / WINDOW;
-                            win += (s - win) & (S - 1);     // this workgroup's first window that the range can touch
-                            for (; win * WINDOW < hi; win += S) {
-                                const int at = ((win - s) >> a.s_log) - batch * BATCH;
-                                if (at < 0) continue;
-                                if (at >= BATCH) break;
+                            // this workgroup's windows that the range touches, from the batch's first on
+                            int at = max((lo / WINDOW - s + S - 1) / S, batch * BATCH);
+                            int win = at * S + s;
+                            at -= batch * BATCH;
+                            for (; win * WINDOW < hi && at < BATCH; win += S, ++at) {
                                 const int from = max(lo - win * WINDOW, 0), to = min(hi - win * WINDOW, WINDOW);
                                 uint32_t *row = &s_bits[j][at * (WINDOW / 32)];
                                 for (int b = from >> 5; b <= (to - 1) >> 5 && from < to; ++b)
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(256, 2) void decode_q8_shared_kernel(DecodeQ8Args a
                 }
                 __syncthreads();
             } else {
-                tiles = 2 * max(0, (chunks - my_chunk + 4 * S - 1) >> (a.s_log + 2));
+                tiles = my_chunk < chunks ? 2 * ((chunks - my_chunk + 4 * S - 1) / (4 * S)) : 0;
             }
             // Word w of the batch: 64 consecutive keys; the union of its rows' bits, the same in every lane.  A wave has words wave, wave + 4, ..
             auto word_of = [&](int i, uint32_t &lo, uint32_t &hi) {   // this lane's row's bits of the wave's i-th word
@@ -177,8 +177,8 @@ __global__ __launch_bounds__(256, 2) void decode_q8_shared_kernel(DecodeQ8Args a
                         }
                         if (m != 0u) {
                             const int to = have + __popcll(some & ((1ull << lane) - 1ull));
-                            const int win = ((batch * BATCH + (at_word >> 3)) << a.s_log) + s;
-                            s_key[wave][to] = win * WINDOW + (at_word & 7) * 64 + lane;
+                            const int win = (batch * BATCH + at_word / WINDOW_WORDS) * S + s;
+                            s_key[wave][to] = win * WINDOW + at_word % WINDOW_WORDS * 64 + lane;
                             s_key_rows[wave][to] = (unsigned short)m;
                         }
                         have = uniform(have + __popcll(some));
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(256, 2) void decode_q8_shared_kernel(DecodeQ8Args a
 
 void launch_decode_q8_shared(const DecodeQ8Args &a, bool wide, hipEvent_t ev0, hipEvent_t ev1, hipStream_t s)
 {
-    const int grid = (((a.H * a.groups) << a.s_log) + 7) / 8 * 8;
+    const int grid = (a.H * a.groups * a.parts + 7) / 8 * 8;
     auto *kernel = wide ? decode_q8_shared_kernel<true> : decode_q8_shared_kernel<false>;
     if (ev0) hipExtLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, ev0, ev1, 0, a);
     else hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, a);

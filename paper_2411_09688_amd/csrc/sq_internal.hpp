@@ -398,7 +398,7 @@ struct DecodeQ8Args {
     int p_log, n_pages, max_pages; // tokens per page: 2^p_log
     float scale;                   // sm_scale * log2(e)
     int splits;                    // (the launcher's) workgroups of each row, or 0: shares of all rows' tiles
-    int groups, rows_per_group, s_log;   // (the launcher's) groups of rows of a head that share its keys, 0: none; 2^s_log workgroups each
+    int groups, rows_per_group, parts;   // (the launcher's) groups of rows of a head that share its keys, 0: none; workgroups of each
 };
 // Rows of a head that are taken together: from 8 on, in groups that fill 16 columns, and only where the rows have this many keys to
 // select from between them.  Below it what several rows keep comes from the caches again, and marking the union costs more than that.
@@ -413,8 +413,9 @@ struct DecodeQ8Args {
 //   40               x  8       x  32768 ( 10 M)       28.0 / 33.4   53.7 / 44.3    117 / 48.6
 //   16               x  8       x 131072 ( 17 M)       30.8 / 40.7   83.2 / 66.4    224 / 84.0
 constexpr long long Q8_SHARED_MIN_KEYS = 2 << 20;
+constexpr int Q8_SHARED_GRID = 512, Q8_WINDOW = 256;
 struct Q8Groups {
-    int groups, rows, s_log;
+    int groups, rows, parts;
 };
 inline Q8Groups q8_groups(int B, int H, int per, int g, int L)
 {
@@ -422,9 +423,8 @@ inline Q8Groups q8_groups(int B, int H, int per, int g, int L)
     const long long in_head = (long long)B * per;
     if (in_head < 8 || rows < 8 || in_head * H * L < Q8_SHARED_MIN_KEYS) return Q8Groups{0, 0, 0};
     const long long groups = (in_head + rows - 1) / rows;
-    int s_log = 0;
-    while (s_log < 9 && (groups * H << (s_log + 1)) <= Q8_GRID && (512 << (s_log + 1)) <= L + 511) ++s_log;
-    return Q8Groups{(int)groups, rows, s_log};
+    const long long parts = Q8_SHARED_GRID / (groups * H), windows = (L + Q8_WINDOW - 1) / Q8_WINDOW;
+    return Q8Groups{(int)groups, rows, (int)(parts < 1 ? 1 : parts > windows ? windows : parts)};
 }
 void launch_decode_q8_shared(const DecodeQ8Args &a, bool wide, hipEvent_t ev0, hipEvent_t ev1, hipStream_t s);
 hipError_t launch_decode_q8(const DecodeQ8Args &a, hipStream_t s);

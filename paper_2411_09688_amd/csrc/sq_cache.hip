@@ -89,9 +89,9 @@ __device__ __forceinline__ bool find_piece(const AppendArgs &a, int unit, Piece 
     return true;
 }
 
-// fp32 arithmetic of a key is off by at most this much, 16 roundings, of |a| + |b| of its pair (a, b) before the rotation: a sum of 128
-// squares (13 additions in a row, of which the root halves the error), the reciprocal root (a last place: two roundings), two products,
-// and three roundings of the rotation make 14.
+// fp32 arithmetic of a key is off by at most this much, 16 roundings, of (|a| + |b|) max(|c|, |s|) of its pair (a, b), turned by (c, s)
+// of any size: a sum of 128 squares (13 additions in a row, of which the root halves the error), the reciprocal root (a last place: two
+// roundings), two products, and three roundings of the rotation make 14.
 constexpr float KEY_ERROR = 1.0f / (1 << 20);
 
 // A key's values in double precision, one pair after the other so that it takes few registers.
@@ -218,8 +218,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryA
     float amax = page_max(most);                            // (behind its barrier every thread has read the scale)
     uint32_t again = 0;                                     // tokens to be taken again in double precision, a bit each
     const auto exponent = [](float v) { return scale_exponent(__builtin_bit_cast(uint32_t, v)); };
-    // An infinity sets no scale; and where the largest value lies within its error of one's limit, it is taken exactly (|a| + |b| of its
-    // pair is at most twice the value).
+    // An infinity sets no scale; and where the largest value lies within its error of one's limit, it is taken exactly ((c, s) is
+    // a rotation times a length, so (|a| + |b|) max(|c|, |s|) is at most twice the larger value of the turned pair).
     const bool near = !value && inexact && exponent(amax * (1.0f - 4 * KEY_ERROR)) != exponent(amax * (1.0f + 4 * KEY_ERROR));
     if (near || amax > 3.4e38f) {
         if (near) again = (1u << T) - 1;

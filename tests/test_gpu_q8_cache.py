@@ -127,6 +127,20 @@ def test_a_prompt_at_once_is_the_same_as_in_parts_where_the_scale_stays():
     assert np.array_equal(a.d[1].view(torch.uint8).cpu().numpy(), b.d[1].view(torch.uint8).cpu().numpy())
 
 
+@pytest.mark.parametrize("m", [64.0, 1.375, 2.0 ** -6])
+def test_cosines_and_sines_of_any_size(m):
+    """A table may be scaled (a softmax temperature put into it): the codes are those of exact arithmetic all the same."""
+    rng = np.random.default_rng(7)
+    H, T = 4, 4096
+    pool = Pool(rng, 1, H, 64, T // 64)
+    lay = layer(rng, True, 128, False, 16)
+    scaled = (lay[1] * np.float32(m)).astype(np.float32)
+    lay = (lay[0], scaled, False, sq.make_rotary(cu(scaled), False, *(cu(x) for x in lay[0]), eps=EPS))
+    k, v = (cu(rng.standard_normal((T, H, 128)).astype(np.float16)) for _ in range(2))
+    step(pool, lay, None, k, v, (np.arange(T) % 16).astype(np.int32), [0], [T], 1, True)
+    pool.check()
+
+
 def test_bad_pages_and_full_sequences_drop_tokens():
     rng = np.random.default_rng(3)
     H, P = 2, 16

@@ -527,8 +527,8 @@ int sq_calibrate_threshold(const sq_shape_t *shape, const float *logits, const f
  *   rotation:             pair (i, i + rot_dim/2) of the first rot_dim dimensions, or (2i, 2i + 1) if interleaved != 0:
  *                         (a, b) <- (a c - b s, b c + a s),  (c, s) = cos_sin[position][i]
  * Dimensions from rot_dim on are only normed.  rot_dim: a multiple of 8 in [0, d]; 0: no rotation (cos_sin not read).  A
- * position outside [0, n_positions) is read as the nearest one inside.  eps must be finite and not
- * negative; cosines and sines may be of any size (a scaled table).
+ * position outside [0, n_positions) is read as the nearest one inside.  eps must be finite, not
+ * negative and not subnormal; cosines and sines may be of any size (a scaled table).
  */
 typedef struct sq_rotary_t {
     int32_t rot_dim, interleaved, n_positions;

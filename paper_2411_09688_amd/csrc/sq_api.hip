@@ -1673,7 +1673,9 @@ int check_rotary(const char *fn, const sq_rotary_t *rot, const int32_t *position
     if (!rot) return fail(SQ_ERR_INVALID_ARG, "%s: rot is NULL", fn);
     if (rot->rot_dim < 0 || rot->rot_dim > sq::D || rot->rot_dim % 8)
         return fail(SQ_ERR_INVALID_ARG, "%s: rot_dim = %d must be a multiple of 8 in [0, %d]", fn, rot->rot_dim, sq::D);
-    if (!(rot->eps >= 0.0f) || rot->eps > 3.4e38f) return fail(SQ_ERR_INVALID_ARG, "%s: eps must be finite and not negative", fn);
+    // (the root of a subnormal number is not taken)
+    if (!(rot->eps >= 0.0f) || rot->eps > 3.4e38f || (rot->eps > 0.0f && rot->eps < 1.1754944e-38f))
+        return fail(SQ_ERR_INVALID_ARG, "%s: eps must be finite, not negative and not subnormal", fn);
     if (rot->rot_dim > 0) {
         if (rot->n_positions <= 0) return fail(SQ_ERR_INVALID_ARG, "%s: n_positions = %d must be positive", fn, rot->n_positions);
         if (!rot->cos_sin || !aligned16(rot->cos_sin)) return fail(SQ_ERR_INVALID_ARG, "%s: cos_sin is NULL or not 16-byte aligned", fn);

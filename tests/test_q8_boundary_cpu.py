@@ -51,6 +51,7 @@ def test_norm_rotate_refuses(sq):
     refused(sq, call(rot=rotary(sq, eps=-1.0)), INV, b"eps")
     refused(sq, call(rot=rotary(sq, eps=float("nan"))), INV, b"eps")
     refused(sq, call(rot=rotary(sq, eps=float("inf"))), INV, b"eps")
+    refused(sq, call(rot=rotary(sq, eps=1e-39)), INV, b"eps")
     refused(sq, call(rot=rotary(sq, n_positions=0)), INV, b"n_positions")
     refused(sq, call(rot=rotary(sq, cos_sin=None)), INV, b"cos_sin")
     refused(sq, call(rot=rotary(sq, q_weight=at(20, 8))), INV, b"weight")

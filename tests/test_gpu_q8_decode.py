@@ -271,3 +271,56 @@ def test_two_graphs_share_a_workspace_and_a_side_stream():
         torch.cuda.synchronize()
         assert torch.equal(p.out, want)
         o.check()
+
+
+def test_a_group_of_rows_with_input_outside_the_contract():
+    """Rows whose ranges lie outside the context, overlap or are too many; the group's other rows are as they would be."""
+    p = Problem(16, 16, 1, 1, 140001, 900, 0.01, [70] * 16, 16, False)
+    p.ranges[1, :3] = ((-5, 40), (140000, 50), (2 ** 31 - 1, 2 ** 31 - 1))
+    p.ranges[2, :2] = ((-2 ** 31, 2 ** 31 - 1), (100, -3))
+    p.ranges[3, :4] = ((7, 100), (50, 100), (7, 100), (0, 1))
+    p.n_ranges[4], p.n_ranges[5] = 10 ** 9, -4
+    p.n_keys[6], p.n_keys[7] = -1, 10 ** 9
+    p.table[8, 1] = -1
+    args = p.upload()
+    p.lengths[9] = 80                                           # (all of the pages there are, for the reference)
+    args[11][9] = 10 ** 9
+    for c in args[10].tensors[:2]:                              # (behind the last token: what a reused page holds)
+        c.view(torch.uint8)[(c.view(torch.uint8) & 0x7f) == 0x7f] = 0x11
+    for i in range(2):
+        p.cache[i][(p.cache[i] & 0x7f) == 0x7f] = 0x11
+    sq.sq_sparse_attn_decode_q8(*args, p.out, p.lse, p.ws)
+    torch.cuda.synchronize()
+    p.check(rows=[0] + list(range(8, 16)))
+    assert torch.isfinite(p.out).all() and torch.isfinite(p.lse).all()
+
+
+def test_two_calls_at_once_and_a_captured_group():
+    """A group of rows captured and replayed for rows that change, while another call runs on a stream and workspace of its own."""
+    p = Problem(17, 16, 1, 1, 140001, 900, 0.01, [20, 0, 65, 300] * 4, 16, False)
+    args = p.upload()
+    o = Problem(18, 1, 3, 2, 9000, 300, 0.5, [64], 64, False)
+    oargs = o.upload()
+    sq.sq_sparse_attn_decode_q8(*args, p.out, p.lse, p.ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sq.sq_sparse_attn_decode_q8(*args, p.out, p.lse, p.ws)
+    side = torch.cuda.Stream()
+    lengths = p.lengths.copy()
+    for i in range(4):
+        p.lengths = (lengths * (i + 1) // 4).astype(np.int32)
+        p.n_ranges[i], p.n_keys[i] = 0, 0
+        for t, x in ((args[11], p.lengths), (args[8], p.n_ranges), (args[9], p.n_keys)):
+            t.copy_(cu(x).view(t.shape))
+        p.out.fill_(9.0), o.out.fill_(9.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        sq.sq_sparse_attn_decode_q8(*oargs, o.out, o.lse, o.ws, stream=side)
+        torch.cuda.synchronize()
+        p.check(rows=[i, 5, 11, 15])
+        o.check()
+        again = p.out.clone()
+        sq.sq_sparse_attn_decode_q8(*args, p.out, p.lse, p.ws)
+        torch.cuda.synchronize()
+        assert torch.equal(p.out, again)

@@ -89,10 +89,11 @@ __device__ __forceinline__ bool find_piece(const AppendArgs &a, int unit, Piece 
     return true;
 }
 
-// fp32 arithmetic of a key is off by at most this much, 16 roundings, of (|a| + |b|) max(|c|, |s|) of its pair (a, b), turned by (c, s)
-// of any size: a sum of 128 squares (13 additions in a row, of which the root halves the error), the reciprocal root (a last place: two
-// roundings), two products, and three roundings of the rotation make 14.
-constexpr float KEY_ERROR = 1.0f / (1 << 20);
+// fp32 arithmetic of a key is off by at most 14 roundings of (|a| + |b|) max(|c|, |s|) of its pair (a, b), turned by (c, s) of any size: a
+// sum of 128 squares (13 additions in a row, of which the root halves the error), the reciprocal root (a last place: two roundings), two
+// products, and three roundings of the rotation.  (c, s) is a rotation times a length, so that is at most sqrt(2) times the length of the
+// turned pair (u, v), and that at most |u| + |v|: 20 roundings of |u| + |v|, and as |u| + |v| is off as well, 24.
+constexpr float KEY_ERROR = 1.5f / (1 << 20);
 
 // A key's values in double precision, one pair after the other so that it takes few registers.
 template <bool ADJACENT>
@@ -161,7 +162,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryA
         return (value ? a.v + (size_t)token * a.v_stride : a.k + (size_t)token * a.k_stride) + (size_t)h * D;
     };
     auto position_of = [&](int token) { return ra.rot_dim ? a.positions[token] : 0; };
-    float x[T][8], off[T][4];                               // values, and how far those of a pair may be off
+    float x[T][8];
     h4 wa = {}, wb = {};
     {
         h4 lo[T], hi[T];
@@ -183,7 +184,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryA
         if (page < 0 || page >= a.n_pages) return;
 #pragma unroll
         for (int i = 0; i < T; ++i) {
-            if (!value) norm_rotate<ADJACENT, PARTIAL, true>(x[i], lo[i], hi[i], wa, wb, norm, ra.eps, cs[i], lp.turns, off[i]);
+            if (!value) norm_rotate<ADJACENT, PARTIAL>(x[i], lo[i], hi[i], wa, wb, norm, ra.eps, cs[i], lp.turns);
             else
 #pragma unroll
                 for (int c = 0; c < 8; ++c) x[i][c] = (float)(c < 4 ? lo[i][c & 3] : hi[i][c & 3]);
@@ -218,9 +219,9 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryA
     float amax = page_max(most);                            // (behind its barrier every thread has read the scale)
     uint32_t again = 0;                                     // tokens to be taken again in double precision, a bit each
     const auto exponent = [](float v) { return scale_exponent(__builtin_bit_cast(uint32_t, v)); };
-    // An infinity sets no scale; and where the largest value lies within its error of one's limit, it is taken exactly ((c, s) is
-    // a rotation times a length, so (|a| + |b|) max(|c|, |s|) is at most twice the larger value of the turned pair).
-    const bool near = !value && inexact && exponent(amax * (1.0f - 4 * KEY_ERROR)) != exponent(amax * (1.0f + 4 * KEY_ERROR));
+    // An infinity sets no scale; and where the largest value lies within its error of one's limit, it is taken exactly (|u| + |v|
+    // is at most twice the larger).
+    const bool near = !value && inexact && exponent(amax * (1.0f - 2 * KEY_ERROR)) != exponent(amax * (1.0f + 2 * KEY_ERROR));
     if (near || amax > 3.4e38f) {
         if (near) again = (1u << T) - 1;
         most = 0.0f;
@@ -264,7 +265,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryA
             float less[8], more[8];
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
-                const float v = x[i][c] * inv, d = off[i][ADJACENT ? c >> 1 : c & 3] * (KEY_ERROR * inv);
+                const float v = x[i][c] * inv;              // (an infinity or NaN is its pair's, if it was turned, and of no other value)
+                const float d = (fabsf(x[i][c]) + fabsf(lp.turns ? x[i][ADJACENT ? c ^ 1 : c ^ 4] : x[i][c])) * (KEY_ERROR * inv);
                 less[c] = v - d;
                 more[c] = v + d;
             }

@@ -52,10 +52,9 @@ __device__ __forceinline__ void load_turn(float (&cs)[8], const RotaryArgs &ra, 
                    : ((ra).rot_dim < D ? call(false, true) : call(false, false)))
 
 // The lane's dimensions x, y (pieces a, b) normed and rotated, fp32 arithmetic; wa, wb: the weight's, same places; turns: this lane
-// rotates.  pair (if PAIRS): (|a| + |b|) max(|c|, |s|) of each pair (a, b) before it is turned: what its products come to at most.
-template <bool ADJACENT, bool PARTIAL, bool PAIRS>
-__device__ __forceinline__ void norm_rotate(float (&e)[8], h4 x, h4 y, h4 wa, h4 wb, bool norm, float eps, const float (&cs)[8], bool turns,
-                                            float (&pair)[4])
+// rotates.
+template <bool ADJACENT, bool PARTIAL>
+__device__ __forceinline__ void norm_rotate(float (&e)[8], h4 x, h4 y, h4 wa, h4 wb, bool norm, float eps, const float (&cs)[8], bool turns)
 {
     if (norm) {
         float ss = 0;
@@ -79,7 +78,6 @@ __device__ __forceinline__ void norm_rotate(float (&e)[8], h4 x, h4 y, h4 wa, h4
     }
     auto turn = [&](int ia, int ib, int i) {
         const float a = e[ia], b = e[ib], c = cs[2 * i], s = cs[2 * i + 1];
-        if (PAIRS) pair[i] = (fabsf(a) + fabsf(b)) * fmaxf(fabsf(c), fabsf(s));
         const float u = __builtin_fmaf(a, c, -(b * s)), v = __builtin_fmaf(b, c, a * s);
         e[ia] = PARTIAL && !turns ? a : u;
         e[ib] = PARTIAL && !turns ? b : v;
@@ -115,13 +113,13 @@ __device__ __forceinline__ void turn_rows(const TurnRows &t, const RotaryArgs &r
         if (i < t.n) {
             if (t.kind[i] != 2) {
                 const _Float16 *weight = ra.weight[t.kind[i]];
-                float e[8], pair[4];
+                float e[8];
                 h4 wa = {}, wb = {};
                 if (weight) {
                     wa = *reinterpret_cast<const h4 *>(weight + lp.a);
                     wb = *reinterpret_cast<const h4 *>(weight + lp.b);
                 }
-                norm_rotate<ADJACENT, PARTIAL, false>(e, x[i], y[i], wa, wb, weight != nullptr, ra.eps, cs, lp.turns, pair);
+                norm_rotate<ADJACENT, PARTIAL>(e, x[i], y[i], wa, wb, weight != nullptr, ra.eps, cs, lp.turns);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     x[i][c] = (_Float16)e[c];

@@ -170,6 +170,17 @@ def test_infinities_and_nan_become_nan_codes_and_set_no_scale():
     pool.check()
 
 
+@pytest.mark.parametrize("norm,rot,adjacent", [(True, 0, False), (False, 64, False), (True, 64, True), (True, 96, False), (False, 128, True)])
+def test_infinities_and_nan_of_keys_stay_with_what_is_computed_from_them(norm, rot, adjacent):
+    rng = np.random.default_rng(8)
+    pool = Pool(rng, 1, 2, 16, 2)
+    x = rng.standard_normal((2, 30, 2, 128)).astype(np.float16)
+    x[0, 1, 0, 3], x[0, 2, 0, 127], x[0, 9, 1, 100], x[0, 20, 0, 70], x[0, 29, 1, 0] = np.inf, np.nan, -np.inf, np.inf, np.nan
+    lay = layer(rng, norm, rot, adjacent, 64)
+    step(pool, lay, None, cu(x[0]), cu(x[1]), np.arange(30, dtype=np.int32), [0], [30], 1, True)
+    pool.check()
+
+
 def test_on_another_stream_and_captured():
     rng = np.random.default_rng(6)
     B, H, P = 3, 2, 16

@@ -6,8 +6,13 @@
 // A key's code is decided at a border between two values that lie 1/8 apart, and with the f16 row, the f32 table and the f16 weight
 // given exactly, 53 bits decide it as exact arithmetic does but once in some 10^14 values, where 24 bits would differ once in a
 // million.  So the arithmetic is fp32 with a bound on its error: where the value less the bound and the value and the bound have
-// the same code, that is the code; the others, one wave in a hundred, are taken again in double precision.  (In double precision
-// throughout, the keys and values of 16384 tokens of 8 heads took 77 us, of which the memory needs 20.)
+// the same code, that is the code; the others, of one wave in twenty, are taken again in double precision.
+//
+// 16384 tokens of 13 prompts, 32 query and 8 K/V heads (372 MB): 88 us, 4.2 TB/s.  The queries alone take 55, at what the memory
+// gives; keys and values alone 44, of which the memory needs 20: their reads follow one another (the sequence's length, the page and
+// the position, the row of the table), five waves a SIMD hide that in part (four: 100 us in all; six, with registers in memory: 117).
+// In double precision throughout keys and values took 77.  One token of a sequence: 3.7 us on the GPU, one of 64 sequences 4.8, a chain
+// of the same reads; the call itself takes the calling thread 7.
 #include "sq_head_row.hpp"
 #include "sq_internal.hpp"
 
@@ -126,8 +131,8 @@ __device__ __forceinline__ void exact_key(float (&x)[8], h4 lo, h4 hi, h4 wa, h4
 
 // Tokens g, g + 16, .. of a page by 16 lanes each: T of them a thread.  Workgroups of the heads of one page, keys and values, follow one
 // another: together they read the page's tokens of the projection row by row.
-template <int T, bool ADJACENT, bool PARTIAL>
-__global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryArgs ra)
+template <int T, bool ADJACENT, bool PARTIAL, bool STREAM>
+__global__ __launch_bounds__(256, 5) void cache_append_kernel(AppendArgs a, RotaryArgs ra)
 {
     const int tid = threadIdx.x, j = tid & 15, g = tid >> 4, wide = blockDim.x >> 4, waves = blockDim.x >> 6;
     __shared__ float s_max[4];
@@ -145,7 +150,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, RotaryA
             rows.src[i] = a.q + (size_t)token * a.q_stride + (size_t)h * D;
             rows.dst[i] = a.q_out + ((size_t)token * a.Hq + h) * D;
         }
-        turn_rows<ADJACENT, PARTIAL>(rows, ra, ra.rot_dim ? a.positions[token] : 0, j);
+        turn_rows<ADJACENT, PARTIAL, STREAM>(rows, ra, ra.rot_dim ? a.positions[token] : 0, j);
         return;
     }
     const int hv = blockIdx.x % (2 * a.H), unit = blockIdx.x / (2 * a.H);
@@ -309,10 +314,14 @@ hipError_t launch_cache_append(AppendArgs a, const RotaryArgs &ra, hipStream_t s
     const long long q = a.q ? ((long long)a.n_tokens * 16 + threads - 1) / threads * ((a.Hq + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE) : 0;
     if (kv + q > 0x7fffffffll) return hipErrorInvalidConfiguration;
     a.kv_blocks = (int)kv;
-#define SQ_APPEND_1(A, P) cache_append_kernel<1, A, P>
-#define SQ_APPEND_2(A, P) cache_append_kernel<2, A, P>
-#define SQ_APPEND_4(A, P) cache_append_kernel<4, A, P>
-    auto *kernel = most > 32 ? SQ_FOR_ROTARY(ra, SQ_APPEND_4) : most > 16 ? SQ_FOR_ROTARY(ra, SQ_APPEND_2) : SQ_FOR_ROTARY(ra, SQ_APPEND_1);
+#define SQ_APPEND_1(A, P) cache_append_kernel<1, A, P, false>
+#define SQ_APPEND_2(A, P) cache_append_kernel<2, A, P, false>
+#define SQ_APPEND_4(A, P) cache_append_kernel<4, A, P, false>
+#define SQ_APPEND_STREAM(A, P) cache_append_kernel<4, A, P, true>
+    // (only the queries pass the caches, 94 -> 88 us for 16384 tokens of 32 + 8 heads; keys and values as well: 90.  Where no sequence
+    // brings many tokens, the rows of a call are few)
+    const bool stream = a.q && streams((size_t)a.n_tokens * ((size_t)a.Hq * 4 + (size_t)a.H * 6) * D);
+    auto *kernel = most > 32 ? (stream ? SQ_FOR_ROTARY(ra, SQ_APPEND_STREAM) : SQ_FOR_ROTARY(ra, SQ_APPEND_4)) : most > 16 ? SQ_FOR_ROTARY(ra, SQ_APPEND_2) : SQ_FOR_ROTARY(ra, SQ_APPEND_1);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(kv + q)), dim3(threads), 0, s, a, ra);
     return hipGetLastError();
 }

@@ -16,6 +16,19 @@ typedef float f2v __attribute__((ext_vector_type(2)));
 typedef uint32_t u2v __attribute__((ext_vector_type(2)));
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 
+// What a kernel reads or writes once.  STREAM: past the caches, where the call's data would not stay in them.
+template <bool STREAM, typename T>
+__device__ __forceinline__ T load_once(const T *p)
+{
+    return STREAM ? __builtin_nontemporal_load(p) : *p;
+}
+template <bool STREAM, typename T>
+__device__ __forceinline__ void store_once(T *p, T v)
+{
+    if (STREAM) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+
 // The least e with amax <= 448 * 2^e; amax: bits of a float that is finite and not negative.  448 = 1.75 * 2^8, so e is the
 // value's own exponent less 8, and one more where its mantissa is over 1.75: 0x1fffff carries exactly then.
 __device__ __forceinline__ int scale_exponent(uint32_t amax)

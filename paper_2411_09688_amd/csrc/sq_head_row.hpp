@@ -95,7 +95,7 @@ struct TurnRows {
     int kind[ROWS_AT_ONCE];
     int n;
 };
-template <bool ADJACENT, bool PARTIAL>
+template <bool ADJACENT, bool PARTIAL, bool STREAM>
 __device__ __forceinline__ void turn_rows(const TurnRows &t, const RotaryArgs &ra, int position, int j)
 {
     const LanePieces lp = lane_pieces<ADJACENT, PARTIAL>(j, ra.rot_dim);
@@ -103,8 +103,8 @@ __device__ __forceinline__ void turn_rows(const TurnRows &t, const RotaryArgs &r
 #pragma unroll
     for (int i = 0; i < ROWS_AT_ONCE; ++i)
         if (i < t.n) {
-            x[i] = *reinterpret_cast<const h4 *>(t.src[i] + lp.a);
-            y[i] = *reinterpret_cast<const h4 *>(t.src[i] + lp.b);
+            x[i] = load_once<STREAM>(reinterpret_cast<const h4 *>(t.src[i] + lp.a));
+            y[i] = load_once<STREAM>(reinterpret_cast<const h4 *>(t.src[i] + lp.b));
         }
     float cs[8];
     load_turn(cs, ra, position, j, lp.turns && t.kind[0] != 2);   // (values come last)
@@ -126,8 +126,8 @@ __device__ __forceinline__ void turn_rows(const TurnRows &t, const RotaryArgs &r
                     y[i][c] = (_Float16)e[c + 4];
                 }
             }
-            *reinterpret_cast<h4 *>(t.dst[i] + lp.a) = x[i];
-            *reinterpret_cast<h4 *>(t.dst[i] + lp.b) = y[i];
+            store_once<STREAM>(reinterpret_cast<h4 *>(t.dst[i] + lp.a), x[i]);
+            store_once<STREAM>(reinterpret_cast<h4 *>(t.dst[i] + lp.b), y[i]);
         }
 }
 

@@ -9,7 +9,7 @@ namespace sq {
 
 // A workgroup takes 16 consecutive tokens, 16 lanes each, and four heads: a head's rows of consecutive tokens lie side by side in the
 // output.
-template <bool ADJACENT, bool PARTIAL>
+template <bool ADJACENT, bool PARTIAL, bool STREAM>
 __global__ __launch_bounds__(256) void head_rows_kernel(HeadRows hr, RotaryArgs ra, int tokens)
 {
     const int heads = hr.n[0] + hr.n[1] + hr.n[2], quads = (heads + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE;
@@ -28,15 +28,17 @@ __global__ __launch_bounds__(256) void head_rows_kernel(HeadRows hr, RotaryArgs 
         rows.src[i] = hr.src[part] + token * hr.stride[part] + (size_t)h * D;
         rows.dst[i] = hr.dst[part] + (((size_t)b * hr.n[part] + h) * hr.Lq + t) * D;
     }
-    turn_rows<ADJACENT, PARTIAL>(rows, ra, ra.rot_dim ? hr.positions[token] : 0, j);
+    turn_rows<ADJACENT, PARTIAL, STREAM>(rows, ra, ra.rot_dim ? hr.positions[token] : 0, j);
 }
 
 hipError_t launch_head_rows(const HeadRows &hr, const RotaryArgs &ra, int tokens, hipStream_t s)
 {
     const int heads = hr.n[0] + hr.n[1] + hr.n[2];
     const dim3 grid((unsigned)((long long)((tokens + 15) / 16) * ((heads + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE)));
-#define SQ_HEAD_ROWS(A, P) head_rows_kernel<A, P>
-    hipLaunchKernelGGL(SQ_FOR_ROTARY(ra, SQ_HEAD_ROWS), grid, dim3(256), 0, s, hr, ra, tokens);
+#define SQ_HEAD_ROWS(A, P) head_rows_kernel<A, P, false>
+#define SQ_HEAD_ROWS_STREAM(A, P) head_rows_kernel<A, P, true>
+    auto *kernel = streams((size_t)tokens * heads * D * 4) ? SQ_FOR_ROTARY(ra, SQ_HEAD_ROWS_STREAM) : SQ_FOR_ROTARY(ra, SQ_HEAD_ROWS);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, hr, ra, tokens);
     return hipGetLastError();
 }
 

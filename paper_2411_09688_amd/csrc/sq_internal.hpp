@@ -349,6 +349,12 @@ hipError_t launch_decode_attn_index(const void *q, const void *Kf, const void *V
 
 // Keys and values in 8 bits (sq_head_rows.hip, sq_quantize.hip, sq_cache.hip, sq_decode_q8.hip).
 struct RotaryArgs;
+// What a call of these reads and writes once passes the caches if it is more than the last of them holds: 256 MB.  us per call with the
+// caches / past them, a call on what the call before it used, and on what four calls before it did:
+//   norm and rotation:  101 MB 17.7 / 20.5, 23.1 / 21.1;  201 MB 33.6 / 38.3, 40.3 / 37.8;  403 MB 75.7 / 69.0;  1611 MB 297 / 275
+//   quantizing:         101 MB 19.9 / 20.0, 24.7 / 20.5;  202 MB 35.5 / 36.5, 43.4 / 37.7;  405 MB 78.4 / 68.2;   810 MB 148 / 130
+constexpr size_t CACHED_BYTES = 256u << 20;
+inline bool streams(size_t bytes) { return bytes > CACHED_BYTES; }
 struct HeadRows {                  // queries, keys, values; n: heads (0: not given)
     const _Float16 *src[3];
     _Float16 *dst[3];

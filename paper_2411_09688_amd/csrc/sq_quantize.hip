@@ -7,6 +7,7 @@
 
 namespace sq {
 
+template <bool STREAM>
 __global__ __launch_bounds__(256) void kv_quantize_kernel(QuantizeArgs a)
 {
     const int tid = threadIdx.x, j = tid & 15, g = tid >> 4;
@@ -25,7 +26,7 @@ __global__ __launch_bounds__(256) void kv_quantize_kernel(QuantizeArgs a)
         const int r = i * 16 + g;
         int src = first + min(r, n - 1);
         if (perm) src = min(max(perm[src], 0), a.L - 1);
-        const h8 v = *reinterpret_cast<const h8 *>(X + (size_t)src * D + 8 * j);
+        const h8 v = load_once<STREAM>(reinterpret_cast<const h8 *>(X + (size_t)src * D + 8 * j));
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             x[i][e] = (float)v[e];
@@ -42,14 +43,15 @@ __global__ __launch_bounds__(256) void kv_quantize_kernel(QuantizeArgs a)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = i * 16 + g;
-        if (r < n) *reinterpret_cast<u2v *>(codes + (size_t)(first + r) * D + 8 * j) = e4m3_encode8(x[i], inv);
+        if (r < n) store_once<STREAM>(reinterpret_cast<u2v *>(codes + (size_t)(first + r) * D + 8 * j), e4m3_encode8(x[i], inv));
     }
     if (tid == 0) a.scale[which][bh * a.blocks + blk] = exp2_int(e);
 }
 
 hipError_t launch_kv_quantize(const QuantizeArgs &a, int heads, hipStream_t s)
 {
-    hipLaunchKernelGGL(kv_quantize_kernel, dim3((unsigned)((size_t)a.blocks * heads * a.tensors)), dim3(256), 0, s, a);
+    auto *kernel = streams((size_t)a.L * heads * a.tensors * D * 3) ? kv_quantize_kernel<true> : kv_quantize_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((size_t)a.blocks * heads * a.tensors)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 

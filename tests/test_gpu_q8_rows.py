@@ -144,3 +144,44 @@ def test_every_finite_half_is_rounded_to_the_nearest_code():
     sq.sq_kv_quantize(sq.make_shape(1, 1, L, 1, 1, 0, 1.0), cu(X), None, None, K8, None, ks, None)
     c, s = ref.quantize(X, None)
     assert np.array_equal(ks.cpu().numpy(), s) and np.array_equal(K8.view(torch.uint8).cpu().numpy(), c)
+
+
+def test_calls_on_more_than_the_caches_hold_equal_small_ones():
+    """More than 268 MB are read and written past the caches; the parts of such a call, each by itself, are not."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    H, L = 11, 32003                                            # 270 MB
+    K, V = (torch.randn(1, H, L, 128, generator=g, device="cuda").half() for _ in range(2))
+    perm = torch.stack([torch.randperm(L, generator=g, device="cuda") for _ in range(H)])[None].int()
+    n = -(-L // 64)
+    got = [torch.zeros(1, H, L, 128, dtype=sq.F8, device="cuda") for _ in range(2)] + [torch.zeros(1, H, n, device="cuda") for _ in range(2)]
+    sq.sq_kv_quantize(sq.make_shape(1, H, L, 1, 1, 0, 1.0), K, V, perm, *got)
+    for h in range(H):
+        want = [torch.zeros(1, 1, L, 128, dtype=sq.F8, device="cuda") for _ in range(2)] + [torch.zeros(1, 1, n, device="cuda") for _ in range(2)]
+        sq.sq_kv_quantize(sq.make_shape(1, 1, L, 1, 1, 0, 1.0), *(x[:, h:h + 1].clone() for x in (K, V, perm)), *want)
+        for a, b in zip(got, want):
+            assert torch.equal(a[:, h:h + 1].view(torch.uint8 if a.dtype is sq.F8 else a.dtype), b.view(torch.uint8 if b.dtype is sq.F8 else b.dtype))
+    H, T, G = 5, 17001, 5                                       # 304 and 283 MB
+    for rot_dim, adjacent in ((128, False), (64, True)):
+        w = cu(np.linspace(0.5, 1.5, 128).astype(np.float16))
+        rot = sq.make_rotary(cu(table(100, rot_dim)), adjacent, w, w, eps=2.0 ** -20)
+        x = torch.randn(T, H * (G + 2), 128, generator=g, device="cuda").half()
+        pos = (torch.arange(T, device="cuda") % 100).int()
+        parts = (x[:, :H * G], x[:, H * G:H * G + H], x[:, H * G + H:])
+        outs = [torch.zeros(1, h, T, 128, dtype=torch.float16, device="cuda") for h in (H * G, H, H)]
+        sq.sq_head_norm_rotate(sq.make_shape(1, H, 1, 1, T, 0, 1.0), G, rot, pos, *parts, *outs)
+        # ... and of an append, its queries
+        table_ = torch.arange(-(-T // 64), device="cuda").int()[None]
+        cache = sq.make_cache(*(torch.zeros(len(table_[0]), H, 64, 128, dtype=sq.F8, device="cuda") for _ in range(2)),
+                              *(torch.zeros(len(table_[0]), H, device="cuda") for _ in range(2)), table_)
+        q_out = torch.zeros(T, H * G, 128, dtype=torch.float16, device="cuda")
+        sq.sq_cache_append(sq.make_shape(1, H, 1, 1, T, 0, 1.0), G, rot, cache, torch.zeros(1, dtype=torch.int32, device="cuda"), pos, *parts, q_out)
+        for i in range(0, T, 2000):
+            m = min(2000, T - i)
+            want = [torch.zeros(1, h, m, 128, dtype=torch.float16, device="cuda") for h in (H * G, H, H)]
+            sq.sq_head_norm_rotate(sq.make_shape(1, H, 1, 1, m, 0, 1.0), G, rot, pos[i:i + m].clone(), *(p[i:i + m] for p in parts), *want)
+            for a, b in zip(outs, want):
+                assert torch.equal(a[:, :, i:i + m], b)
+        some = torch.arange(0, T, 7)
+        want = ref.norm_rotate(parts[0][some.cuda()].cpu().numpy(), np.linspace(0.5, 1.5, 128).astype(np.float16), 2.0 ** -20,
+                               table(100, rot_dim), some.numpy() % 100, adjacent)
+        rows_close(q_out.cpu().numpy()[some], want, None, True)

@@ -5,6 +5,14 @@
 // the kept keys of the fixed context, then the user's -- are cut into tiles of 32; the tiles of all rows, laid end to end, are cut
 // into equal shares, one per workgroup, so rows that keep more get more of the chip.  What bounds it is the 256 bytes of a key and
 // its value, read once per row.
+//
+// A wave lists 64 keys at a time, a step before it reads them, by itself: no barrier stands between two tiles, and two workgroups a CU
+// hide the reads; two tiles on their way instead of one are slower (32 heads 16 -> 18 us), three
+// workgroups with registers in memory much slower.  Measured, kernel and merge:
+//   8 sequences x 8 heads of 4 queries with one set, 128K keys of which 1/16, up to 16K user keys (318 MB): 62 + 5 us, 4.8 TB/s
+//   32 heads, 32K keys of which 1/8, 512 user keys (38 MB):           13 + 4 us: a chain of reads (the row's numbers, its ranges, the
+//                                                                     scales, keys, values), a tile or two a wave, and a second launch
+//   4 heads, 4096 keys of which 1/4, 128 user keys (1.2 MB):          7 + 3 us, as long as the calling thread takes for two launches
 #include "sq_decode_q8.hpp"
 
 namespace sq {

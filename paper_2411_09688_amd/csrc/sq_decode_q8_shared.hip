@@ -6,6 +6,9 @@
 // once for all rows, the scores of rows that do not keep it hidden.  So a key that several rows keep is read once, not once per row;
 // what bounds it is the 256 bytes of a key and its value over the union of the rows' sets.  The rows' own user keys follow in the same
 // way, hidden from the other rows, and divided among the S workgroups of the group, each of which leaves one partial result per query.
+// 16 sequences over 32 heads of 32K keys that keep 1/8 each, up to 256 user keys (264 MB with the union; the rows by themselves 660 MB):
+// 60 + 5 us for the kernel and the merge, 4.4 TB/s, where the rows by themselves take 89.  Marking, listing and folding take the vector
+// units 25 us of that, at two workgroups a CU.
 //
 // A NaN among the values of a key that is hidden from a row would still reach it, as zero times NaN.  A workgroup that ends with a NaN
 // therefore takes its rows again, one by one, with that row's keys only.
@@ -22,7 +25,7 @@ constexpr int BATCH = BATCH_WORDS / WINDOW_WORDS;
 
 }  // namespace
 
-template <bool WIDE>
+template <bool WIDE, bool STREAM>
 __global__ __launch_bounds__(256, 2) void decode_q8_shared_kernel(DecodeQ8Args a)
 {
     typedef decltype(KeyList<WIDE>::at[0] + 0) offset_t;
@@ -230,16 +233,16 @@ __global__ __launch_bounds__(256, 2) void decode_q8_shared_kernel(DecodeQ8Args a
             auto load_k = [&](int t) {
                 const auto *at = t < tiles ? s_list[wave][(t >> 1) & 1].at + (t & 1) * QT : s_none;
                 const offset_t k0 = at[c16] + 32 * g4, k1 = at[16 + c16] + 32 * g4;
-                k[0][0] = *reinterpret_cast<global<u4v>>(Kb + k0);
-                k[0][1] = *reinterpret_cast<global<u4v>>(Kb + k0 + 16);
-                k[1][0] = *reinterpret_cast<global<u4v>>(Kb + k1);
-                k[1][1] = *reinterpret_cast<global<u4v>>(Kb + k1 + 16);
+                k[0][0] = load_once<STREAM>(reinterpret_cast<global<u4v>>(Kb + k0));
+                k[0][1] = load_once<STREAM>(reinterpret_cast<global<u4v>>(Kb + k0 + 16));
+                k[1][0] = load_once<STREAM>(reinterpret_cast<global<u4v>>(Kb + k1));
+                k[1][1] = load_once<STREAM>(reinterpret_cast<global<u4v>>(Kb + k1 + 16));
             };
             auto load_v = [&](int t) {
                 const auto *at = (t < tiles ? s_list[wave][(t >> 1) & 1].at + (t & 1) * QT : s_none) + 4 * g4;
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    v[i] = *reinterpret_cast<global<u2v>>(Vb + (offset_t)(at[(i < 4 ? 0 : 12) + i] + 8 * c16));
+                    v[i] = load_once<STREAM>(reinterpret_cast<global<u2v>>(Vb + (offset_t)(at[(i < 4 ? 0 : 12) + i] + 8 * c16)));
             };
             list(0);
             load_k(0);
@@ -290,7 +293,11 @@ __global__ __launch_bounds__(256, 2) void decode_q8_shared_kernel(DecodeQ8Args a
 void launch_decode_q8_shared(const DecodeQ8Args &a, bool wide, hipEvent_t ev0, hipEvent_t ev1, hipStream_t s)
 {
     const int grid = (a.H * a.groups * a.parts + 7) / 8 * 8;
-    auto *kernel = wide ? decode_q8_shared_kernel<true> : decode_q8_shared_kernel<false>;
+    // Where a head has one group of rows, nothing is read twice: past the caches, if the context is more than they hold (16 sequences over
+    // 32 heads of 32K keys 70 -> 63 us; 40 sequences, three groups, the other way round, 40 -> 45).
+    const bool once = a.groups == 1 && streams((size_t)a.H * a.L * D * 2);
+    auto *kernel = wide ? (once ? decode_q8_shared_kernel<true, true> : decode_q8_shared_kernel<true, false>)
+                        : (once ? decode_q8_shared_kernel<false, true> : decode_q8_shared_kernel<false, false>);
     if (ev0) hipExtLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, ev0, ev1, 0, a);
     else hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, a);
 }

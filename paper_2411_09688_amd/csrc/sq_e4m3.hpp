@@ -17,8 +17,8 @@ typedef uint32_t u2v __attribute__((ext_vector_type(2)));
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 
 // What a kernel reads or writes once.  STREAM: past the caches, where the call's data would not stay in them.
-template <bool STREAM, typename T>
-__device__ __forceinline__ T load_once(const T *p)
+template <bool STREAM, typename P>
+__device__ __forceinline__ auto load_once(P p)
 {
     return STREAM ? __builtin_nontemporal_load(p) : *p;
 }

@@ -1,7 +1,8 @@
 // sq_head_norm_rotate: a projection's token-major rows normed, rotated and laid out head by head.
 //
 // One pass over the data and nothing else: 256 bytes read and 256 written per row of a head, and the token's 8 bytes per pair
-// of the table once for all of its heads.
+// of the table once for all of its heads.  What bounds it is the memory: 32768 tokens of 32 + 8 + 8 heads (822 MB) 145 to 149 us,
+// 5.6 TB/s, 1024 tokens of 32 + 32 + 32 heads (50 MB, which the caches hold) 10.0; a single token 4 us, a chain of three reads.
 #include "sq_head_row.hpp"
 #include "sq_internal.hpp"
 

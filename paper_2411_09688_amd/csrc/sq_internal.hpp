@@ -349,12 +349,12 @@ hipError_t launch_decode_attn_index(const void *q, const void *Kf, const void *V
 
 // Keys and values in 8 bits (sq_head_rows.hip, sq_quantize.hip, sq_cache.hip, sq_decode_q8.hip).
 struct RotaryArgs;
-// What a call of these reads and writes once passes the caches if it is more than the last of them holds: 256 MB.  us per call with the
+// What a call of these reads and writes once passes the caches if it is what the last of them holds or more: 256 MB.  us per call with the
 // caches / past them, a call on what the call before it used, and on what four calls before it did:
 //   norm and rotation:  101 MB 17.7 / 20.5, 23.1 / 21.1;  201 MB 33.6 / 38.3, 40.3 / 37.8;  403 MB 75.7 / 69.0;  1611 MB 297 / 275
 //   quantizing:         101 MB 19.9 / 20.0, 24.7 / 20.5;  202 MB 35.5 / 36.5, 43.4 / 37.7;  405 MB 78.4 / 68.2;   810 MB 148 / 130
 constexpr size_t CACHED_BYTES = 256u << 20;
-inline bool streams(size_t bytes) { return bytes > CACHED_BYTES; }
+inline bool streams(size_t bytes) { return bytes >= CACHED_BYTES; }
 struct HeadRows {                  // queries, keys, values; n: heads (0: not given)
     const _Float16 *src[3];
     _Float16 *dst[3];
@@ -413,11 +413,11 @@ struct DecodeQ8Args {
 //    8 rows of each of  8 heads x   4096 ( 262 K)      10.6 / 18.6   11.1 / 19.5   13.3 / 19.8
 //   16               x  8       x   4096 ( 524 K)      10.9 / 21.3   12.8 / 22.2   18.1 / 21.1
 //    8               x  4       x  16384 ( 524 K)      10.5 / 19.5   12.3 / 20.7   18.5 / 22.0
-//   16               x  8       x  16384 (  2 M)       15.8 / 23.0   23.2 / 24.2   37.1 / 24.5
-//    8               x  8       x  32768 (  2 M)       16.0 / 21.4   23.1 / 23.4   38.5 / 26.5
-//    8               x 32       x  32768 (  8 M)       25.8 / 30.7   51.5 / 55.2    121 / 69.6
-//   40               x  8       x  32768 ( 10 M)       28.0 / 33.4   53.7 / 44.3    117 / 48.6
-//   16               x  8       x 131072 ( 17 M)       30.8 / 40.7   83.2 / 66.4    224 / 84.0
+//   16               x  8       x  16384 (  2 M)       15.8 / 23.2   23.2 / 24.9   37.1 / 26.6
+//    8               x  8       x  32768 (  2 M)       16.0 / 21.4   23.1 / 24.2   38.5 / 28.2
+//    8               x 32       x  32768 (  8 M)       25.8 / 33.3   51.5 / 51.6    121 / 64.4
+//   40               x  8       x  32768 ( 10 M)       28.0 / 33.4   53.7 / 40.5    117 / 46.4
+//   16               x  8       x 131072 ( 17 M)       30.8 / 43.6   83.2 / 64.8    224 / 82.8
 constexpr long long Q8_SHARED_MIN_KEYS = 2 << 20;
 constexpr int Q8_SHARED_GRID = 512, Q8_WINDOW = 256;
 struct Q8Groups {

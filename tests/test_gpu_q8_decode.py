@@ -130,6 +130,7 @@ CASES = [  # B, H, Lq, L, C, keep, lengths, page, one_set, spread
     (2, 2, 8, 70000, 500, [0.02, 0.0, 0.04], [90, 0], 16, False, 0),
     (9, 2, 2, 131072, 3000, [0.01, 0.03], [3] * 9, 64, True, 2),           # two query heads to a set, eight rows to a group
     (40, 8, 1, 131072, 4096, [0.004, 0.01], [40] * 40, 16, False, 0),      # more windows than are marked at a time
+    (8, 8, 1, 131072, 2048, [0.01, 0.0, 0.03], [40, 0] * 4, 16, False, 2),  # a context of 268 MB, and one group: past the caches
     (11, 1, 3, 65536, 16, [0.0] * 30 + [1.0], [3000] + [0] * 10, 16, False, 0),   # one sequence's own; one row of everything
 ]
 

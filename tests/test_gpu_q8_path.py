@@ -134,7 +134,7 @@ def test_a_pool_of_more_than_4_gb():
         ref.append(codes[i], scales[i], local, [0] * B, new, first, x[i].astype(np.float64))
         assert np.array_equal((K8, V8)[i].view(torch.uint8)[torch.from_numpy(used).cuda().long()].cpu().numpy(), codes[i])
         assert np.array_equal((ks, vs)[i][torch.from_numpy(used).cuda().long()].cpu().numpy(), scales[i].astype(np.float32))
-    for L in (None, 32768):                                     # 8 sequences x 8 heads x 32768 keys: the union
+    for L in (None, 32768, 131072):                             # 8 sequences x 8 heads x 32768 keys: the union; 131072: past the caches
         sh = sq.make_shape(B, H, L or 1, 2, 1, 0, SCALE)
         fixed = [None] * 7
         if L:

@@ -6,7 +6,7 @@
 // once for all rows, the scores of rows that do not keep it hidden.  So a key that several rows keep is read once, not once per row;
 // what bounds it is the 256 bytes of a key and its value over the union of the rows' sets.  The rows' own user keys follow in the same
 // way, hidden from the other rows, and divided among the S workgroups of the group, each of which leaves one partial result per query.
-// 16 sequences over 32 heads of 32K keys that keep 1/8 each, up to 256 user keys (264 MB with the union; the rows by themselves 660 MB):
+// 16 sequences over 32 heads of 32K keys that keep 1/8 each, up to 256 user keys (264 MB with the union; the rows by themselves 550 MB):
 // 60 + 5 us for the kernel and the merge, 4.4 TB/s, where the rows by themselves take 89.  Marking, listing and folding take the vector
 // units 25 us of that, at two workgroups a CU.
 //

@@ -8,11 +8,11 @@
 // million.  So the arithmetic is fp32 with a bound on its error: where the value less the bound and the value and the bound have
 // the same code, that is the code; the others, of one wave in twenty, are taken again in double precision.
 //
-// 16384 tokens of 13 prompts, 32 query and 8 K/V heads (372 MB): 88 us, 4.2 TB/s.  The queries alone take 55, at what the memory
-// gives; keys and values alone 44, of which the memory needs 20: their reads follow one another (the sequence's length, the page and
-// the position, the row of the table), five waves a SIMD hide that in part (four: 100 us in all; six, with registers in memory: 117).
-// In double precision throughout keys and values took 77.  One token of a sequence: 3.7 us on the GPU, one of 64 sequences 4.8, a chain
-// of the same reads; the call itself takes the calling thread 7.
+// 16384 tokens of 13 prompts, 32 query and 8 K/V heads (372 MB): 81 us, 4.6 TB/s.  Most of it are the queries, at the memory's rate.
+// Keys and values wait for reads that follow one another (the sequence's length, the page and the position, the row of the table); rows,
+// positions and weights are asked for without a branch between them (88 us with), and five waves a SIMD hide part of the rest (four: 7 us
+// more; six, with registers in memory: 23 more).  In double precision throughout keys and values took 77 alone.  One token of a
+// sequence: 3.7 us on the GPU, one of 64 sequences 4.8, a chain of the same reads; the call itself takes the calling thread 7.
 #include "sq_head_row.hpp"
 #include "sq_internal.hpp"
 
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(256, 5) void cache_append_kernel(AppendArgs a, Rota
             rows.src[i] = a.q + (size_t)token * a.q_stride + (size_t)h * D;
             rows.dst[i] = a.q_out + ((size_t)token * a.Hq + h) * D;
         }
-        turn_rows<ADJACENT, PARTIAL, STREAM>(rows, ra, ra.rot_dim ? a.positions[token] : 0, j);
+        turn_rows<ADJACENT, PARTIAL, STREAM>(rows, ra, a.positions[ra.rot_dim ? token : 0], j);
         return;
     }
     const int hv = blockIdx.x % (2 * a.H), unit = blockIdx.x / (2 * a.H);
@@ -166,12 +166,15 @@ __global__ __launch_bounds__(256, 5) void cache_append_kernel(AppendArgs a, Rota
     auto row_of = [&](int token) {
         return (value ? a.v + (size_t)token * a.v_stride : a.k + (size_t)token * a.k_stride) + (size_t)h * D;
     };
-    auto position_of = [&](int token) { return ra.rot_dim ? a.positions[token] : 0; };
+    auto position_of = [&](int token) { return a.positions[ra.rot_dim ? token : 0]; };
     float x[T][8];
     h4 wa = {}, wb = {};
     {
         h4 lo[T], hi[T];
         float cs[T][8];
+        int position[T];                                    // (first: the table's rows are waited for behind them)
+#pragma unroll
+        for (int i = 0; i < T; ++i) position[i] = position_of(token_of(i));
 #pragma unroll
         for (int i = 0; i < T; ++i) {
             const _Float16 *src = row_of(token_of(i));
@@ -184,7 +187,7 @@ __global__ __launch_bounds__(256, 5) void cache_append_kernel(AppendArgs a, Rota
                 wb = *reinterpret_cast<const h4 *>(ra.weight[1] + lp.b);
             }
 #pragma unroll
-            for (int i = 0; i < T; ++i) load_turn(cs[i], ra, position_of(token_of(i)), j, lp.turns);
+            for (int i = 0; i < T; ++i) load_turn(cs[i], ra, position[i], j, lp.turns);
         }
         if (page < 0 || page >= a.n_pages) return;
 #pragma unroll
@@ -314,11 +317,12 @@ hipError_t launch_cache_append(AppendArgs a, const RotaryArgs &ra, hipStream_t s
     const long long q = a.q ? ((long long)a.n_tokens * 16 + threads - 1) / threads * ((a.Hq + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE) : 0;
     if (kv + q > 0x7fffffffll) return hipErrorInvalidConfiguration;
     a.kv_blocks = (int)kv;
+    if (ra.rot_dim == 0) a.positions = a.seq_len;           // (read all the same, without a branch, and not used)
 #define SQ_APPEND_1(A, P) cache_append_kernel<1, A, P, false>
 #define SQ_APPEND_2(A, P) cache_append_kernel<2, A, P, false>
 #define SQ_APPEND_4(A, P) cache_append_kernel<4, A, P, false>
 #define SQ_APPEND_STREAM(A, P) cache_append_kernel<4, A, P, true>
-    // (only the queries pass the caches, 94 -> 88 us for 16384 tokens of 32 + 8 heads; keys and values as well: 90.  Where no sequence
+    // (only the queries pass the caches, 6 us less for 16384 tokens of 32 + 8 heads; keys and values as well: 4 less.  Where no sequence
     // brings many tokens, the rows of a call are few)
     const bool stream = a.q && streams((size_t)a.n_tokens * ((size_t)a.Hq * 4 + (size_t)a.H * 6) * D);
     auto *kernel = most > 32 ? (stream ? SQ_FOR_ROTARY(ra, SQ_APPEND_STREAM) : SQ_FOR_ROTARY(ra, SQ_APPEND_4)) : most > 16 ? SQ_FOR_ROTARY(ra, SQ_APPEND_2) : SQ_FOR_ROTARY(ra, SQ_APPEND_1);

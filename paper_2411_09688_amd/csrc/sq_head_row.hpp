@@ -101,25 +101,26 @@ __device__ __forceinline__ void turn_rows(const TurnRows &t, const RotaryArgs &r
     const LanePieces lp = lane_pieces<ADJACENT, PARTIAL>(j, ra.rot_dim);
     h4 x[ROWS_AT_ONCE], y[ROWS_AT_ONCE];
 #pragma unroll
-    for (int i = 0; i < ROWS_AT_ONCE; ++i)
-        if (i < t.n) {
-            x[i] = load_once<STREAM>(reinterpret_cast<const h4 *>(t.src[i] + lp.a));
-            y[i] = load_once<STREAM>(reinterpret_cast<const h4 *>(t.src[i] + lp.b));
-        }
+    for (int i = 0; i < ROWS_AT_ONCE; ++i) {                // (behind the last the last again, without a branch)
+        x[i] = load_once<STREAM>(reinterpret_cast<const h4 *>(t.src[i] + lp.a));
+        y[i] = load_once<STREAM>(reinterpret_cast<const h4 *>(t.src[i] + lp.b));
+    }
     float cs[8];
     load_turn(cs, ra, position, j, lp.turns && t.kind[0] != 2);   // (values come last)
+    h4 wa[2] = {}, wb[2] = {};
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        if (ra.weight[k]) {
+            wa[k] = *reinterpret_cast<const h4 *>(ra.weight[k] + lp.a);
+            wb[k] = *reinterpret_cast<const h4 *>(ra.weight[k] + lp.b);
+        }
 #pragma unroll
     for (int i = 0; i < ROWS_AT_ONCE; ++i)
         if (i < t.n) {
             if (t.kind[i] != 2) {
-                const _Float16 *weight = ra.weight[t.kind[i]];
+                const bool key = t.kind[i] == 1;
                 float e[8];
-                h4 wa = {}, wb = {};
-                if (weight) {
-                    wa = *reinterpret_cast<const h4 *>(weight + lp.a);
-                    wb = *reinterpret_cast<const h4 *>(weight + lp.b);
-                }
-                norm_rotate<ADJACENT, PARTIAL>(e, x[i], y[i], wa, wb, weight != nullptr, ra.eps, cs, lp.turns);
+                norm_rotate<ADJACENT, PARTIAL>(e, x[i], y[i], key ? wa[1] : wa[0], key ? wb[1] : wb[0], ra.weight[key] != nullptr, ra.eps, cs, lp.turns);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     x[i][c] = (_Float16)e[c];

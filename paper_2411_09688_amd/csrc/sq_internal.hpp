@@ -363,7 +363,7 @@ struct HeadRows {                  // queries, keys, values; n: heads (0: not gi
     int Lq;
     const int32_t *positions;
 };
-hipError_t launch_head_rows(const HeadRows &hr, const RotaryArgs &ra, int tokens, hipStream_t s);
+hipError_t launch_head_rows(HeadRows hr, const RotaryArgs &ra, int tokens, hipStream_t s);
 
 struct QuantizeArgs {              // keys, values (tensors: 1 or 2 of them)
     const _Float16 *X[2];

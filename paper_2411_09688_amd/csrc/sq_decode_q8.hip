@@ -32,11 +32,20 @@ __device__ __forceinline__ RowTiles tiles_of(int nf, int nu)
     const int tf = (nf + QT - 1) / QT;
     return RowTiles{nf, nu, tf, max(1, tf + (nu + QT - 1) / QT)};
 }
-__device__ __forceinline__ RowTiles row_tiles(const DecodeQ8Args &a, int i)
+// A row's numbers, read side by side without a branch (of what is not there, some number that is not used).
+struct RowKeys {
+    int nf, nu;
+};
+__device__ __forceinline__ RowKeys read_row(const DecodeQ8Args &a, const Row &w)
 {
-    const Row w = dealt_row(a, i);
-    return tiles_of(a.ranges ? min(max(a.n_keys[w.r], 0), a.L) : 0, a.seq_len ? min(max(a.seq_len[w.b], 0), a.max_pages << a.p_log) : 0);
+    const int32_t *nf = a.ranges ? a.n_keys + w.r : a.seq_len, *nu = a.seq_len ? a.seq_len + w.b : a.n_keys;
+    return RowKeys{*nf, *nu};
 }
+__device__ __forceinline__ RowTiles row_tiles(const DecodeQ8Args &a, const RowKeys &n)
+{
+    return tiles_of(a.ranges ? min(max(n.nf, 0), a.L) : 0, a.seq_len ? min(max(n.nu, 0), a.max_pages << a.p_log) : 0);
+}
+__device__ __forceinline__ RowTiles row_tiles(const DecodeQ8Args &a, int i) { return row_tiles(a, read_row(a, dealt_row(a, i))); }
 
 __device__ __forceinline__ int block_exclusive(int v, int tid, int *s_w /*[4]*/, int &total)
 {
@@ -101,11 +110,17 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
         if (R <= 256) {
             // every wave for itself, four rows a lane
             const int lane = tid & 63;
+            Row rows[4];
+            RowKeys n[4];
             RowTiles mine[4];
             int sum = 0;
 #pragma unroll
+            for (int k = 0; k < 4; ++k) rows[k] = dealt_row(a, min(4 * lane + k, R - 1));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) n[k] = read_row(a, rows[k]);
+#pragma unroll
             for (int k = 0; k < 4; ++k) {
-                mine[k] = row_tiles(a, min(4 * lane + k, R - 1));
+                mine[k] = row_tiles(a, n[k]);
                 if (4 * lane + k >= R) mine[k].total = 0;
                 sum += mine[k].total;
             }

@@ -219,7 +219,8 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
             const bool fixed = phase == 0;
             const int f0 = fixed ? w0 : max(w0, rt.tf) - rt.tf;          // first tile of the phase, and how many
             const int tiles = (fixed ? min(w1, rt.tf) : w1 - rt.tf) - f0;
-            if (tiles <= 0) continue;
+            // (the one tile of a row without keys reads nothing: where there is no cache there is no first row either)
+            if (tiles <= 0 || (!fixed && rt.nu == 0)) continue;
             const size_t head = fixed ? (size_t)h * a.L * D : 0;
             const global<uint8_t> Kb = uniform((fixed ? a.K8 : a.cK) + head), Vb = uniform((fixed ? a.V8 : a.cV) + head);
             const global<float> kscale = uniform(fixed ? a.ks : a.cks), vscale = uniform(fixed ? a.vs : a.cvs);

@@ -26,7 +26,7 @@ constexpr int O_STRIDE = 132;
 // Offsets of 32 bits go straight into the loads, beside a scalar base: a pool of more than 4 GB takes those of 64 (WIDE).
 template <bool WIDE>
 struct KeyList {
-    std::conditional_t<WIDE, unsigned long long, uint32_t> at[64];   // (0 for a slot without a key: the first row, which there is)
+    std::conditional_t<WIDE, unsigned long long, uint32_t> at[64];   // (0 for a slot without a key: the first row, which there is where a list is made)
     float ks[64], vs[64];                                            // ks: times the softmax's
 };
 struct WaveOut {                             // the four waves' results of a row

@@ -227,28 +227,27 @@ __global__ __launch_bounds__(256, 5) void cache_append_kernel(AppendArgs a, Rota
     float amax = page_max(most);                            // (behind its barrier every thread has read the scale)
     uint32_t again = 0;                                     // tokens to be taken again in double precision, a bit each
     const auto exponent = [](float v) { return scale_exponent(__builtin_bit_cast(uint32_t, v)); };
-    // An infinity sets no scale; and where the largest value lies within its error of one's limit, it is taken exactly (|u| + |v|
-    // is at most twice the larger).
-    const bool near = !value && inexact && exponent(amax * (1.0f - 2 * KEY_ERROR)) != exponent(amax * (1.0f + 2 * KEY_ERROR));
-    if (near || amax > 3.4e38f) {
-        if (near) again = (1u << T) - 1;
+    if (amax > 3.4e38f) {                                   // an infinity sets no scale
+        most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < T; ++i)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) most = fmaxf(most, __builtin_bit_cast(float, finite_abs(x[i][c])));
+        __syncthreads();                                    // (the first maxima have been read)
+        amax = page_max(most);
+    }
+    // Where the largest finite value lies within its error of one's limit, it is taken exactly (|u| + |v| is at most twice the larger).
+    if (!value && inexact && exponent(amax * (1.0f - 2 * KEY_ERROR)) != exponent(amax * (1.0f + 2 * KEY_ERROR))) {
+        again = (1u << T) - 1;
         most = 0.0f;
 #pragma unroll 1
         for (int i = 0; i < T; ++i) {
             float y[8];
-            if (near) {
-                exactly(y, i);
-            } else {
-#pragma unroll
-                for (int k = 0; k < T; ++k)
-                    if (k == i)
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) y[c] = x[k][c];
-            }
+            exactly(y, i);
 #pragma unroll
             for (int c = 0; c < 8; ++c) most = fmaxf(most, __builtin_bit_cast(float, finite_abs(y[c])));
         }
-        __syncthreads();                                    // (the first maxima have been read)
+        __syncthreads();                                    // (the maxima so far have been read)
         amax = page_max(most);
     }
     const int e = max(exponent(amax), e_old);

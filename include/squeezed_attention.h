@@ -587,8 +587,10 @@ typedef struct sq_cache_t {
  * rotation's (NULL if rot_dim is 0) and need not be cache positions.
  * A page's first token sets its scales anew, whatever the page held.  A later token may raise them: the codes of the
  * page's earlier tokens are then multiplied by the old scale over the new one, and rounded again (which is exact for all
- * but the smallest values, those below 2^-6 of the new scale).  Slots behind the last token keep their codes.  Appending
- * the same rows again with the same seq_len leaves the cache as it is, so a step can be repeated.
+ * but the smallest values, those below 2^-6 of the new scale).  A scale that is no power of two (of a page that was not
+ * filled by this call; at most 2^64 in magnitude) is raised to the next one in the same way, the product rounded in fp32
+ * first.  Slots behind the last token keep their codes.  Appending the same rows again with the same seq_len leaves the
+ * cache as it is, so a step can be repeated.
  * The values that are rounded are those of exact arithmetic on the f16 rows, f32 table and f16 weight, up to the rounding
  * of double precision.
  * Out: the cache; q_out f16 [n_tokens, H*G, d] = the normed and rotated queries (for one token per sequence that is

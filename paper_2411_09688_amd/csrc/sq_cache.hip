@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256, 5) void cache_append_kernel(AppendArgs a, Rota
     const size_t ph = (size_t)page * a.H + h;
     uint8_t *codes = (value ? a.V8 : a.K8) + ph * a.P * D;
     float *scale = (value ? a.v_scale : a.k_scale) + ph;
-    const int e_old = p.old > 0 ? exponent_of(*scale) : E4M3_EXP_MIN;
+    const float held = p.old > 0 ? *scale : 0.0f;           // the scale of the page's earlier tokens
     // One token's key, read and computed again in double precision.
     auto exactly = [&](float (&y)[8], int i) {
         const int token = token_of(i);
@@ -250,16 +250,15 @@ __global__ __launch_bounds__(256, 5) void cache_append_kernel(AppendArgs a, Rota
         __syncthreads();                                    // (the maxima so far have been read)
         amax = page_max(most);
     }
-    const int e = max(exponent(amax), e_old);
-    if (p.old > 0 && e > e_old) {
-        const float f = exp2_int(max(e_old - e, -126));
+    const int e = __builtin_amdgcn_readfirstlane(max(exponent(amax), exponent_holding(held)));
+    const float inv = exp2_int(-e), f = held * inv;         // (f: 1 unless the scale rises or was no power of two)
+    if (p.old > 0 && f != 1.0f) {
         for (int i = tid; i < p.old * (D / 16); i += blockDim.x) {
             u4v *c = reinterpret_cast<u4v *>(codes) + i;
             const u4v v = *c;
             *c = u4v{e4m3_rescale4(v.x, f), e4m3_rescale4(v.y, f), e4m3_rescale4(v.z, f), e4m3_rescale4(v.w, f)};
         }
     }
-    const float inv = exp2_int(-e);
     auto store = [&](int i, u2v c) {
         if (i * 16 + g >= p.n) return;
         uint8_t *row = codes + (size_t)(p.old + i * 16 + g) * D;

@@ -39,10 +39,10 @@ __device__ __forceinline__ int scale_exponent(uint32_t amax)
 
 __device__ __forceinline__ float exp2_int(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 
-// Exponent of a stored scale (anything else that may stand there is read as a scale of the legal range).
-__device__ __forceinline__ int exponent_of(float scale)
+// The least e with |scale| <= 2^e, for a scale that stands in a page: of a power of two its own exponent.
+__device__ __forceinline__ int exponent_holding(float scale)
 {
-    const int e = (int)((__builtin_bit_cast(uint32_t, scale) >> 23) & 0xff) - 127;
+    const int e = (int)(((__builtin_bit_cast(uint32_t, scale) & 0x7fffffffu) + 0x7fffffu) >> 23) - 127;
     return min(max(e, E4M3_EXP_MIN), E4M3_EXP_MAX);
 }
 
@@ -72,7 +72,8 @@ __device__ __forceinline__ u2v e4m3_encode8(const float (&x)[8], float inv)
     return e4m3_encode8(y);
 }
 
-// Four codes, scaled by a power of two, to four codes.
+// Four codes times a factor, to four codes (exact before the rounding to codes if the factor is a power of two, else rounded in fp32 first:
+// a product that 24 bits put onto a border between two codes is off by 2^-24 of itself more than half a step).
 __device__ __forceinline__ uint32_t e4m3_rescale4(uint32_t w, float f)
 {
     const f2v a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);

@@ -35,3 +35,30 @@ def test_a_page_with_an_infinity_whose_finite_maximum_is_next_to_a_scales_limit(
     lay = ([None, None], cs, adjacent, sq.make_rotary(cu(cs), adjacent, eps=EPS))
     step(pool, lay, None, cu(x[0]), cu(x[1]), pos, [old], [new], 1, True, repeat=2)
     pool.check()
+
+
+@pytest.mark.parametrize("P,old,new", [(16, 3, 1), (32, 31, 40), (64, 17, 60)])
+@pytest.mark.parametrize("level", [2.0 ** -14, 1.0])
+def test_a_page_whose_scale_is_no_power_of_two_keeps_its_values(P, old, new, level):
+    """Pages filled elsewhere: a scale goes to the next power of two, and the codes with it."""
+    rng = np.random.default_rng(P + new)
+    H = 12
+    pool = Pool(rng, 1, H, P, -(-(old + new) // P))
+    for c, s in zip(pool.codes, pool.scales):
+        c[:] = ref.encode((rng.standard_normal(c.shape) * 100).clip(-448, 448))
+        c[:, :, 1] = np.arange(128) | 0x80                      # every code
+        c[:, :, 2] = np.arange(128)
+        s[:] = np.array([1.1 * 2.0 ** -7, 0.0, 3e-9, -1.5 * 2.0 ** -7, 2.0 ** -70, 1.3 * 2.0 ** -70, 2.0 ** 64, 1.9 * 2.0 ** 63, 1e-39,
+                         2.0 ** -7, 1 + 2.0 ** -23, 2 - 2.0 ** -23]).astype(np.float32)
+    pool.upload()
+    x = (rng.standard_normal((2, new, H, 128)) * level).astype(np.float16)
+    page = pool.table[0, 0]
+    for c, s, rows in zip(pool.codes, pool.scales, x.astype(np.float64)):   # the old codes at the page's new scale, rounded once
+        for h in range(H):
+            top = max(ref.scale_of(rows[:P - old, h]), 2.0 ** np.ceil(np.log2(max(abs(s[page, h]), 2.0 ** -64))))
+            v = ref.VALUES[c[page, h, :old]].astype(np.float32) * np.float32(s[page, h] / top)
+            c[page, h, :old] = np.where(np.isnan(v), c[page, h, :old], ref.encode(v))
+            s[page, h] = top
+    lay = ([None, None], None, False, sq.make_rotary(None))
+    step(pool, lay, None, cu(x[0]), cu(x[1]), np.zeros(new, np.int32), [old], [new], 1, True, repeat=2)
+    pool.check()

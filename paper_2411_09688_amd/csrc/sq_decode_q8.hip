@@ -107,7 +107,7 @@ __global__ __launch_bounds__(256, 2) void decode_q8_kernel(DecodeQ8Args a)
             return true;
         };
         int nf, nu;
-        if (R <= 256) {
+        if (R <= Q8_WAVE_ROWS) {
             // every wave for itself, four rows a lane
             const int lane = tid & 63;
             Row rows[4];
@@ -476,12 +476,8 @@ hipError_t launch_decode_q8(const DecodeQ8Args &args, hipStream_t s)
         a.parts = shared.parts;
         launch_decode_q8_shared(a, wide, timed ? ev0 : nullptr, ev1, s);
     } else {
-        // Workgroups for each row: no search for a share, 3 us less, but a row that keeps more takes longer.  What the rows keep is not
-        // known here; up to 36000 tiles if they kept everything (1.2 million keys), of which they keep some 1/8, the search costs more
-        // than the difference (one set per head, uneven by 1.8 at most, us by rows / in shares: 4 x 4224 keys 10.2 / 12.1; 32 x 33280,
-        // of which 4608, 15.8 / 17.6; 64 x 147456, of which 20000, 73 / 66).
         const long long rows = (long long)a.B * a.H * a.per, most = (a.ranges ? a.L : 0) + (a.seq_len ? a.max_pages << a.p_log : 0);
-        a.splits = rows <= Q8_GRID / 4 && rows * ((most + QT - 1) / QT + 1) <= 36 * 1024 ? (int)(Q8_GRID / rows) : 0;
+        a.splits = q8_splits(rows, most);
         const int grid = a.splits ? (int)rows * a.splits : Q8_GRID;
         auto *kernel = wide ? decode_q8_kernel<true> : decode_q8_kernel<false>;
         if (timed) hipExtLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, ev0, ev1, 0, a);

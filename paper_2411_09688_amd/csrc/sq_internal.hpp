@@ -387,6 +387,7 @@ struct AppendArgs {
 hipError_t launch_cache_append(AppendArgs a, const RotaryArgs &ra, hipStream_t s);
 
 constexpr int Q8_GRID = 512;       // workgroups that share the keys of a call
+constexpr int Q8_WAVE_ROWS = 256;   // rows up to which every wave finds its workgroup's share by itself, four rows a lane
 struct DecodeQ8Args {
     const _Float16 *q;
     const uint8_t *K8, *V8;
@@ -406,6 +407,16 @@ struct DecodeQ8Args {
     int splits;                    // (the launcher's) workgroups of each row, or 0: shares of all rows' tiles
     int groups, rows_per_group, parts;   // (the launcher's) groups of rows of a head that share its keys, 0: none; workgroups of each
 };
+// Workgroups for each row: no search for a share, 3 us less, but a row that keeps more takes longer.  What the rows keep and hold is not
+// known here; up to 36000 tiles if they kept everything and the cache were full (1.2 million keys), of which they keep some 1/8, the search
+// costs more than the difference (one set per head, uneven by 1.8 at most, us by rows / in shares: 4 x 4224 keys 10.2 / 12.1; 32 x 33280,
+// of which 4608, 15.8 / 17.6; 64 x 147456, of which 20000, 73 / 66; nothing was measured between the last two).  So a page table far
+// larger than what the sequences hold takes the second form, and those 2 us.
+constexpr long long Q8_ROW_TILES = 36 * 1024;
+inline int q8_splits(long long rows, long long most_keys)   // workgroups of each row, or 0: shares of all rows' tiles
+{
+    return rows <= Q8_GRID / 4 && rows * ((most_keys + 31) / 32 + 1) <= Q8_ROW_TILES ? (int)(Q8_GRID / rows) : 0;
+}
 // Rows of a head that are taken together: from 8 on, in groups that fill 16 columns, and only where the rows have this many keys to
 // select from between them.  Below it what several rows keep comes from the caches again, and marking the union costs more than that.
 // us per call, rows by themselves / their union, by the share of the keys kept (128 user keys a sequence):

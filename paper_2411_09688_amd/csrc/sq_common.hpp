@@ -272,4 +272,13 @@ __device__ __forceinline__ h4 lds_read_tr16(const _Float16 *p)
     return __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_ptr_t)(p)));
 }
 
+// LDS traffic inside a wave needs no hardware barrier (a wave's LDS operations complete in order), only a point
+// the compiler does not move LDS accesses across.
+__device__ __forceinline__ void wave_lds_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 }  // namespace sq

@@ -89,15 +89,6 @@ __device__ __forceinline__ void store_result(const DecodeQ8Args &a, size_t query
     if (d == 0 && a.lse) a.lse[query] = any ? (m + log2f(l)) * 0.69314718055994531f : SQ_NEG_INF;
 }
 
-
-// What one lane writes to LDS another lane of the wave reads.
-__device__ __forceinline__ void wave_lds_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // The thread's index as a value that the compiler cannot move: what is computed from it is computed where it stands, and takes no
 // registers elsewhere.
 __device__ __forceinline__ int thread_here()

@@ -69,15 +69,6 @@ struct WaveLds {                 // private to one wave, except while a segment'
 };
 static_assert(sizeof(_Float16) * 32 * SV_STRIDE >= sizeof(float) * SG * D, "the V tile doubles as the output staging");
 
-// LDS traffic inside a wave needs no hardware barrier (a wave's LDS operations complete in order), only a point
-// the compiler does not move LDS accesses across.
-__device__ __forceinline__ void wave_lds_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 __global__ __launch_bounds__(256, 3) void decode_attn_shared_kernel(
     const _Float16 *__restrict__ q, const _Float16 *__restrict__ Kf, const _Float16 *__restrict__ Vf,
     const _Float16 *__restrict__ Ku, const _Float16 *__restrict__ Vu, DecodePlan plan,

@@ -518,7 +518,8 @@ int sq_calibrate_threshold(const sq_shape_t *shape, const float *logits, const f
  * of tokens: 64 keys of the fixed context in their stored order, or one page of the user cache.  A scale written here is
  * the least power of two 2^e, -64 <= e <= 64, with |x| <= 448 * 2^e for every finite x of the block (2^-64 for a block
  * of zeros), so that dividing by it is exact and each value is rounded once, to nearest even: by at most 2^-4 of itself,
- * or 2^-10 of the scale where that is more.  NaN and infinities become the NaN code, and set no scale.
+ * or 2^-10 of the scale where that is more.  NaN and infinities become the NaN code, and set no scale.  Keys that a scaled
+ * table or weight makes larger than 448 * 2^64 have the scale 2^64, and what rounds past 448 times it is the NaN code.
  * ---------------------------------------------------------------------------------------------------------------- */
 
 /*
@@ -527,8 +528,8 @@ int sq_calibrate_threshold(const sq_shape_t *shape, const float *logits, const f
  *   rotation:             pair (i, i + rot_dim/2) of the first rot_dim dimensions, or (2i, 2i + 1) if interleaved != 0:
  *                         (a, b) <- (a c - b s, b c + a s),  (c, s) = cos_sin[position][i]
  * Dimensions from rot_dim on are only normed.  rot_dim: a multiple of 8 in [0, d]; 0: no rotation (cos_sin not read).  A
- * position outside [0, n_positions) is read as the nearest one inside.  eps must be finite, not
- * negative and not subnormal; cosines and sines may be of any size (a scaled table).
+ * position outside [0, n_positions) is read as the nearest one inside.  eps must be finite, not negative and not subnormal;
+ * cosines and sines may be of any size (a scaled table) that leaves the turned pairs in fp32's range.
  */
 typedef struct sq_rotary_t {
     int32_t rot_dim, interleaved, n_positions;
@@ -611,9 +612,10 @@ int sq_cache_append(const sq_shape_t *shape, int32_t G, const sq_rotary_t *rot, 
  * Lq of the shape is the number of query heads per K/V head, 1 .. 16 (the shape that scored them: logits [B,H,Lq,C]); query
  * head h * Lq + g reads K/V head h.
  * In:  q f16 [B,H*Lq,1,d]; K8, V8 e4m3 [H,L,d], k_scale, v_scale f32 [H,ceil(L/64)] as written by sq_kv_quantize (any finite
- *      scale will do); with one_set == 0, ranges i32 [B,H*Lq,1,C,2], n_ranges, n_keys i32 [B,H*Lq,1]: every query head's own, as
- *      written by sq_select; with one_set != 0, ranges [B,H,C,2], n_ranges, n_keys [B,H]: one kept set for the query heads of a
- *      K/V head, as written by sq_select_mean, and each kept key is read once for them.
+ *      scales will do that leave the scores and 448 times a value's scale in fp32's range); with one_set == 0, ranges i32
+ *      [B,H*Lq,1,C,2], n_ranges, n_keys i32 [B,H*Lq,1]: every query head's own, as written by sq_select; with one_set != 0, ranges
+ *      [B,H,C,2], n_ranges, n_keys [B,H]: one kept set for the query heads of a K/V head, as written by sq_select_mean, and each
+ *      kept key is read once for them.
  *      Ranges ascending, disjoint, within [0, L); n_keys = the sum of their counts (it is read, and divides the work).
  *      Input outside this contract never faults and is not reported: a row uses at most C ranges, entries with count <= 0 are
  *      skipped, and nothing outside [0, L) is read; which keys such a row then attends to is not specified.

@@ -1,11 +1,12 @@
 """Scales of sq_cache_append where they are hard to decide: the codes and scales have to be those of exact arithmetic."""
 import numpy as np
 import pytest
+import torch
 
 import q8_reference as ref
 from paper_2411_09688_amd import binding as sq
 from test_gpu_q8_cache import EPS, Pool, step
-from test_gpu_q8_rows import cu
+from test_gpu_q8_rows import cu, table
 
 pytestmark = pytest.mark.gpu
 
@@ -62,3 +63,27 @@ def test_a_page_whose_scale_is_no_power_of_two_keeps_its_values(P, old, new, lev
     lay = ([None, None], None, False, sq.make_rotary(None))
     step(pool, lay, None, cu(x[0]), cu(x[1]), np.zeros(new, np.int32), [old], [new], 1, True, repeat=2)
     pool.check()
+
+
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("power", [-100, -60, 60, 72, 76, 100])
+def test_keys_that_a_scaled_table_takes_out_of_the_scales_range(norm, power):
+    rng = np.random.default_rng(power + 200)
+    T, H, P = 70, 2, 32
+    pool = Pool(rng, 1, H, P, 3)
+    cs = (table(16, 128) * 2.0 ** power).astype(np.float32)
+    w = (1 + 0.2 * rng.standard_normal(128)).astype(np.float16) if norm else None
+    rot = sq.make_rotary(cu(cs), False, None, None if w is None else cu(w), eps=EPS)
+    k, v = (rng.standard_normal((T, H, 128)).astype(np.float16) for _ in range(2))
+    pos = (np.arange(T) % 16).astype(np.int32)
+    sq.sq_cache_append(sq.make_shape(1, H, 1, 1, T, 0, 1.0), 1, rot, pool.cache, cu(np.zeros(1, np.int32)), cu(pos), None, cu(k), cu(v), None)
+    turned = ref.norm_rotate(k, w, EPS, cs, pos, False)
+    got, scales = pool.d[0].view(torch.uint8).cpu().numpy(), pool.d[2].cpu().numpy()
+    for i in range(3):
+        for h in range(H):
+            x = turned[i * P:(i + 1) * P, h]
+            s = ref.scale_of(x)
+            y = x / s
+            assert scales[pool.table[0, i], h] == s
+            want = ref.encode(np.where(np.abs(y) > 464, np.nan, y.clip(-448, 448)))   # (464: between the last code and what would be the next)
+            assert ref.same_codes(got[pool.table[0, i], h, :len(x)], want).all()

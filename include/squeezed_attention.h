@@ -583,9 +583,10 @@ typedef struct sq_cache_t {
  * tokens' queries: one call per layer and step of a serving loop, for one token of every sequence or for whole prompts.
  * Rows of q, k and v as in sq_head_norm_rotate, n_tokens of them.  Sequence b appends rows cu_tokens[b] .. cu_tokens[b+1]-1
  * (i32 [B+1], from 0, non-decreasing, at most n_tokens; possibly none) or, with cu_tokens NULL, its shape->Lq rows
- * b * Lq .. b * Lq + Lq - 1 (n_tokens must be B * Lq).  seq_len i32 [B] is how many tokens the sequence holds BEFORE the
- * call; the call does not change it.  Tokens past max_pages * page_tokens are dropped; positions i32 [n_tokens] are the
- * rotation's (NULL if rot_dim is 0) and need not be cache positions.
+ * b * Lq .. b * Lq + Lq - 1 (n_tokens must be B * Lq; the faster form where it fits, above all for one token each).
+ * seq_len i32 [B] is how many tokens the sequence holds BEFORE the call; the call does not change it.  Tokens past
+ * max_pages * page_tokens are dropped; positions i32 [n_tokens] are the rotation's (NULL if rot_dim is 0) and need not be
+ * cache positions.
  * A page's first token sets its scales anew, whatever the page held.  A later token may raise them: the codes of the
  * page's earlier tokens are then multiplied by the old scale over the new one, and rounded again (which is exact for all
  * but the smallest values, those below 2^-6 of the new scale).  A scale that is no power of two (of a page that was not

@@ -6,12 +6,13 @@
 // A key's code is decided at a border between two values that lie 1/8 apart, and with the f16 row, the f32 table and the f16 weight
 // given exactly, 53 bits decide it as exact arithmetic does but once in some 10^14 values, where 24 bits would differ once in a
 // million.  So the arithmetic is fp32 with a bound on its error: where the value less the bound and the value and the bound have
-// the same code, that is the code; the others, of one wave in twenty, are taken again in double precision.
+// the same code, that is the code; the others are taken again in double precision, the four tokens of a wave together (counted on the host
+// over standard normal keys: one value in 5000 to 14000 is in doubt, four tokens in 9 to 28 have one, by the kind of rotation).
 //
 // 16384 tokens of 13 prompts, 32 query and 8 K/V heads (372 MB): 81 us, 4.6 TB/s.  Most of it are the queries, at the memory's rate.
 // Keys and values wait for reads that follow one another (the sequence's length, the page and the position, the row of the table); rows,
-// positions and weights are asked for without a branch between them (88 us with), and five waves a SIMD hide part of the rest (four: 7 us
-// more; six, with registers in memory: 23 more).  In double precision throughout keys and values took 77 alone.  One token of a
+// positions and weights are asked for without a branch between them (88 us with), and five waves a SIMD hide part of the rest (four: 3 us
+// more; six, with registers in memory: 25 more; where rot_dim < 128 and a page may get more than 32 tokens, one or two are there at five).  In double precision throughout keys and values took 77 alone.  One token of a
 // sequence: 3.7 us on the GPU, one of 64 sequences 4.8, a chain of the same reads; the call itself takes the calling thread 7.
 #include "sq_head_row.hpp"
 #include "sq_internal.hpp"
@@ -299,7 +300,9 @@ hipError_t launch_cache_append(AppendArgs a, const RotaryArgs &ra, hipStream_t s
     long long units;
     int most;                                               // new tokens that a page can get
     if (a.cu) {
-        // n tokens touch at most n pages, and at most n / P + 2
+        // n tokens touch at most n pages, and at most n / P + 2.  How they are dealt is not known here: the kernel is that of one sequence
+        // with all of them, and where every sequence has one it takes rows of 64 tokens' lanes to it (8 heads of 4 queries, pages of 64, us
+        // with / without cu_tokens: 64 sequences 12.6 / 3.9, 1024 sequences 135 / 13).
         const long long some = a.B < a.n_tokens ? a.B : a.n_tokens;
         units = (long long)a.n_tokens / a.P + 2 * some;
         if (units > a.n_tokens) units = a.n_tokens;

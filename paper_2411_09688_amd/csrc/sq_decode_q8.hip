@@ -7,8 +7,8 @@
 // its value, read once per row.
 //
 // A wave lists 64 keys at a time, a step before it reads them, by itself: no barrier stands between two tiles, and two workgroups a CU
-// hide the reads; two tiles on their way instead of one are slower (32 heads 16 -> 18 us), three
-// workgroups with registers in memory much slower.  Measured, kernel and merge:
+// hide the reads (Q8_GRID; the registers and LDS of three would fit where offsets have 32 bits, which was not measured).  Two tiles on
+// their way instead of one are slower (32 heads 16 -> 18 us).  Measured, kernel and merge:
 //   8 sequences x 8 heads of 4 queries with one set, 128K keys of which 1/16, up to 16K user keys (318 MB): 62 + 5 us, 4.8 TB/s
 //   32 heads, 32K keys of which 1/8, 512 user keys (38 MB):           13 + 4 us: a chain of reads (the row's numbers, its ranges, the
 //                                                                     scales, keys, values), a tile or two a wave, and a second launch

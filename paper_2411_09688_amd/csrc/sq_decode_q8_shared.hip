@@ -8,7 +8,9 @@
 // way, hidden from the other rows, and divided among the S workgroups of the group, each of which leaves one partial result per query.
 // 16 sequences over 32 heads of 32K keys that keep 1/8 each, up to 256 user keys (264 MB with the union; the rows by themselves 550 MB):
 // 60 + 5 us for the kernel and the merge, 4.4 TB/s, where the rows by themselves take 89.  Marking, listing and folding take the vector
-// units 25 us of that, at two workgroups a CU.
+// units 25 us of that (15.2 million vector instructions of 4 cycles over 1024 SIMDs), at two workgroups a CU (Q8_SHARED_GRID; three would
+// fit where offsets have 32 bits, which was not measured).  Each workgroup reads the ranges of all its rows to find its own windows,
+// whatever the rows keep: that is most of the time where they keep little.
 //
 // A NaN among the values of a key that is hidden from a row would still reach it, as zero times NaN.  A workgroup that ends with a NaN
 // therefore takes its rows again, one by one, with that row's keys only.

@@ -301,8 +301,8 @@ hipError_t launch_cache_append(AppendArgs a, const RotaryArgs &ra, hipStream_t s
     int most;                                               // new tokens that a page can get
     if (a.cu) {
         // n tokens touch at most n pages, and at most n / P + 2.  How they are dealt is not known here: the kernel is that of one sequence
-        // with all of them, and where every sequence has one it takes rows of 64 tokens' lanes to it (8 heads of 4 queries, pages of 64, us
-        // with / without cu_tokens: 64 sequences 12.6 / 3.9, 1024 sequences 135 / 13).
+        // with all of them, which gives a page that gets one token the lanes and reads of up to 64 (8 heads of 4 queries, pages of 64, us with
+        // / without cu_tokens: a token of each of 64 sequences 12.6 / 3.9, of 1024 sequences 135 / 13).
         const long long some = a.B < a.n_tokens ? a.B : a.n_tokens;
         units = (long long)a.n_tokens / a.P + 2 * some;
         if (units > a.n_tokens) units = a.n_tokens;

@@ -14,7 +14,6 @@
 
 namespace sq {
 
-
 typedef int i2v __attribute__((ext_vector_type(2)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));

@@ -1,8 +1,9 @@
 /*
  * squeezed_attention.h -- C ABI of the MI355X (gfx950) implementation of the online path of
  * Squeezed Attention (arxiv 2411.09688): centroid scoring, threshold selection with key-range
- * compaction, sparse flash attention for decode and prefill, and the two-level centroid lookup; and
- * of keys and values in 8 bits: rotation, quantization, a paged user cache, and decode on them.
+ * compaction, sparse flash attention for decode and prefill, and the two-level centroid lookup; of
+ * keys and values in 8 bits: rotation, quantization, a paged user cache, and decode on them; and of drafted
+ * tokens: their trees, their attention over the 8-bit keys, and what is accepted of them into the cache.
  *
  * Conventions shared by every entry point
  *   - Every tensor pointer is a DEVICE pointer owned by the caller, contiguous in the stated
@@ -66,7 +67,8 @@ typedef enum sq_call {
     SQ_CALL_HIER_PREFILL_MEAN_STEP = 16,
     SQ_CALL_GQA_MEAN_DECODE_STEP = 17,
     SQ_CALL_HIER_PREFILL_STEP = 18,
-    SQ_CALL_ATTN_DECODE_Q8 = 19
+    SQ_CALL_ATTN_DECODE_Q8 = 19,
+    SQ_CALL_TREE_ATTN_Q8 = 20
 } sq_call;
 
 /*
@@ -633,6 +635,96 @@ int sq_sparse_attn_decode_q8(const sq_shape_t *shape, int32_t one_set, const voi
                              const float *k_scale, const float *v_scale, const int32_t *ranges, const int32_t *n_ranges,
                              const int32_t *n_keys, const sq_cache_t *cache, const int32_t *seq_len, void *out, float *lse,
                              void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * DRAFTED TOKENS -- several tokens of a sequence checked in one step.  A sequence has up to T drafts, numbered 0 .. T-1: draft 0
+ * is the token that has been chosen already and is not in the cache yet, and every other draft follows its parent, a draft with a smaller
+ * number.  parents i32 [B, T]: a parent outside [0, t) is none, and draft t begins a tree of its own (parents[b][0] is not
+ * looked at).  n_drafts i32 [B]: sequence b has drafts 0 .. n_drafts[b] - 1 (clamped to [0, T]); NULL: all T of them.
+ *
+ * A step of a serving loop: sq_tree_prepare; sq_head_norm_rotate on the drafts' rows (Lq = T, positions as written here); sq_centroid_score and
+ * sq_select_mean with Lq = G * T rows per K/V head (the paper's rule for a prompt; give rows behind n_drafts some draft's query, since they
+ * are averaged too); sq_tree_attn_q8; the rest of the model; sq_tree_accept; sq_cache_commit of every layer's k_out and v_out.  None of
+ * them asks the host for what was accepted, so the step can be captured.
+ * ---------------------------------------------------------------------------------------------------------------- */
+
+/*
+ * Masks and positions of trees of drafts.  first_position i32 [B], or NULL: 0.
+ * Out: tree_mask u32 [B,T,ceil(T/32)]: bit (j % 32) of word (j / 32) of row t = draft t is draft j or comes after it in its tree (rows and bits
+ *      of drafts that there are not are 0); positions i32 [B,T] = first_position[b] + number of drafts above t (first_position[b] for
+ *      drafts that there are not).  Either may be NULL, not both.  The outputs must not overlap the inputs or one another.
+ * shape: B, Lq = T, at most SQ_MAX_DRAFTS.  No workspace.  A thread walks up from each draft, so a tree costs its depth.
+ */
+#define SQ_MAX_DRAFTS 1024
+int sq_tree_prepare(const sq_shape_t *shape, const int32_t *parents, const int32_t *n_drafts, const int32_t *first_position,
+                    uint32_t *tree_mask, int32_t *positions, void *stream);
+
+/*
+ * Attention of T drafts of every sequence: exact softmax attention of each draft's query heads over ONE kept set of the fixed context
+ * per (sequence, K/V head), the seq_len[b] tokens of its sequence in the paged cache, and the drafts that the draft sees, one softmax
+ * over the union; fp32 accumulation, the probabilities rounded to f16 (11 bits, down to 2^-28 of the largest) where they multiply values.
+ * Lq of the shape is the number of query rows per K/V head, Lq = G * T for G query heads (1 .. 64) per K/V head: the shape that scored
+ * them (logits [B,H,Lq,C]).
+ * In:  q f16 [B,H*G,T,d] (q_out of sq_head_norm_rotate);
+ *      K8, V8 e4m3 [H,L,d], k_scale, v_scale f32 [H,ceil(L/64)] as written by sq_kv_quantize; ranges i32 [B,H,C,2], n_ranges, n_keys i32
+ *      [B,H] as written by sq_select_mean (ascending, disjoint, within [0, L); n_keys = the sum of their counts: it is read, and divides
+ *      the work).  ranges NULL (then n_ranges, n_keys, K8, V8 and the scales are too): no fixed context.
+ *      cache, seq_len: as in sq_sparse_attn_decode_q8; cache NULL (then seq_len is too): no user keys.
+ *      K_draft, V_draft f16 [B,H,T,d] (k_out and v_out of sq_head_norm_rotate), the drafts' own keys and values; both may be NULL: the
+ *      queries see the context and the cache only.
+ *      tree_mask u32 [B,T,ceil(T/32)]: draft t sees draft j if bit j of row t is set (any mask: it need be no tree, and a row may be
+ *      empty); NULL: a chain, draft t sees drafts 0 .. t -- a prompt behind the context and the cache, of any length.  Bits from n_drafts[b] on
+ *      are not looked at.  It must be NULL where K_draft is.
+ *      One of the three sources at least.  All scales must be positive and normal, finite, and leave the scores in fp32's range.
+ *      Input outside this contract never faults and is not reported: at most C ranges are used, entries with count <= 0 are skipped, nothing
+ *      outside [0, L) is read, a page that is none has no keys; which keys such a row then attends to is not specified.
+ * Out: out f16 [B,H*G,T,d]; lse f32 [B,H*G,T], or NULL.  A row without visible keys gets out = 0 and lse = -inf.  Rows of drafts from
+ *      n_drafts[b] on are left as they were.  out and lse must not overlap the inputs.
+ *      A key that a row does not see has no influence on it, whatever its rows hold; infinities and NaN that it sees make it not finite.
+ *      The keys of all (sequence, head)s are divided into equal shares, so that the order of a row's sums, and with it its last bits, follows
+ *      from the number of keys of all of them.
+ * Workspace: sq_workspace_bytes(shape, SQ_CALL_TREE_ATTN_Q8).
+ */
+int sq_tree_attn_q8(const sq_shape_t *shape, int32_t T, const void *q, const void *K8, const void *V8, const float *k_scale,
+                    const float *v_scale, const int32_t *ranges, const int32_t *n_ranges, const int32_t *n_keys, const sq_cache_t *cache,
+                    const int32_t *seq_len, const void *K_draft, const void *V_draft, const uint32_t *tree_mask, const int32_t *n_drafts,
+                    void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Which drafts the model agrees with.  tokens i32 [B,T]: the drafts' tokens; target i32 [B,T]: the token that the model puts after draft t
+ * (its best one, or one drawn from its distribution: either way the accepted tokens are what it would have generated by itself).  Draft 0 is
+ * accepted; behind an accepted draft t the child with the lowest number whose token is target[t], until there is none.
+ * Out: n_accepted i32 [B] (0 for a sequence without drafts); path i32 [B,T]: the accepted drafts, ascending, then -1; next_token i32 [B] or
+ *      NULL: target of the last accepted draft, the next step's draft 0 (-1 without drafts); new_len i32 [B] or NULL: seq_len[b] +
+ *      n_accepted[b] (seq_len i32 [B] is read only for it, and may be NULL without it).  The outputs must not overlap the inputs or one another.
+ * shape: B, Lq = T, at most SQ_MAX_DRAFTS.  No workspace.
+ */
+int sq_tree_accept(const sq_shape_t *shape, const int32_t *parents, const int32_t *n_drafts, const int32_t *tokens, const int32_t *target,
+                   const int32_t *seq_len, int32_t *n_accepted, int32_t *path, int32_t *next_token, int32_t *new_len, void *stream);
+
+/*
+ * Appends rows that are normed and rotated already to the cache: row path[b][i] (path i32 [B,T], as written by sq_tree_accept; NULL: row i) of
+ * K[b,h] and V[b,h] becomes token seq_len[b] + i of sequence b, for i < n_rows[b] (i32 [B], clamped to [0, T]; NULL: T).  Pages, scales, earlier
+ * tokens and what is dropped are those of sq_cache_append; here the values that are rounded are the f16 rows themselves.  A path entry
+ * outside [0, T) is read as the nearest row inside.  Appending the same rows again with the same seq_len leaves the cache as it is.
+ * In:  K, V f16 [B,H,T,d] (k_out and v_out of sq_head_norm_rotate); seq_len i32 [B]: tokens BEFORE the call, which does not change it.
+ * Out: the cache, which must not overlap the inputs.  A page that a sequence appends to must stand in no other place of the table that this
+ *      call appends to.
+ * shape: B, H, Lq = T, d.  No workspace.
+ */
+int sq_cache_commit(const sq_shape_t *shape, const sq_cache_t *cache, const int32_t *seq_len, const int32_t *path, const int32_t *n_rows,
+                    const void *K, const void *V, void *stream);
+
+/*
+ * Reads a cache back: K_out[b,h,u,:] = key of token first[b] + u of sequence b (first i32 [B], or NULL: 0; a negative one counts as 0), for
+ * u < U with first[b] + u < seq_len[b]; likewise V_out.  A code times its page's scale, rounded to f16 once (to an infinity past f16's range); tokens
+ * of a page that is none are zeros.  Rows without a token are left as they were.  For the calls that take f16 rows: K_user and V_user of a
+ * prefill step, or a conversation on its way to sq_kmeans_normalize, sq_cluster_layout and sq_kv_quantize.
+ * Out: K_out, V_out f16 [B,H,U,d], which must not overlap the inputs or one another.
+ * shape: B, H, U (positive), d.  No workspace.
+ */
+int sq_cache_read(const sq_shape_t *shape, const sq_cache_t *cache, const int32_t *first, const int32_t *seq_len, void *K_out, void *V_out,
+                  void *stream);
 
 /* ------------------------------------------------------------------------------------------------------------------
  * MEASUREMENT HOOKS -- sq_profile_begin / sq_profile_end / sq_probe_stream_read.  Not part of the method and not

@@ -22,7 +22,7 @@ SQ_OK, SQ_ERR_INVALID_ARG, SQ_ERR_UNSUPPORTED, SQ_ERR_WORKSPACE, SQ_ERR_HIP = 0,
  SQ_CALL_DECODE_STEP, SQ_CALL_HIER_DECODE_STEP, SQ_CALL_SELECT_MEAN, SQ_CALL_ATTN_PREFILL_SHARED,
  SQ_CALL_PREFILL_STEP, SQ_CALL_PREFILL_MEAN_STEP, SQ_CALL_GQA_DECODE_STEP, SQ_CALL_MULTILEVEL_SELECT,
  SQ_CALL_MULTILEVEL_DECODE_STEP, SQ_CALL_KMEANS_STEP, SQ_CALL_CALIBRATE, SQ_CALL_HIER_PREFILL_MEAN_STEP, SQ_CALL_GQA_MEAN_DECODE_STEP, SQ_CALL_HIER_PREFILL_STEP,
- SQ_CALL_ATTN_DECODE_Q8) = range(20)
+ SQ_CALL_ATTN_DECODE_Q8, SQ_CALL_TREE_ATTN_Q8) = range(21)
 SQ_MAX_LEVELS = 4
 
 EXPORTS = ("sq_workspace_bytes", "sq_last_error", "sq_version", "sq_centroid_score", "sq_select",
@@ -30,7 +30,8 @@ EXPORTS = ("sq_workspace_bytes", "sq_last_error", "sq_version", "sq_centroid_sco
            "sq_hier_decode_step", "sq_decode_step_noalloc", "sq_select_mean", "sq_sparse_attn_prefill_shared", "sq_prefill_step",
            "sq_prefill_mean_step", "sq_gqa_decode_step", "sq_multilevel_select", "sq_multilevel_decode_step",
            "sq_kmeans_normalize", "sq_kmeans_step", "sq_cluster_layout", "sq_cluster_nest", "sq_calibrate_threshold", "sq_hier_prefill_mean_step", "sq_hier_prefill_step", "sq_gqa_mean_decode_step", "sq_head_norm_rotate", "sq_kv_quantize",
-           "sq_cache_append", "sq_sparse_attn_decode_q8", "sq_profile_begin",
+           "sq_cache_append", "sq_sparse_attn_decode_q8", "sq_tree_prepare", "sq_tree_attn_q8", "sq_tree_accept", "sq_cache_commit",
+           "sq_cache_read", "sq_profile_begin",
            "sq_profile_end", "sq_probe_stream_read")
 
 
@@ -108,6 +109,11 @@ def lib() -> C.CDLL:
         L.sq_kv_quantize.argtypes = [sp] + [vp] * 8
         L.sq_cache_append.argtypes = [sp, i32, rp, ap, i32] + [vp] * 3 + [vp, i64] * 3 + [vp] * 2
         L.sq_sparse_attn_decode_q8.argtypes = [sp, i32] + [vp] * 8 + [ap] + [vp] * 4 + [sz, vp]
+        L.sq_tree_prepare.argtypes = [sp] + [vp] * 6
+        L.sq_tree_attn_q8.argtypes = [sp, i32] + [vp] * 8 + [ap] + [vp] * 8 + [sz, vp]
+        L.sq_tree_accept.argtypes = [sp] + [vp] * 10
+        L.sq_cache_commit.argtypes = [sp, ap] + [vp] * 6
+        L.sq_cache_read.argtypes = [sp, ap] + [vp] * 5
         L.sq_probe_stream_read.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p, C.c_int, C.c_void_p]
         L.sq_profile_begin.argtypes = [C.c_int]
         L.sq_profile_end.argtypes = [C.POINTER(C.c_float)] * 3
@@ -514,6 +520,14 @@ def _raw_stream(stream, device):
     return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
+def _ws_here(ws, device):
+    if ws is None:
+        return None, 0
+    if ws.get_device() != device:
+        raise ValueError(f"the workspace must be on the current device {device}, is on {ws.device}")
+    return ws.data_ptr(), ws.nbytes
+
+
 def sq_head_norm_rotate(shape, G, rot, positions, q, k, v, q_out, k_out, v_out, stream=None):
     """q [B*Lq, H*G, 128], k, v [B*Lq, H, 128] (rows may be apart) -> q_out [B,H*G,Lq,128], k_out, v_out [B,H,Lq,128]."""
     dev = _device_of(stream, rot)
@@ -558,18 +572,78 @@ def sq_sparse_attn_decode_q8(shape, one_set, q, K8, V8, k_scale, v_scale, ranges
     heads = B * H * Lq
     rows = B * H if one_set else heads
     codes, scales, n = H * L * HEAD_DIM, H * ((L + 63) // 64), heads * HEAD_DIM
-    if ws is None:
-        wp, wn = None, 0
-    else:
-        if ws.get_device() != dev:
-            raise ValueError(f"the workspace must be on the current device {dev}, is on {ws.device}")
-        wp, wn = ws.data_ptr(), ws.nbytes
+    wp, wn = _ws_here(ws, dev)
     _check(lib().sq_sparse_attn_decode_q8(
         C.byref(shape), 1 if one_set else 0, _here(q, n, F16, "q", dev), _here(K8, codes, F8, "K8", dev), _here(V8, codes, F8, "V8", dev),
         _here(k_scale, scales, F32, "k_scale", dev), _here(v_scale, scales, F32, "v_scale", dev),
         _here(ranges, rows * shape.C * 2, I32, "ranges", dev), _here(n_ranges, rows, I32, "n_ranges", dev),
         _here(n_keys, rows, I32, "n_keys", dev), None if cache is None else cache.ref, _here(seq_len, B, I32, "seq_len", dev),
         _here(out, n, F16, "out", dev), _here(lse, heads, F32, "lse", dev), wp, wn, _raw_stream(stream, dev)))
+
+
+# Drafted tokens: the same rules.  Masks are i32 tensors that hold the library's u32 words.
+def sq_tree_prepare(shape, parents, n_drafts, first_position, tree_mask, positions, stream=None):
+    """parents [B, T] -> tree_mask i32 [B, T, ceil(T/32)], positions i32 [B, T] (T: Lq of the shape); n_drafts, first_position [B] or None."""
+    dev = _device_of(stream)
+    B, T = shape.B, shape.Lq
+    _check(lib().sq_tree_prepare(
+        C.byref(shape), _here(parents, B * T, I32, "parents", dev), _here(n_drafts, B, I32, "n_drafts", dev),
+        _here(first_position, B, I32, "first_position", dev), _here(tree_mask, B * T * ((T + 31) // 32), I32, "tree_mask", dev),
+        _here(positions, B * T, I32, "positions", dev), _raw_stream(stream, dev)))
+
+
+def sq_tree_attn_q8(shape, T, q, K8, V8, k_scale, v_scale, ranges, n_ranges, n_keys, cache, seq_len, K_draft, V_draft, tree_mask, n_drafts,
+                    out, lse, ws, stream=None):
+    """Lq of the shape: query heads per K/V head times T drafts.  The seven tensors of the fixed context may be None, or cache and seq_len, or
+    K_draft and V_draft; tree_mask None: a chain; n_drafts None: T of them."""
+    dev = _device_of(stream, cache)
+    B, H, L, Lq = shape.B, shape.H, shape.L, shape.Lq
+    if cache is not None:
+        _for_sequences(cache, B, H)
+    heads, codes, scales, drafts = B * H, H * L * HEAD_DIM, H * ((L + 63) // 64), B * H * T * HEAD_DIM
+    n = heads * Lq * HEAD_DIM
+    wp, wn = _ws_here(ws, dev)
+    _check(lib().sq_tree_attn_q8(
+        C.byref(shape), T, _here(q, n, F16, "q", dev), _here(K8, codes, F8, "K8", dev), _here(V8, codes, F8, "V8", dev),
+        _here(k_scale, scales, F32, "k_scale", dev), _here(v_scale, scales, F32, "v_scale", dev),
+        _here(ranges, heads * shape.C * 2, I32, "ranges", dev), _here(n_ranges, heads, I32, "n_ranges", dev),
+        _here(n_keys, heads, I32, "n_keys", dev), None if cache is None else cache.ref, _here(seq_len, B, I32, "seq_len", dev),
+        _here(K_draft, drafts, F16, "K_draft", dev), _here(V_draft, drafts, F16, "V_draft", dev),
+        _here(tree_mask, B * T * ((T + 31) // 32), I32, "tree_mask", dev), _here(n_drafts, B, I32, "n_drafts", dev),
+        _here(out, n, F16, "out", dev), _here(lse, heads * Lq, F32, "lse", dev), wp, wn, _raw_stream(stream, dev)))
+
+
+def sq_tree_accept(shape, parents, n_drafts, tokens, target, seq_len, n_accepted, path, next_token, new_len, stream=None):
+    """parents, tokens, target, path [B, T], the others [B]; n_drafts, next_token, and seq_len with new_len may be None."""
+    dev = _device_of(stream)
+    B, n = shape.B, shape.B * shape.Lq
+    _check(lib().sq_tree_accept(
+        C.byref(shape), _here(parents, n, I32, "parents", dev), _here(n_drafts, B, I32, "n_drafts", dev),
+        _here(tokens, n, I32, "tokens", dev), _here(target, n, I32, "target", dev), _here(seq_len, B, I32, "seq_len", dev),
+        _here(n_accepted, B, I32, "n_accepted", dev), _here(path, n, I32, "path", dev), _here(next_token, B, I32, "next_token", dev),
+        _here(new_len, B, I32, "new_len", dev), _raw_stream(stream, dev)))
+
+
+def sq_cache_commit(shape, cache, seq_len, path, n_rows, K, V, stream=None):
+    """K, V [B, H, T, 128] (T: Lq of the shape); path [B, T] or None: the rows in order; n_rows [B] or None: T of them."""
+    dev = _device_of(stream, cache)
+    B, H, T = shape.B, shape.H, shape.Lq
+    _for_sequences(cache, B, H)
+    n = B * H * T * HEAD_DIM
+    _check(lib().sq_cache_commit(
+        C.byref(shape), cache.ref, _here(seq_len, B, I32, "seq_len", dev), _here(path, B * T, I32, "path", dev),
+        _here(n_rows, B, I32, "n_rows", dev), _here(K, n, F16, "K", dev), _here(V, n, F16, "V", dev), _raw_stream(stream, dev)))
+
+
+def sq_cache_read(shape, cache, first, seq_len, K_out, V_out, stream=None):
+    """Tokens first[b] (None: 0) .. of every sequence -> K_out, V_out [B, H, U, 128] (U of the shape)."""
+    dev = _device_of(stream, cache)
+    B, H = shape.B, shape.H
+    _for_sequences(cache, B, H)
+    n = B * H * shape.U * HEAD_DIM
+    _check(lib().sq_cache_read(
+        C.byref(shape), cache.ref, _here(first, B, I32, "first", dev), _here(seq_len, B, I32, "seq_len", dev),
+        _here(K_out, n, F16, "K_out", dev), _here(V_out, n, F16, "V_out", dev), _raw_stream(stream, dev)))
 
 
 def sq_probe_stream_read(buf: torch.Tensor, sink: torch.Tensor, workgroups: int, nbytes: Optional[int] = None,

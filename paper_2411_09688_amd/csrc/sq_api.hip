@@ -359,6 +359,17 @@ DecodeQ8Ws carve_decode_q8(Carver &cv, const sq_shape_t *sh)
     return w;
 }
 
+// Attention of drafts: partial results of the shares, and which of them are a unit's.
+DecodeQ8Ws carve_tree(Carver &cv, const sq_shape_t *sh)
+{
+    const sq::TreePlan p = sq::tree_plan(sh->B, sh->H, sh->Lq);
+    DecodeQ8Ws w{};
+    if (p.grid == 0) return w;
+    w.part = cv.take<float>(p.parts * sq::PART_STRIDE);
+    w.info = cv.take<int2>((size_t)p.units);
+    return w;
+}
+
 // Second candidate work list, for lookups of more than two levels.
 sq::DecodePlan carve_cand_plan(Carver &cv, const sq_shape_t *sh)
 {
@@ -662,6 +673,9 @@ size_t sq_workspace_bytes(const sq_shape_t *sh, int which)
         return cv.off;
     case SQ_CALL_ATTN_DECODE_Q8:
         carve_decode_q8(cv, sh);
+        return cv.off;
+    case SQ_CALL_TREE_ATTN_Q8:
+        carve_tree(cv, sh);
         return cv.off;
     default:
         return 0;
@@ -1936,6 +1950,262 @@ int sq_sparse_attn_decode_q8(const sq_shape_t *sh, int32_t one_set, const void *
     a.g = one_set ? sh->Lq : 1;
     a.scale = sh->sm_scale * 1.44269504088896341f;
     SQ_HIP(sq::launch_decode_q8(a, static_cast<hipStream_t>(stream)));
+    g_err[0] = 0;
+    return SQ_OK;
+}
+
+namespace {
+
+int check_drafts(const char *fn, const sq_shape_t *sh)
+{
+    if (sh->Lq > SQ_MAX_DRAFTS) return fail(SQ_ERR_UNSUPPORTED, "%s: Lq = %d drafts, at most %d are supported", fn, sh->Lq, SQ_MAX_DRAFTS);
+    return SQ_OK;
+}
+
+// The cache's four tensors and its table, as something that a call writes or only reads.
+int cache_extents(const sq_cache_t *c, const sq_shape_t *sh, bool written, Extent *x)
+{
+    const size_t heads = (size_t)c->n_pages * sh->H, codes = heads * c->page_tokens * sq::D;
+    x[0] = Extent{"K8", c->K8, codes, written};
+    x[1] = Extent{"V8", c->V8, codes, written};
+    x[2] = Extent{"k_scale", c->k_scale, heads * 4, written};
+    x[3] = Extent{"v_scale", c->v_scale, heads * 4, written};
+    x[4] = Extent{"page_table", c->page_table, (size_t)sh->B * c->max_pages * 4, false};
+    return 5;
+}
+
+}  // namespace
+
+int sq_tree_prepare(const sq_shape_t *sh, const int32_t *parents, const int32_t *n_drafts, const int32_t *first_position,
+                    uint32_t *tree_mask, int32_t *positions, void *stream)
+{
+    if (int rc = check_shape(sh, __func__, false)) return rc;
+    if (int rc = check_drafts(__func__, sh)) return rc;
+    SQ_REQUIRE_PTR(parents);
+    SQ_OPTIONAL_PTR(n_drafts);
+    SQ_OPTIONAL_PTR(first_position);
+    SQ_OPTIONAL_PTR(tree_mask);
+    SQ_OPTIONAL_PTR(positions);
+    if (!tree_mask && !positions) return fail(SQ_ERR_INVALID_ARG, "%s: tree_mask and positions are both NULL", __func__);
+    const size_t B = sh->B, rows = B * sh->Lq;
+    const Extent x[] = {{"parents", parents, rows * 4, false},
+                        {"n_drafts", n_drafts, B * 4, false},
+                        {"first_position", first_position, B * 4, false},
+                        {"tree_mask", tree_mask, rows * ((sh->Lq + 31) / 32) * 4, true},
+                        {"positions", positions, rows * 4, true}};
+    if (int rc = check_overlap(__func__, x, 5)) return rc;
+    if (int rc = check_device(__func__)) return rc;
+    const sq::TreeArgs a{parents, n_drafts, first_position, tree_mask, positions, sh->Lq};
+    SQ_HIP(sq::launch_tree_prepare(a, sh->B, static_cast<hipStream_t>(stream)));
+    g_err[0] = 0;
+    return SQ_OK;
+}
+
+int sq_tree_accept(const sq_shape_t *sh, const int32_t *parents, const int32_t *n_drafts, const int32_t *tokens, const int32_t *target,
+                   const int32_t *seq_len, int32_t *n_accepted, int32_t *path, int32_t *next_token, int32_t *new_len, void *stream)
+{
+    if (int rc = check_shape(sh, __func__, false)) return rc;
+    if (int rc = check_drafts(__func__, sh)) return rc;
+    SQ_REQUIRE_PTR(parents);
+    SQ_OPTIONAL_PTR(n_drafts);
+    SQ_REQUIRE_PTR(tokens);
+    SQ_REQUIRE_PTR(target);
+    SQ_OPTIONAL_PTR(seq_len);
+    SQ_REQUIRE_PTR(n_accepted);
+    SQ_REQUIRE_PTR(path);
+    SQ_OPTIONAL_PTR(next_token);
+    SQ_OPTIONAL_PTR(new_len);
+    if (new_len && !seq_len) return fail(SQ_ERR_INVALID_ARG, "%s: new_len without seq_len", __func__);
+    const size_t B = sh->B, rows = B * sh->Lq;
+    const Extent x[] = {{"parents", parents, rows * 4, false}, {"n_drafts", n_drafts, B * 4, false},   {"tokens", tokens, rows * 4, false},
+                        {"target", target, rows * 4, false},   {"seq_len", seq_len, B * 4, false},     {"n_accepted", n_accepted, B * 4, true},
+                        {"path", path, rows * 4, true},        {"next_token", next_token, B * 4, true}, {"new_len", new_len, B * 4, true}};
+    if (int rc = check_overlap(__func__, x, 9)) return rc;
+    if (int rc = check_device(__func__)) return rc;
+    const sq::AcceptArgs a{parents, n_drafts, tokens, target, seq_len, n_accepted, path, next_token, new_len, sh->Lq};
+    SQ_HIP(sq::launch_tree_accept(a, sh->B, static_cast<hipStream_t>(stream)));
+    g_err[0] = 0;
+    return SQ_OK;
+}
+
+int sq_cache_commit(const sq_shape_t *sh, const sq_cache_t *cache, const int32_t *seq_len, const int32_t *path, const int32_t *n_rows,
+                    const void *K, const void *V, void *stream)
+{
+    if (int rc = check_shape(sh, __func__, false)) return rc;
+    if (!cache) return fail(SQ_ERR_INVALID_ARG, "%s: cache is NULL", __func__);
+    if (int rc = check_cache(__func__, sh, cache, seq_len)) return rc;
+    SQ_OPTIONAL_PTR(path);
+    SQ_OPTIONAL_PTR(n_rows);
+    SQ_REQUIRE_PTR(K);
+    SQ_REQUIRE_PTR(V);
+    const size_t B = sh->B, rows = B * sh->H * sh->Lq;
+    // (the grid: a workgroup for each page that may be touched, head and tensor)
+    if ((long long)B * sh->H * 2 > 0x7fffffffll / ((sh->Lq - 1) / cache->page_tokens + 2) || sh->Lq > sq::MAX_L)
+        return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", __func__);
+    Extent x[10] = {{"seq_len", seq_len, B * 4, false},
+                    {"path", path, B * sh->Lq * 4, false},
+                    {"n_rows", n_rows, B * 4, false},
+                    {"K", K, rows * sq::D * 2, false},
+                    {"V", V, rows * sq::D * 2, false}};
+    const int n = 5 + cache_extents(cache, sh, true, x + 5);
+    if (int rc = check_overlap(__func__, x, n)) return rc;
+    if (int rc = check_device(__func__)) return rc;
+    sq::CommitArgs a{};
+    a.K = static_cast<const _Float16 *>(K);
+    a.V = static_cast<const _Float16 *>(V);
+    a.K8 = static_cast<uint8_t *>(cache->K8);
+    a.V8 = static_cast<uint8_t *>(cache->V8);
+    a.k_scale = cache->k_scale;
+    a.v_scale = cache->v_scale;
+    a.page_table = cache->page_table;
+    a.seq_len = seq_len;
+    a.path = path;
+    a.n_rows = n_rows;
+    a.H = sh->H;
+    a.T = sh->Lq;
+    a.P = cache->page_tokens;
+    a.n_pages = cache->n_pages;
+    a.max_pages = cache->max_pages;
+    SQ_HIP(sq::launch_cache_commit(a, sh->B, static_cast<hipStream_t>(stream)));
+    g_err[0] = 0;
+    return SQ_OK;
+}
+
+int sq_cache_read(const sq_shape_t *sh, const sq_cache_t *cache, const int32_t *first, const int32_t *seq_len, void *K_out, void *V_out,
+                  void *stream)
+{
+    if (int rc = check_shape(sh, __func__, false)) return rc;
+    if (sh->U <= 0) return fail(SQ_ERR_INVALID_ARG, "%s: U = %d must be positive", __func__, sh->U);
+    if (!cache) return fail(SQ_ERR_INVALID_ARG, "%s: cache is NULL", __func__);
+    if (int rc = check_cache(__func__, sh, cache, seq_len)) return rc;
+    SQ_OPTIONAL_PTR(first);
+    SQ_REQUIRE_PTR(K_out);
+    SQ_REQUIRE_PTR(V_out);
+    const size_t B = sh->B, rows = B * sh->H * sh->U;
+    if ((long long)B * sh->H * 2 > 0x7fffffffll / ((sh->U + 63) / 64)) return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", __func__);
+    Extent x[9] = {{"seq_len", seq_len, B * 4, false},
+                   {"first", first, B * 4, false},
+                   {"K_out", K_out, rows * sq::D * 2, true},
+                   {"V_out", V_out, rows * sq::D * 2, true}};
+    const int n = 4 + cache_extents(cache, sh, false, x + 4);
+    if (int rc = check_overlap(__func__, x, n)) return rc;
+    if (int rc = check_device(__func__)) return rc;
+    sq::ReadArgs a{};
+    a.K8 = static_cast<const uint8_t *>(cache->K8);
+    a.V8 = static_cast<const uint8_t *>(cache->V8);
+    a.k_scale = cache->k_scale;
+    a.v_scale = cache->v_scale;
+    a.page_table = cache->page_table;
+    a.seq_len = seq_len;
+    a.first = first;
+    a.K = static_cast<_Float16 *>(K_out);
+    a.V = static_cast<_Float16 *>(V_out);
+    a.H = sh->H;
+    a.U = sh->U;
+    a.p_log = cache->page_tokens == 16 ? 4 : cache->page_tokens == 32 ? 5 : 6;
+    a.n_pages = cache->n_pages;
+    a.max_pages = cache->max_pages;
+    SQ_HIP(sq::launch_cache_read(a, sh->B, static_cast<hipStream_t>(stream)));
+    g_err[0] = 0;
+    return SQ_OK;
+}
+
+int sq_tree_attn_q8(const sq_shape_t *sh, int32_t T, const void *q, const void *K8, const void *V8, const float *k_scale,
+                    const float *v_scale, const int32_t *ranges, const int32_t *n_ranges, const int32_t *n_keys, const sq_cache_t *cache,
+                    const int32_t *seq_len, const void *K_draft, const void *V_draft, const uint32_t *tree_mask, const int32_t *n_drafts,
+                    void *out, float *lse, void *ws, size_t ws_bytes, void *stream)
+{
+    if (int rc = check_shape(sh, __func__, false)) return rc;
+    if (T <= 0 || sh->Lq % T || sh->Lq / T > 64)
+        return fail(SQ_ERR_INVALID_ARG, "%s: Lq = %d must be T = %d drafts times 1 .. 64 query heads per K/V head", __func__, sh->Lq, T);
+    SQ_REQUIRE_PTR(q);
+    SQ_REQUIRE_PTR(out);
+    SQ_OPTIONAL_PTR(lse);
+    if (ranges) {
+        SQ_REQUIRE_PTR(ranges);
+        SQ_REQUIRE_PTR(n_ranges);
+        SQ_REQUIRE_PTR(n_keys);
+        SQ_REQUIRE_PTR(K8);
+        SQ_REQUIRE_PTR(V8);
+        SQ_REQUIRE_PTR(k_scale);
+        SQ_REQUIRE_PTR(v_scale);
+    } else if (n_ranges || n_keys || K8 || V8 || k_scale || v_scale) {
+        return fail(SQ_ERR_INVALID_ARG, "%s: a fixed context without ranges", __func__);
+    }
+    if (!cache && seq_len) return fail(SQ_ERR_INVALID_ARG, "%s: seq_len without a cache", __func__);
+    if (cache)
+        if (int rc = check_cache(__func__, sh, cache, seq_len)) return rc;
+    if (!K_draft != !V_draft) return fail(SQ_ERR_INVALID_ARG, "%s: K_draft and V_draft go together", __func__);
+    SQ_OPTIONAL_PTR(K_draft);
+    SQ_OPTIONAL_PTR(V_draft);
+    if (!K_draft && tree_mask) return fail(SQ_ERR_INVALID_ARG, "%s: tree_mask without drafts' keys", __func__);
+    SQ_OPTIONAL_PTR(tree_mask);
+    SQ_OPTIONAL_PTR(n_drafts);
+    if (!ranges && !cache && !K_draft) return fail(SQ_ERR_INVALID_ARG, "%s: neither ranges of a fixed context nor a cache nor drafts' keys", __func__);
+    const sq::TreePlan plan = sq::tree_plan(sh->B, sh->H, sh->Lq);
+    const long long keys = (ranges ? sh->L : 0) + (cache ? (long long)cache->max_pages * cache->page_tokens : 0) + (K_draft ? T : 0);
+    if ((long long)sh->H * sh->L > 0x7fffffffll || (long long)sh->B * sh->H * sh->Lq > 0x3fffffffll || plan.units > 0x7fffffffll / (keys / 32 + 4) ||
+        T > sq::MAX_L)
+        return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", __func__);
+    const size_t B = sh->B, H = sh->H, blocks = (sh->L + sq::KV_BLOCK - 1) / sq::KV_BLOCK, rows = B * H * sh->Lq, drafts = B * H * T;
+    Extent x[20] = {{"out", out, rows * sq::D * 2, true},
+                    {"lse", lse, rows * 4, true},
+                    {"q", q, rows * sq::D * 2, false},
+                    {"K8", K8, H * sh->L * sq::D, false},
+                    {"V8", V8, H * sh->L * sq::D, false},
+                    {"k_scale", k_scale, H * blocks * 4, false},
+                    {"v_scale", v_scale, H * blocks * 4, false},
+                    {"ranges", ranges, B * H * sh->C * 8, false},
+                    {"n_ranges", n_ranges, B * H * 4, false},
+                    {"n_keys", n_keys, B * H * 4, false},
+                    {"seq_len", seq_len, B * 4, false},
+                    {"K_draft", K_draft, drafts * sq::D * 2, false},
+                    {"V_draft", V_draft, drafts * sq::D * 2, false},
+                    {"tree_mask", tree_mask, B * T * ((T + 31) / 32) * 4, false},
+                    {"n_drafts", n_drafts, B * 4, false}};
+    const int n = 15 + (cache ? cache_extents(cache, sh, false, x + 15) : 0);
+    if (int rc = check_overlap(__func__, x, n)) return rc;
+    if (int rc = check_ws(__func__, sh, SQ_CALL_TREE_ATTN_Q8, ws, ws_bytes)) return rc;
+    if (int rc = check_device(__func__)) return rc;
+    Carver cv(ws);
+    const DecodeQ8Ws w = carve_tree(cv, sh);
+    sq::TreeAttnArgs a{};
+    a.q = static_cast<const _Float16 *>(q);
+    a.K8 = static_cast<const uint8_t *>(K8);
+    a.V8 = static_cast<const uint8_t *>(V8);
+    a.ks = k_scale;
+    a.vs = v_scale;
+    a.ranges = ranges;
+    a.n_ranges = n_ranges;
+    a.n_keys = n_keys;
+    if (cache) {
+        a.cK = static_cast<const uint8_t *>(cache->K8);
+        a.cV = static_cast<const uint8_t *>(cache->V8);
+        a.cks = cache->k_scale;
+        a.cvs = cache->v_scale;
+        a.page_table = cache->page_table;
+        a.seq_len = seq_len;
+        a.p_log = cache->page_tokens == 16 ? 4 : cache->page_tokens == 32 ? 5 : 6;
+        a.n_pages = cache->n_pages;
+        a.max_pages = cache->max_pages;
+    }
+    a.Kd = static_cast<const _Float16 *>(K_draft);
+    a.Vd = static_cast<const _Float16 *>(V_draft);
+    a.mask = tree_mask;
+    a.n_drafts = n_drafts;
+    a.out = static_cast<_Float16 *>(out);
+    a.lse = lse;
+    a.part = w.part;
+    a.info = w.info;
+    a.B = sh->B;
+    a.H = sh->H;
+    a.L = sh->L;
+    a.C = sh->C;
+    a.sblocks = (int)blocks;
+    a.G = sh->Lq / T;
+    a.T = T;
+    a.scale = sh->sm_scale * 1.44269504088896341f;
+    SQ_HIP(sq::launch_tree_attn(a, static_cast<hipStream_t>(stream)));
     g_err[0] = 0;
     return SQ_OK;
 }

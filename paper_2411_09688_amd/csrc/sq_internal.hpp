@@ -448,6 +448,73 @@ inline Q8Groups q8_groups(int B, int H, int per, int g, int L)
 void launch_decode_q8_shared(const DecodeQ8Args &a, bool wide, hipEvent_t ev0, hipEvent_t ev1, hipStream_t s);
 hipError_t launch_decode_q8(const DecodeQ8Args &a, hipStream_t s);
 
+// Drafted tokens (sq_drafts.hip, sq_tree_attn.hip).
+constexpr int MAX_DRAFTS = 1024;   // of a tree: a thread each
+struct TreeArgs {
+    const int32_t *parents, *n_drafts, *first;
+    uint32_t *mask;
+    int32_t *positions;
+    int T;
+};
+hipError_t launch_tree_prepare(const TreeArgs &a, int B, hipStream_t s);
+
+struct AcceptArgs {
+    const int32_t *parents, *n_drafts, *tokens, *target, *seq_len;
+    int32_t *n_accepted, *path, *next_token, *new_len;
+    int T;
+};
+hipError_t launch_tree_accept(const AcceptArgs &a, int B, hipStream_t s);
+
+struct CommitArgs {
+    const _Float16 *K, *V;         // [B, H, T, D]
+    uint8_t *K8, *V8;
+    float *k_scale, *v_scale;
+    const int32_t *page_table, *seq_len, *path, *n_rows;
+    int H, T, P, n_pages, max_pages;
+    int per_seq;                   // (the launcher's) pages that a sequence can append to
+};
+hipError_t launch_cache_commit(CommitArgs a, int B, hipStream_t s);
+
+struct ReadArgs {
+    const uint8_t *K8, *V8;
+    const float *k_scale, *v_scale;
+    const int32_t *page_table, *seq_len, *first;
+    _Float16 *K, *V;               // [B, H, U, D]
+    int H, U, p_log, n_pages, max_pages;
+    int chunks;                    // (the launcher's)
+};
+hipError_t launch_cache_read(ReadArgs a, int B, hipStream_t s);
+
+constexpr int TREE_GRID = 512;     // workgroups that share the keys of a call
+struct TreeAttnArgs {
+    const _Float16 *q;             // [B, H, G, T, D]
+    const uint8_t *K8, *V8;
+    const float *ks, *vs;
+    const int32_t *ranges, *n_ranges, *n_keys;
+    const uint8_t *cK, *cV;
+    const float *cks, *cvs;
+    const int32_t *page_table, *seq_len;
+    const _Float16 *Kd, *Vd;       // [B, H, T, D]
+    const uint32_t *mask;
+    const int32_t *n_drafts;
+    _Float16 *out;
+    float *lse;
+    float *part;
+    int2 *info;                    // per unit: first partial result, how many (0: the unit is done)
+    int B, H, L, C, sblocks, G, T;
+    int p_log, n_pages, max_pages;
+    float scale;                   // sm_scale * log2(e)
+    int row_waves, blocks;         // waves of a workgroup that have rows of their own; blocks of rows of a (sequence, head)
+};
+struct TreePlan {
+    int tiles, row_waves, blocks;  // 16 rows each that a wave has; see above
+    long long units;               // (sequence, head, block of rows)
+    int grid;                      // workgroups that share the keys of all units, or 0: a workgroup per unit
+    size_t parts;                  // rows of partial results
+};
+TreePlan tree_plan(int B, int H, int rows);
+hipError_t launch_tree_attn(TreeAttnArgs a, hipStream_t s);
+
 // Records the calling thread's error message (what sq_last_error returns) and hands back `code`.
 int set_error(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 

@@ -662,7 +662,7 @@ int sq_tree_prepare(const sq_shape_t *shape, const int32_t *parents, const int32
 /*
  * Attention of T drafts of every sequence: exact softmax attention of each draft's query heads over ONE kept set of the fixed context
  * per (sequence, K/V head), the seq_len[b] tokens of its sequence in the paged cache, and the drafts that the draft sees, one softmax
- * over the union; fp32 accumulation, the probabilities rounded to f16 (11 bits, down to 2^-28 of the largest) where they multiply values.
+ * over the union; fp32 accumulation, the probabilities rounded to f16 (11 bits, down to 2^-22 of the largest) where they multiply values.
  * Lq of the shape is the number of query rows per K/V head, Lq = G * T for G query heads (1 .. 64) per K/V head: the shape that scored
  * them (logits [B,H,Lq,C]).
  * In:  q f16 [B,H*G,T,d] (q_out of sq_head_norm_rotate);

@@ -362,10 +362,10 @@ DecodeQ8Ws carve_decode_q8(Carver &cv, const sq_shape_t *sh)
 // Attention of drafts: partial results of the shares, and which of them are a unit's.
 DecodeQ8Ws carve_tree(Carver &cv, const sq_shape_t *sh)
 {
-    const sq::TreePlan p = sq::tree_plan(sh->B, sh->H, sh->Lq);
+    const sq::TreePlan p = sq::tree_plan(sh->B, sh->H, sh->Lq, 0);
     DecodeQ8Ws w{};
-    if (p.grid == 0) return w;
-    w.part = cv.take<float>(p.parts * sq::PART_STRIDE);
+    if (sq::tree_parts(p) == 0) return w;
+    w.part = cv.take<float>(sq::tree_parts(p) * sq::PART_STRIDE);
     w.info = cv.take<int2>((size_t)p.units);
     return w;
 }
@@ -2142,9 +2142,9 @@ int sq_tree_attn_q8(const sq_shape_t *sh, int32_t T, const void *q, const void *
     SQ_OPTIONAL_PTR(tree_mask);
     SQ_OPTIONAL_PTR(n_drafts);
     if (!ranges && !cache && !K_draft) return fail(SQ_ERR_INVALID_ARG, "%s: neither ranges of a fixed context nor a cache nor drafts' keys", __func__);
-    const sq::TreePlan plan = sq::tree_plan(sh->B, sh->H, sh->Lq);
     const long long keys = (ranges ? sh->L : 0) + (cache ? (long long)cache->max_pages * cache->page_tokens : 0) + (K_draft ? T : 0);
-    if ((long long)sh->H * sh->L > 0x7fffffffll || (long long)sh->B * sh->H * sh->Lq > 0x3fffffffll || plan.units > 0x7fffffffll / (keys / 32 + 4) ||
+    const sq::TreePlan plan = sq::tree_plan(sh->B, sh->H, sh->Lq, keys);
+    if ((long long)sh->H * sh->L > 0x7fffffffll || (long long)sh->B * sh->H * sh->Lq > 0x3fffffffll || plan.units > 0x7fffffffll / (keys / 32 + 4 + sq::TREE_AHEAD) ||
         T > sq::MAX_L)
         return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", __func__);
     const size_t B = sh->B, H = sh->H, blocks = (sh->L + sq::KV_BLOCK - 1) / sq::KV_BLOCK, rows = B * H * sh->Lq, drafts = B * H * T;

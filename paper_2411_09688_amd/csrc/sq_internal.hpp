@@ -486,6 +486,8 @@ struct ReadArgs {
 hipError_t launch_cache_read(ReadArgs a, int B, hipStream_t s);
 
 constexpr int TREE_GRID = 512;     // workgroups that share the keys of a call
+constexpr int TREE_SHARED_UNITS = 1024;   // blocks of rows up to which they do: each workgroup counts the tiles of all blocks
+constexpr int TREE_AHEAD = 12;     // tiles of 32 keys that take as long as beginning and ending a block
 struct TreeAttnArgs {
     const _Float16 *q;             // [B, H, G, T, D]
     const uint8_t *K8, *V8;
@@ -504,15 +506,16 @@ struct TreeAttnArgs {
     int B, H, L, C, sblocks, G, T;
     int p_log, n_pages, max_pages;
     float scale;                   // sm_scale * log2(e)
-    int row_waves, blocks;         // waves of a workgroup that have rows of their own; blocks of rows of a (sequence, head)
+    int blocks;                    // blocks of rows of a (sequence, head)
 };
 struct TreePlan {
-    int tiles, row_waves, blocks;  // 16 rows each that a wave has; see above
-    long long units;               // (sequence, head, block of rows)
-    int grid;                      // workgroups that share the keys of all units, or 0: a workgroup per unit
-    size_t parts;                  // rows of partial results
+    int tiles, blocks;             // 16 rows each of a block; see above
+    int units;                     // (sequence, head, block of rows)
+    int splits;                    // workgroups of each unit, or 0: shares of all units' tiles
+    long long grid;
 };
-TreePlan tree_plan(int B, int H, int rows);
+TreePlan tree_plan(int B, int H, int rows, long long keys);
+inline size_t tree_parts(const TreePlan &p) { return p.units > TREE_SHARED_UNITS ? 0 : (size_t)2 * TREE_GRID * 16 * p.tiles; }   // rows of partial results
 hipError_t launch_tree_attn(TreeAttnArgs a, hipStream_t s);
 
 // Records the calling thread's error message (what sq_last_error returns) and hands back `code`.

@@ -8,21 +8,24 @@
 // equal shares, one per workgroup; a second launch merges the blocks that several workgroups took.
 //
 //   S^T [32 keys x 16 TILES] = K q^T    codes to f16 (exact), once for all columns
-//   t = S * (key's scale * sm_scale * log2 e) + log2(value's scale),   M = running maximum of t,   p = 2^(t - M + 14)
+//   t = S * (key's scale * sm_scale * log2 e) + log2(value's scale),   M: a reference near the maximum of t,   p = 2^(t - M + 8)
 //   O^T [128 x 16 TILES]    += V^T P^T  codes to f16 (exact), P rounded to f16
 //   l                       += p / value's scale                       (the unrounded p)
-// With the value's scale in the exponent P needs no factor, whatever the scales are: it lies in (0, 2^14], and has its 11 bits down to 2^-28
-// of the largest.  out = O / l, log-sum-exp = (M - 14 + log2 l) ln 2.
+// With the value's scale in the exponent P needs no factor, whatever the scales are: it is at most 2^15, and has its 11 bits down to 2^-22
+// of the largest.  out = O / l, log-sum-exp = (M - 8 + log2 l) ln 2.
+#include <algorithm>
+
 #include "sq_decode_q8.hpp"
 
 namespace sq {
 
 namespace {
 
-constexpr int SENTINEL = INT32_MIN;
 constexpr int GROUP = 64;                    // ranges that a wave holds at a time
 constexpr int MAX_GROUPS = SELECT_MAX_C / GROUP;
-constexpr float LIFT = 14.0f;                // p is at most 2^14
+// The reference M of a column follows its largest t once that is more than 2^SLACK times it: of 64 columns one finds a new maximum in most
+// tiles, and moving a reference costs as much as half a tile.
+constexpr float LIFT = 8.0f, SLACK = 7.0f;   // p is at most 2^15
 
 // 64 keys of a wave: where they stand (as in KeyList), and what their scales make of a score and of a probability.
 template <bool WIDE>
@@ -36,31 +39,53 @@ struct Unit {
     int n;                                   // drafts of the sequence
     int nf, nu, tf, tu, td, total;           // keys and tiles: fixed, user's, drafts'
 };
-
-__device__ __forceinline__ int unit_rows(const TreeAttnArgs &a, int tiles) { return 16 * tiles * a.row_waves; }
+struct Counts {
+    int nf, nu, n;                           // as they stand in memory
+};
 
 // Unit i: the blocks of rows of a head follow one another, head by head, as rows of sq_decode_q8.
-__device__ __forceinline__ Unit unit_of(const TreeAttnArgs &a, int i, int tiles)
+__device__ __forceinline__ Unit place_of(const TreeAttnArgs &a, int i)
 {
     Unit u;
-    u.block = i % a.blocks;
     const int hb = i / a.blocks;
-    u.b = hb % a.B;
+    u.block = i - hb * a.blocks;
     u.h = hb / a.B;
-    // (read side by side without a branch: of what is not there, some number that is not used)
-    const int32_t *some = a.ranges ? a.n_keys : a.seq_len ? a.seq_len : a.n_drafts;
-    const int32_t *pf = a.ranges ? a.n_keys + u.b * a.H + u.h : some, *pu = a.seq_len ? a.seq_len + u.b : some, *pn = a.n_drafts ? a.n_drafts + u.b : some;
-    const int nf = pf ? *pf : 0, nu = pu ? *pu : 0, n = pn ? *pn : 0;
-    u.n = a.n_drafts ? min(max(n, 0), a.T) : a.T;
-    u.nf = a.ranges ? min(max(nf, 0), a.L) : 0;
-    u.nu = a.seq_len ? min(max(nu, 0), a.max_pages << a.p_log) : 0;
+    u.b = hb - u.h * a.B;
+    return u;
+}
+// A unit's numbers, read side by side without a branch (of what is not there, some number that is not used).
+__device__ __forceinline__ Counts counts_of(const TreeAttnArgs &a, const Unit &u)
+{
+    const int32_t *any = a.ranges ? a.n_keys : a.seq_len ? a.seq_len : a.n_drafts ? a.n_drafts : reinterpret_cast<const int32_t *>(a.q);
+    const int32_t *nf = a.ranges ? a.n_keys + u.b * a.H + u.h : any, *nu = a.seq_len ? a.seq_len + u.b : any, *n = a.n_drafts ? a.n_drafts + u.b : any;
+    return Counts{*nf, *nu, *n};
+}
+__device__ __forceinline__ void count(const TreeAttnArgs &a, const Counts &c, int tiles, Unit &u)
+{
+    u.n = a.n_drafts ? min(max(c.n, 0), a.T) : a.T;
+    u.nf = a.ranges ? min(max(c.nf, 0), a.L) : 0;
+    u.nu = a.seq_len ? min(max(c.nu, 0), a.max_pages << a.p_log) : 0;
     u.tf = (u.nf + QT - 1) / QT;
     u.tu = (u.nu + QT - 1) / QT;
-    const int row0 = u.block * unit_rows(a, tiles), rows = min(u.n * a.G, row0 + unit_rows(a, tiles));
+    const int row0 = u.block * 16 * tiles, rows = min(u.n * a.G, row0 + 16 * tiles);
     const int seen = !a.Kd ? 0 : a.mask ? u.n : (rows - 1) / a.G + 1;       // (a chain's last row sees the drafts up to its own)
     u.td = (seen + QT - 1) / QT;
     u.total = rows > row0 ? max(1, u.tf + u.tu + u.td) : 0;                 // (a unit without rows has no tiles, one without keys one)
+}
+__device__ __forceinline__ Unit unit_of(const TreeAttnArgs &a, int i, int tiles)
+{
+    Unit u = place_of(a, i);
+    count(a, counts_of(a, u), tiles, u);
     return u;
+}
+
+// The kernel's arguments, read again from where they stand: what is read from the one reference is not kept for the other, some 60 scalar
+// registers that the loops need.
+__device__ __forceinline__ const TreeAttnArgs &arguments()
+{
+    auto p = (const __attribute__((address_space(4))) TreeAttnArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const TreeAttnArgs *)p;
 }
 
 __device__ __forceinline__ int block_exclusive(int v, int tid, int *s_w /*[4]*/, int &total)
@@ -75,12 +100,19 @@ __device__ __forceinline__ int block_exclusive(int v, int tid, int *s_w /*[4]*/,
     return ex;
 }
 
-__device__ __forceinline__ void store_row(const TreeAttnArgs &a, const Unit &u, int row, int d, float m, float l, float o)
+// Dimensions d .. d + 7 of a row's result: l is zero where it sees no key, and NaN where it sees one.
+__device__ __forceinline__ void store_dims(const TreeAttnArgs &a, const Unit &u, int row, int d, float m, float l, f4 x, f4 y)
 {
     const int t = row / a.G, g = row - t * a.G;
     const size_t at = (((size_t)u.b * a.H + u.h) * a.G + g) * a.T + t;
     const bool any = l > 0.0f || l != l;
-    a.out[at * D + d] = (_Float16)(any ? o / l : 0.0f);
+    h8 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[i] = (_Float16)(any ? x[i] / l : 0.0f);
+        v[4 + i] = (_Float16)(any ? y[i] / l : 0.0f);
+    }
+    *reinterpret_cast<h8 *>(a.out + at * D + d) = v;
     if (d == 0 && a.lse) a.lse[at] = any ? (m - LIFT + log2f(l)) * 0.69314718055994531f : SQ_NEG_INF;
 }
 
@@ -91,27 +123,37 @@ struct Columns {
     f4 o[TILES][8];
 };
 
-// Folds a tile's scores t (key 16 u + 4 g4 + i of column c16 in t[n][4 u + i]) into maximum and sum; p in f16 for the second product.
-template <int TILES>
-__device__ __forceinline__ void fold_scores(Columns<TILES> &st, const float (&t)[TILES][8], const float (&inv)[8], h8 (&p)[TILES])
+// Folds a tile's scores x (key 16 u + 4 g4 + i of column c16 in x[n][4 u + i]) into the maxima and sums of N tiles of columns; p in f16 for
+// the second product.
+template <int N>
+__device__ __forceinline__ void fold_scores(float *m, float *l, f4 (*o)[8], const float (&x)[N][8], const float (&inv)[8], h8 *p)
 {
+    float mx[N];
+    bool more = false;
 #pragma unroll
-    for (int n = 0; n < TILES; ++n) {
-        const float mx = fmaxf(fmaxf(fmaxf(t[n][0], t[n][1]), fmaxf(t[n][2], t[n][3])), fmaxf(fmaxf(t[n][4], t[n][5]), fmaxf(t[n][6], t[n][7])));
-        if (__any(mx > st.m[n])) {                          // (rare behind the first tiles)
-            const float mn = fmaxf(st.m[n], cross16_max(mx));
-            const float alpha = mn == SQ_NEG_INF ? 1.0f : __builtin_amdgcn_exp2f(st.m[n] - mn);
-            st.m[n] = mn;
-            st.l[n] *= alpha;
+    for (int n = 0; n < N; ++n) {
+        mx[n] = fmaxf(fmaxf(fmaxf(x[n][0], x[n][1]), fmaxf(x[n][2], x[n][3])), fmaxf(fmaxf(x[n][4], x[n][5]), fmaxf(x[n][6], x[n][7])));
+        more = more || mx[n] > m[n] + SLACK;
+    }
+    if (__any(more)) {
 #pragma unroll
-            for (int dt = 0; dt < 8; ++dt) st.o[n][dt] *= alpha;
+        for (int n = 0; n < N; ++n) {
+            const float mn = fmaxf(m[n], cross16_max(mx[n]));
+            const float alpha = mn == SQ_NEG_INF ? 1.0f : __builtin_amdgcn_exp2f(m[n] - mn);
+            m[n] = mn;
+            l[n] *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) o[n][dt] *= alpha;
         }
-        const float base = st.m[n] == SQ_NEG_INF ? 0.0f : st.m[n] - LIFT;
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const float base = m[n] == SQ_NEG_INF ? 0.0f : m[n] - LIFT;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float x = __builtin_amdgcn_exp2f(t[n][i] - base);
-            st.l[n] += x * inv[i];
-            p[n][i] = (_Float16)x;
+            const float e = __builtin_amdgcn_exp2f(x[n][i] - base);
+            l[n] += e * inv[i];
+            p[n][i] = (_Float16)e;
         }
     }
 }
@@ -119,55 +161,86 @@ __device__ __forceinline__ void fold_scores(Columns<TILES> &st, const float (&t)
 }  // namespace
 
 template <int TILES, bool WIDE>
-__global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a, int units, int grid)
+__global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see arguments() */, TreePlan plan)
 {
     typedef std::conditional_t<WIDE, unsigned long long, uint32_t> offset_t;
     constexpr bool Q_IN_LDS = TILES == 4;
-    constexpr int Q_BYTES = Q_IN_LDS ? 4 * 64 * D * 2 : 0;
-    // The queries (64 rows of 256 bytes for each wave that has its own, 16 bytes at place p of row r standing at p ^ (r & 15)) and, behind the
-    // keys, the waves' results of 16 rows.
-    __shared__ __align__(16) char s_mem[Q_BYTES > (int)sizeof(WaveOut) ? Q_BYTES : (int)sizeof(WaveOut)];
+    // The queries (64 rows of 256 bytes, 16 bytes at place p of row r standing at p ^ (r & 15)) and, behind the keys, two
+    // sums of results (likewise).
+    __shared__ __align__(16) char s_mem[2 * 16 * TILES * D * sizeof(float)];
     __shared__ __align__(16) TreeList<WIDE> s_list[4][2];
     __shared__ __align__(16) offset_t s_none[QT];           // where a wave reads ahead behind its last tile: the first row
-    __shared__ int s_delta[4][64];
     __shared__ int s_group[MAX_GROUPS];
     __shared__ int s_w[4], s_found[2];
-    __shared__ float s_ml[2][4][16];
+    __shared__ float s_ml[2][4][16 * TILES];
 
     const int wave = uniform(threadIdx.x >> 6), tid = threadIdx.x;
-    const int row_wave = wave % a.row_waves, key_wave = wave / a.row_waves, key_waves = 4 / a.row_waves;
     if (tid < QT) s_none[tid] = 0;
     __syncthreads();
-    // This workgroup's share: tiles [t0, t1), counted from unit ui's first less unit_start.
-    int share, per, t0, t1, ui, unit_start;
+    // This workgroup's share: [t0, t1) of the units' tiles, laid end to end with `ahead` more in front of each unit's for what it costs to
+    // begin one (a share that begins inside a unit pays as much); unit ui begins at unit_start.
+    int share, share0, per, t0, t1, ui, unit_start, ahead;   // share0 + t / per is who has tile t
     Unit u;
-    if (grid == 0) {
-        ui = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);       // (each XCD takes consecutive units)
-        if (ui >= units) return;
+    if (plan.splits > 0) {
+        // A workgroup per unit and part of it, without a look at the other units.
+        const TreeAttnArgs &a = arguments();
+        share = blockIdx.x;
+        ui = share / plan.splits;
         u = unit_of(a, ui, TILES);
-        if (u.total == 0) return;
-        share = ui;
-        per = t1 = u.total;
-        t0 = unit_start = 0;
+        per = max(4, (u.total + plan.splits - 1) / plan.splits);
+        share0 = ui * plan.splits;
+        t0 = (share - share0) * per;
+        t1 = min(u.total, t0 + per);
+        if (t0 >= t1) return;
+        unit_start = ahead = 0;
     } else {
-        const int each = (units + 255) / 256, i_lo = min(units, tid * each), i_hi = min(units, i_lo + each);
-        int mine = 0, all;
-        for (int i = i_lo; i < i_hi; ++i) mine += unit_of(a, i, TILES).total;
+        const TreeAttnArgs &a = arguments();
+        // Every thread counts up to four consecutive units, read side by side.
+        const int units = plan.units, each = (units + 255) / 256, i_lo = tid * each;
+        ahead = TREE_AHEAD;
+        int totals[TREE_SHARED_UNITS / 256], mine = 0, all;
+        {
+            Unit v[TREE_SHARED_UNITS / 256];
+            Counts c[TREE_SHARED_UNITS / 256];
+            v[0] = place_of(a, min(i_lo, units - 1));
+#pragma unroll
+            for (int k = 0; k < TREE_SHARED_UNITS / 256; ++k) {
+                if (k > 0) {                                // the unit behind it (the last one again where it ends)
+                    v[k] = v[k - 1];
+                    if (i_lo + k < units && ++v[k].block == a.blocks) {
+                        v[k].block = 0;
+                        if (++v[k].b == a.B) {
+                            v[k].b = 0;
+                            ++v[k].h;
+                        }
+                    }
+                }
+                c[k] = counts_of(a, v[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < TREE_SHARED_UNITS / 256; ++k) {
+                count(a, c[k], TILES, v[k]);
+                totals[k] = k < each && i_lo + k < units && v[k].total > 0 ? v[k].total + ahead : 0;
+                mine += totals[k];
+            }
+        }
         int before = block_exclusive(mine, tid, s_w, all);
-        const int shares = min(grid, (all + key_waves - 1) / key_waves), per_xcd = (shares + 7) / 8;      // (at least a tile for each wave)
+        const int shares = min(TREE_GRID, (all + 3) / 4), per_xcd = (shares + 7) / 8;      // (at least a tile for each wave)
         if (all == 0) return;
         per = (all + shares - 1) / shares;
-        share = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+        share = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);             // (each XCD takes consecutive shares)
         if ((int)(blockIdx.x >> 3) >= per_xcd || (long long)share * per >= all) return;
+        share0 = 0;
         t0 = share * per;
         t1 = min(all, t0 + per);
         if (before <= t0 && t0 < before + mine) {
             int i = i_lo;
-            for (;; ++i) {
-                const int n = unit_of(a, i, TILES).total;
-                if (t0 < before + n) break;
-                before += n;
-            }
+#pragma unroll
+            for (int k = 0; k + 1 < TREE_SHARED_UNITS / 256; ++k)
+                if (i == i_lo + k && t0 >= before + totals[k]) {
+                    before += totals[k];
+                    ++i;
+                }
             s_found[0] = i;
             s_found[1] = before;
         }
@@ -176,42 +249,49 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a, int u
         unit_start = uniform(s_found[1]);
         u = unit_of(a, ui, TILES);
     }
-
+    // (a share may end, or begin, in what stands in front of a unit's tiles)
+    int slot = 2 * share;                                   // of its first unit's partial result; one of a later unit comes behind it
     for (;;) {
         const int lane = thread_here() & 63, c16 = lane & 15, g4 = lane >> 4;
         const int b = uniform(u.b), h = uniform(u.h), n_drafts = uniform(u.n), tf = uniform(u.tf), tu = uniform(u.tu);
         const int nf = uniform(u.nf), nu = uniform(u.nu), total = uniform(u.total);
-        const size_t bh = (size_t)b * a.H + h;
-        const int lo = max(t0 - unit_start, 0), hi = min(t1 - unit_start, total);
-        const int row0 = u.block * unit_rows(a, TILES), end_row = n_drafts * a.G;      // rows from end_row on are nobody's
-        // The queries.
-        auto query = [&](int row) -> const h8 * {
-            const int t = row / a.G, g = row - t * a.G;
+        const size_t bh = (size_t)b * arguments().H + h;
+        const int lo = max(t0 - unit_start - ahead, 0), hi = min(t1 - unit_start - ahead, total);
+        if (lo >= hi) break;                                // (only of a last unit)
+        const int row0 = u.block * 16 * TILES, end_row = n_drafts * arguments().G;      // rows from end_row on are nobody's
+        const TreeAttnArgs &a = arguments();
+        // The queries, and what says which keys: read side by side.
+        auto query = [&](int row) {                         // of a row behind the last, the last row's
+            const int r = min(row, end_row - 1), t = r / a.G, g = r - t * a.G;
             return reinterpret_cast<const h8 *>(a.q + ((bh * a.G + g) * a.T + t) * D);
         };
+        const global<i2v> rg = uniform(reinterpret_cast<const i2v *>(a.ranges) + bh * a.C);
+        auto range_of = [&](int gi) { return rg[min(gi * GROUP + lane, a.C - 1)]; };   // as it stands in memory: see in_bounds
+        const bool has_fixed = lo < tf;
+        i2v near[4] = {};                                   // up to four groups of 64 ranges every wave has in registers
+        int nr = 0;
+        if (has_fixed) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) near[k] = range_of(k);
+            nr = a.n_ranges[bh];
+        }
         h8 q[Q_IN_LDS ? 1 : TILES][4];
         h8 *const sq_ = reinterpret_cast<h8 *>(s_mem);
         if constexpr (Q_IN_LDS) {
-            for (int i = tid; i < 64 * a.row_waves * 16; i += 256) {
-                const int r = i >> 4, p = i & 15;
-                h8 v = {};
-                if (row0 + r < end_row) v = query(row0 + r)[p];
-                sq_[r * 16 + (p ^ (r & 15))] = v;
-            }
+            h8 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = query(row0 + k * 16 + (tid >> 4))[tid & 15];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sq_[(k * 16 + (tid >> 4)) * 16 + ((tid & 15) ^ (tid >> 4))] = v[k];
             __syncthreads();
         } else {
 #pragma unroll
-            for (int n = 0; n < TILES; ++n) {
-                const int row = row0 + (row_wave * TILES + n) * 16 + c16;
+            for (int n = 0; n < TILES; ++n)
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const h8 zero = {};
-                    q[n][s] = row < end_row ? query(row)[4 * g4 + s] : zero;
-                }
-            }
+                for (int s = 0; s < 4; ++s) q[n][s] = query(row0 + n * 16 + c16)[4 * g4 + s];
         }
         auto q_of = [&](int n, int s) {
-            if constexpr (Q_IN_LDS) return sq_[((row_wave * 4 + n) * 16 + c16) * 16 + ((4 * g4 + s) ^ c16)];
+            if constexpr (Q_IN_LDS) return sq_[(n * 16 + c16) * 16 + ((4 * g4 + s) ^ c16)];
             else return q[n][s];
         };
         Columns<TILES> st;
@@ -223,16 +303,14 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a, int u
             for (int dt = 0; dt < 8; ++dt) st.o[n][dt] = f4{0.f, 0.f, 0.f, 0.f};
         }
 
-        // The head's ranges in groups of 64: how many keys lie before each group, for a wave to find its first.
-        const global<i2v> rg = uniform(reinterpret_cast<const i2v *>(a.ranges) + bh * a.C);
-        auto range_of = [&](int gi) { return rg[min(gi * GROUP + lane, a.C - 1)]; };   // as it stands in memory: see in_bounds
-        const bool has_fixed = lo < tf;
-        const int nr = uniform(has_fixed ? min(max(a.n_ranges[bh], 0), a.C) : 0), groups = (nr + GROUP - 1) / GROUP;
+        // How many keys lie before each group of ranges, for a wave to find its first.
+        nr = uniform(min(max(nr, 0), a.C));
+        const int groups = (nr + GROUP - 1) / GROUP;
         auto in_bounds = [&](i2v e, int gi) {               // a lane's range of a group; (0, 0) behind the last
             const bool ok = gi * GROUP + lane < nr;
             return i2v{min(max(e.x, -MAX_L), MAX_L), ok ? min(max(e.y, 0), a.L) : 0};
         };
-        if (has_fixed) {
+        if (groups > 4) {
             for (int gi = wave; gi < groups; gi += 4) {
                 // (counts that sum to more than a head can have are cut, far from overflow)
                 const int n = min(wave_sum_i(in_bounds(range_of(gi), gi).y), MAX_L);
@@ -242,12 +320,13 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a, int u
         }
 
         // This wave's part of the tiles.
-        const int w0 = lo + (int)((long long)(hi - lo) * key_wave / key_waves), w1 = lo + (int)((long long)(hi - lo) * (key_wave + 1) / key_waves);
+        const int w0 = lo + (int)((long long)(hi - lo) * wave / 4), w1 = lo + (int)((long long)(hi - lo) * (wave + 1) / 4);
         int phase = 0;
 #pragma clang loop unroll(disable)
         for (; phase < 2; ++phase) {
             asm volatile("" : "+s"(phase));                 // (one copy of the loop below for both)
             const bool fixed = phase == 0;
+            const TreeAttnArgs &a = arguments();
             const int f0 = fixed ? w0 : max(w0 - tf, 0);    // first tile of the phase, and how many
             const int tiles = (fixed ? min(w1, tf) : min(w1 - tf, tu)) - f0;
             if (tiles <= 0) continue;
@@ -261,25 +340,43 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a, int u
             int gi = 0, first = 0, ends = 0;
             i2v e = {0, 0}, e_next = {0, 0};                 // user: e.x is the page of position p + lane, read ahead
             if (fixed) {
-                int sum[MAX_GROUPS / 64], at = 0, start = 0;
+                int start = 0, listed = 0;                  // keys before group gi, keys of all groups
+                if (groups <= 4) {
+                    e = in_bounds(near[0], 0);
 #pragma unroll
-                for (int i = 0; i < MAX_GROUPS / 64; ++i) {
-                    sum[i] = 4 * lane + i < groups ? s_group[4 * lane + i] : 0;
-                    at += sum[i];
-                }
-                const int inc = wave_inclusive_scan(at, lane), listed = __builtin_amdgcn_readlane(inc, 63);
-                at = inc - at;
-                int here = 0;                               // groups that end at or before p
+                    for (int k = 0; k < 4; ++k) {
+                        listed += wave_sum_i(in_bounds(near[k], k).y);
+                        if (k + 1 < groups && listed <= p) {
+                            gi = k + 1;
+                            start = listed;
+                            e = in_bounds(near[k < 3 ? k + 1 : 3], k + 1);
+                        }
+                    }
+                    listed = uniform(listed);
+                } else {
+                    int sum[MAX_GROUPS / 64], at = 0;
 #pragma unroll
-                for (int i = 0; i < MAX_GROUPS / 64; ++i) {
-                    const bool passed = 4 * lane + i < groups && at + sum[i] <= p;
-                    here += __popcll(__ballot(passed));
-                    start += passed ? sum[i] : 0;
-                    at += sum[i];
+                    for (int i = 0; i < MAX_GROUPS / 64; ++i) {
+                        sum[i] = 4 * lane + i < groups ? s_group[4 * lane + i] : 0;
+                        at += sum[i];
+                    }
+                    const int inc = wave_inclusive_scan(at, lane);
+                    listed = __builtin_amdgcn_readlane(inc, 63);
+                    at = inc - at;
+                    int here = 0;                           // groups that end at or before p
+#pragma unroll
+                    for (int i = 0; i < MAX_GROUPS / 64; ++i) {
+                        const bool passed = 4 * lane + i < groups && at + sum[i] <= p;
+                        here += __popcll(__ballot(passed));
+                        start += passed ? sum[i] : 0;
+                        at += sum[i];
+                    }
+                    gi = min(here, groups - 1);
+                    start = wave_sum_i(start);
+                    e = in_bounds(range_of(uniform(gi)), gi);
                 }
-                gi = uniform(max(min(here, groups - 1), 0));
-                start = uniform(wave_sum_i(start));
-                e = in_bounds(range_of(gi), gi);
+                gi = uniform(gi);
+                start = uniform(start);
                 end = min(nf, listed);
                 e_next = range_of(gi + 1);
                 const int c = wave_inclusive_scan(e.y, lane);
@@ -298,11 +395,20 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a, int u
                 offset_t at = 0;
                 int sc = 0;
                 if (fixed) {
-                    s_delta[wave][lane] = SENTINEL;
-                    wave_lds_sync();
+                    // The ranges that reach into these positions, one after the other.
+                    bool found = false;
+                    int key = 0;
                     for (;;) {
-                        const int from = max(first, p), to = min(first + e.y, p + 64);
-                        if (from < to) s_delta[wave][from - p] = e.x - first;
+                        unsigned long long here = __ballot(first < p + 64 && first + e.y > p && e.y > 0);
+                        while (here != 0ull) {
+                            const int r = __ffsll((long long)here) - 1;
+                            here &= here - 1;
+                            const int i = p + lane - __builtin_amdgcn_readlane(first, r);
+                            if (i >= 0 && i < __builtin_amdgcn_readlane(e.y, r)) {
+                                key = __builtin_amdgcn_readlane(e.x, r) + i;
+                                found = true;
+                            }
+                        }
                         if (ends >= p + 64 || gi + 1 >= groups) break;
                         gi = uniform(gi + 1);
                         e = in_bounds(e_next, gi);
@@ -311,12 +417,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a, int u
                         first = ends + c - e.y;
                         ends = uniform(min(ends + __builtin_amdgcn_readlane(c, 63), MAX_L + MAX_L));
                     }
-                    wave_lds_sync();
-                    const unsigned long long marks = __ballot(s_delta[wave][lane] != SENTINEL) & (~0ull >> (63 - lane));
-                    ok = ok && marks != 0ull;
+                    ok = ok && found;
                     if (ok) {
-                        const int d = s_delta[wave][63 - __clzll((long long)marks)];
-                        const int key = min(max(p + lane + d, 0), a.L - 1);
+                        key = min(max(key, 0), a.L - 1);
                         at = (offset_t)key * D;
                         sc = h * a.sblocks + (key >> 6);
                     }
@@ -342,8 +445,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a, int u
             };
             auto list_scales = [&](int buf) {
                 s_list[wave][buf].mul[lane] = ks * a.scale;
-                s_list[wave][buf].add[lane] = log2f(vs);
-                s_list[wave][buf].inv[lane] = 1.0f / vs;
+                s_list[wave][buf].add[lane] = __builtin_amdgcn_logf(vs);
+                s_list[wave][buf].inv[lane] = __builtin_amdgcn_rcpf(vs);
                 wave_lds_sync();
             };
             u4v k[2][2];                                    // keys c16 and 16 + c16, dimensions 32 g4 ..
@@ -387,6 +490,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a, int u
                         acc[n][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qv, acc[n][0], 0, 0, 0);
                         acc[n][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qv, acc[n][1], 0, 0, 0);
                     }
+                    if (TILES == 4) __builtin_amdgcn_sched_barrier(0);      // (the queries of one step in registers at a time)
                 }
                 load_k(t + 1);                              // (as soon as the scores have used this tile's)
                 float x[TILES][8], inv[8];
@@ -423,7 +527,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a, int u
                         }
                 }
                 h8 pr[TILES];
-                fold_scores(st, x, inv, pr);
+                fold_scores<TILES>(st.m, st.l, st.o, x, inv, pr);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     transpose4(w[i][0], w[i][1], w[i][2], w[i][3]);
@@ -440,83 +544,88 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a, int u
             }
         }
 
-        // The drafts: f16 rows, read as they are needed.
-        if (w1 > tf + tu && a.Kd) {
-            const _Float16 *Kd = a.Kd + bh * a.T * D, *Vd = a.Vd + bh * a.T * D;
+        // The drafts: f16 rows.
+        const int d0 = max(w0 - tf - tu, 0), d1 = w1 - tf - tu;             // tiles of theirs
+        if (d0 < d1 && arguments().Kd) {
+            const TreeAttnArgs &a = arguments();
+            typedef global<char> bytes;
+            const bytes Kd = (bytes)uniform(a.Kd + bh * a.T * D), Vd = (bytes)uniform(a.Vd + bh * a.T * D);
             const int words = (a.T + 31) / 32;
             int draft[TILES];                               // of the lane's columns
 #pragma unroll
-            for (int n = 0; n < TILES; ++n) draft[n] = min(row0 + (row_wave * TILES + n) * 16 + c16, end_row - 1) / a.G;
-            for (int t = max(w0 - tf - tu, 0); t < w1 - tf - tu; ++t) {
+            for (int n = 0; n < TILES; ++n) draft[n] = min(row0 + n * 16 + c16, end_row - 1) / a.G;
+            auto row_at = [&](int key) { return (uint32_t)min(key, n_drafts - 1) * (uint32_t)(D * sizeof(_Float16)); };
+            h8 k[2][4], v[8];
+            auto load_k = [&](int t) {                      // (behind the last tile the last draft, again and again)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t at = row_at(t * QT + 16 * j + c16) + 64 * g4;
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) k[j][s] = *reinterpret_cast<global<h8>>(Kd + at + 16 * s);
+                }
+            };
+            bool strange = false;
+            load_k(d0);
+#pragma clang loop unroll(disable)
+            for (int t = d0; t < d1; ++t) {
                 const int key0 = t * QT;
-                auto row_at = [&](int key) { return (size_t)min(key0 + key, n_drafts - 1) * D; };
-                f4 acc[TILES][2];
 #pragma unroll
-                for (int n = 0; n < TILES; ++n) acc[n][0] = acc[n][1] = f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const h8 k0 = *reinterpret_cast<const h8 *>(Kd + row_at(c16) + 32 * g4 + 8 * s);
-                    const h8 k1 = *reinterpret_cast<const h8 *>(Kd + row_at(16 + c16) + 32 * g4 + 8 * s);
-#pragma unroll
-                    for (int n = 0; n < TILES; ++n) {
-                        const h8 qv = q_of(n, s);
-                        acc[n][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qv, acc[n][0], 0, 0, 0);
-                        acc[n][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qv, acc[n][1], 0, 0, 0);
-                    }
-                }
-                h8 v[8];
-                uint32_t odd = 0;                           // bit 15 or 31: an infinity or NaN among the lane's values
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    v[i] = *reinterpret_cast<const h8 *>(Vd + row_at(4 * g4 + (i < 4 ? i : 12 + i)) + 8 * c16);
-                    const u4v bits = __builtin_bit_cast(u4v, v[i]);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) odd |= (bits[c] & 0x7fff7fffu) + 0x04000400u;
-                }
-                const bool strange = __any((odd & 0x80008000u) != 0u);
-                float x[TILES][8], inv[8];
-                uint32_t sees[TILES];
+                for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<global<h8>>(Vd + (row_at(key0 + 4 * g4 + (i < 4 ? i : 12 + i)) + 16 * c16));
                 const uint32_t there = n_drafts - key0 >= 32 ? ~0u : (1u << (n_drafts - key0)) - 1u;
+                float one[8];
 #pragma unroll
-                for (int n = 0; n < TILES; ++n) {
-                    const int own = draft[n] - key0;        // a chain: keys up to the draft itself
-                    sees[n] = a.mask ? a.mask[((size_t)b * a.T + draft[n]) * words + t] : own >= 31 ? ~0u : own < 0 ? 0u : (2u << own) - 1u;
-                    sees[n] &= there;
-                    const uint32_t mine = sees[n] >> (4 * g4);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[n][i] = mine >> (i < 4 ? i : 12 + i) & 1u ? acc[n][i >> 2][i & 3] * a.scale : SQ_NEG_INF;
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) inv[i] = 1.0f;
+                for (int i = 0; i < 8; ++i) one[i] = 1.0f;
                 h8 pr[TILES];
-                fold_scores(st, x, inv, pr);
-                if (__builtin_expect(strange, 0)) {
-                    // Infinities and NaN among the values reach the columns that see their draft, and no others: they are taken out of the
-                    // product and added one by one.
-                    for (int key = 0; key < 32; ++key) {
-                        const int from = (key & 15) >> 2, i = (key & 3) + (key >> 4) * 4;
+                // (two columns at a time, which leaves registers for the tile of values that is on its way)
+                constexpr int PAIR = TILES < 2 ? TILES : 2;
 #pragma unroll
-                        for (int n = 0; n < TILES; ++n) {
-                            float mine = 0.0f;
+                for (int n0 = 0; n0 < TILES; n0 += PAIR) {
+                    f4 acc[PAIR][2];
 #pragma unroll
-                            for (int c = 0; c < 8; ++c) mine = c == i ? (float)pr[n][c] : mine;
-                            const float pv = __shfl(mine, from * 16 + c16);
-                            if (sees[n] >> key & 1u) {
+                    for (int n = 0; n < PAIR; ++n) acc[n][0] = acc[n][1] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                                for (int c = 0; c < 4; ++c) {
-                                    const h8 z = *reinterpret_cast<const h8 *>(Vd + row_at(key) + 32 * g4 + 8 * c);
+                    for (int s = 0; s < 4; ++s) {
 #pragma unroll
-                                    for (int dt = 0; dt < 8; ++dt)
-                                        if (!((float)z[dt] - (float)z[dt] == 0.0f)) st.o[n][dt][c] += pv * (float)z[dt];
-                                }
-                            }
+                        for (int n = 0; n < PAIR; ++n) {
+                            const h8 qv = q_of(n0 + n, s);
+                            acc[n][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[0][s], qv, acc[n][0], 0, 0, 0);
+                            acc[n][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[1][s], qv, acc[n][1], 0, 0, 0);
                         }
                     }
+                    if (n0 + PAIR == TILES) load_k(t + 1);
+                    float x[PAIR][8];
+#pragma unroll
+                    for (int n = 0; n < PAIR; ++n) {
+                        const int d = draft[n0 + n], own = d - key0;        // a chain: keys up to the draft itself
+                        uint32_t sees = own >= 31 ? ~0u : own < 0 ? 0u : (2u << own) - 1u;
+                        if (a.mask) sees = a.mask[((size_t)b * a.T + d) * words + t];
+                        sees &= there;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[n][i] = acc[n][i >> 2][i & 3] * a.scale;
+                        if (!__all(sees == ~0u)) {
+                            const uint32_t mine = sees >> (4 * g4);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) x[n][i] = mine >> (i < 4 ? i : 12 + i) & 1u ? x[n][i] : SQ_NEG_INF;
+                        }
+                    }
+                    fold_scores<PAIR>(st.m + n0, st.l + n0, st.o + n0, x, one, pr + n0);
+                    if (TILES == 4) __builtin_amdgcn_sched_barrier(0);
+                }
+                uint32_t odd = 0;                           // bit 15 or 31: an infinity or NaN among the lane's values
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) odd |= (__builtin_bit_cast(u4v, v[i])[c] & 0x7fff7fffu) + 0x04000400u;
+                if (__builtin_expect(__any((odd & 0x80008000u) != 0u), 0)) {
+                    strange = true;
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
 #pragma unroll
-                        for (int c = 0; c < 8; ++c)
-                            if (!((float)v[i][c] - (float)v[i][c] == 0.0f)) v[i][c] = (_Float16)0.0f;
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t &w = reinterpret_cast<uint32_t *>(&v[i])[c];
+                            if ((w & 0x7c00u) == 0x7c00u) w &= 0xffff0000u;
+                            if ((w & 0x7c000000u) == 0x7c000000u) w &= 0xffffu;
+                        }
                 }
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) {
@@ -525,128 +634,177 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a, int u
                     for (int n = 0; n < TILES; ++n) st.o[n][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pr[n], st.o[n][dt], 0, 0, 0);
                 }
             }
+            if (__builtin_expect(strange, 0)) {
+                // Infinities and NaN among the values, which the products left out, reach the columns that see their draft, and no others.
+#pragma clang loop unroll(disable)
+                for (int key = d0 * QT; key < min(d1 * QT, n_drafts); ++key) {
+                    h8 z[4];
+                    bool any = false;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        z[c] = *reinterpret_cast<global<h8>>(Vd + (row_at(key) + 64 * g4) + 16 * c);
+#pragma unroll
+                        for (int dt = 0; dt < 8; ++dt) {
+                            const bool finite = (float)z[c][dt] - (float)z[c][dt] == 0.0f;
+                            any = any || !finite;
+                            if (finite) z[c][dt] = (_Float16)0.0f;
+                        }
+                    }
+                    if (!__any(any)) continue;
+#pragma unroll
+                    for (int n = 0; n < TILES; ++n) {
+                        bool seen = key <= draft[n];
+                        if (a.mask) seen = a.mask[((size_t)b * a.T + draft[n]) * words + (key >> 5)] >> (key & 31) & 1u;
+                        if (seen)
+#pragma unroll
+                            for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) st.o[n][dt][c] += (float)z[c][dt];
+                    }
+                }
+            }
         }
 
-        // The waves' results, 16 rows of each at a time; those of the same rows are joined.
-        __syncthreads();                                    // (the queries have been read)
-        WaveOut &out = *reinterpret_cast<WaveOut *>(s_mem);
+        // Results: the waves' are joined in two buffers, waves 0 and 1 writing and 2 and 3 adding; a lane has dimensions 32 g4 + 8 i .. + 7 of
+        // its columns, i = 0 .. 3.
+        const TreeAttnArgs &r = arguments();
         const bool whole = lo == 0 && hi == total;
-        const int slot = share + ui;
+        auto out = [&](int buffer, int row, int place) {    // four dimensions of a row
+            return reinterpret_cast<f4 *>(s_mem) + (buffer * 16 * TILES + row) * (D / 4) + (place ^ (row & 15));
+        };
 #pragma unroll
         for (int n = 0; n < TILES; ++n) {
             const float l = cross16_sum(st.l[n]);
             if (g4 == 0) {
-                s_ml[0][wave][c16] = st.m[n];
-                s_ml[1][wave][c16] = l;
+                s_ml[0][wave][n * 16 + c16] = st.m[n];
+                s_ml[1][wave][n * 16 + c16] = l;
             }
+        }
+        __syncthreads();                                    // (and the queries have been read)
+        auto largest = [&](int c) { return fmaxf(fmaxf(s_ml[0][0][c], s_ml[0][1][c]), fmaxf(s_ml[0][2][c], s_ml[0][3][c])); };
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float *dst = &out.o[wave][c16][32 * g4 + 8 * i];
-                *reinterpret_cast<f4 *>(dst) = f4{st.o[n][0][i], st.o[n][1][i], st.o[n][2][i], st.o[n][3][i]};
-                *reinterpret_cast<f4 *>(dst + 4) = f4{st.o[n][4][i], st.o[n][5][i], st.o[n][6][i], st.o[n][7][i]};
-            }
-            __syncthreads();
-            const int here = thread_here();
-            for (int i = here; i < a.row_waves * 16 * D; i += 256) {
-                const int d = i & 127, c = i >> 7 & 15, rw = i >> 11;
-                const int in_block = (rw * TILES + n) * 16 + c;
-                if (row0 + in_block >= end_row) continue;
-                float m = SQ_NEG_INF, ls = 0.0f, o = 0.0f;
-                for (int kw = 0; kw < key_waves; ++kw) m = fmaxf(m, s_ml[0][kw * a.row_waves + rw][c]);
-                const float mu = m == SQ_NEG_INF ? 0.0f : m;
-                for (int kw = 0; kw < key_waves; ++kw) {
-                    const int w = kw * a.row_waves + rw;
-                    const float f = __builtin_amdgcn_exp2f(s_ml[0][w][c] - mu);
-                    ls += f * s_ml[1][w][c];
-                    o += f * out.o[w][c][d];
+        for (int n = 0; n < TILES; ++n) {
+            const float m = largest(n * 16 + c16), f = __builtin_amdgcn_exp2f(st.m[n] - (m == SQ_NEG_INF ? 0.0f : m));
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) st.o[n][dt] *= f;
+        }
+        if (wave < 2) {
+#pragma unroll
+            for (int n = 0; n < TILES; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    *out(wave, n * 16 + c16, 8 * g4 + 2 * i) = f4{st.o[n][0][i], st.o[n][1][i], st.o[n][2][i], st.o[n][3][i]};
+                    *out(wave, n * 16 + c16, 8 * g4 + 2 * i + 1) = f4{st.o[n][4][i], st.o[n][5][i], st.o[n][6][i], st.o[n][7][i]};
                 }
-                if (whole) store_row(a, u, row0 + in_block, d, m, ls, o);
-                else store_partial(a.part + ((size_t)slot * unit_rows(a, TILES) + in_block) * PART_STRIDE, d, Joined{m, ls, o});
+        }
+        __syncthreads();
+        if (wave >= 2) {
+#pragma unroll
+            for (int n = 0; n < TILES; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    *out(wave - 2, n * 16 + c16, 8 * g4 + 2 * i) += f4{st.o[n][0][i], st.o[n][1][i], st.o[n][2][i], st.o[n][3][i]};
+                    *out(wave - 2, n * 16 + c16, 8 * g4 + 2 * i + 1) += f4{st.o[n][4][i], st.o[n][5][i], st.o[n][6][i], st.o[n][7][i]};
+                }
+        }
+        __syncthreads();
+#pragma clang loop unroll(disable)
+        for (int n = 0; n < TILES; ++n) {
+            const int here = thread_here(), row = n * 16 + (here >> 4), d = 8 * (here & 15);
+            if (row0 + row >= end_row) break;
+            const float m = largest(row), mu = m == SQ_NEG_INF ? 0.0f : m;
+            float ls = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) ls += __builtin_amdgcn_exp2f(s_ml[0][w][row] - mu) * s_ml[1][w][row];
+            const f4 x = *out(0, row, d / 4) + *out(1, row, d / 4), y = *out(0, row, d / 4 + 1) + *out(1, row, d / 4 + 1);
+            if (whole) store_dims(r, u, row0 + row, d, m, ls, x, y);
+            else {
+                float *p = r.part + ((size_t)slot * 16 * TILES + row) * PART_STRIDE;
+                *reinterpret_cast<f4 *>(p + 4 + d) = x;
+                *reinterpret_cast<f4 *>(p + 8 + d) = y;
+                if (d == 0) *reinterpret_cast<float2 *>(p) = make_float2(m, ls);
             }
-            __syncthreads();
         }
-        if (grid == 0) return;
+        __syncthreads();
+        if (plan.splits == 1) return;
         if (tid == 0 && lo == 0) {
-            const int last = (unit_start + total - 1) / per;
-            a.info[ui] = int2{slot, whole ? 0 : last - share + 1};
+            const int last = share0 + (unit_start + ahead + total - 1) / per;
+            r.info[ui] = int2{slot, whole ? 0 : last - share + 1};      // (its other partial results are the first of their shares)
         }
-        unit_start += total;
+        unit_start += ahead + total;
         if (unit_start >= t1) break;
-        do u = unit_of(a, ++ui, TILES);
+        slot = 2 * share + 1;
+        do u = unit_of(r, ++ui, TILES);
         while (u.total == 0);
     }
 }
 
-// Rows of blocks that several workgroups took, a wave each: two halves fold every other partial result, a lane four dimensions.
+// Rows of blocks that several workgroups took, a wave each: four groups of 16 lanes fold every fourth partial result, a lane eight
+// dimensions.
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeAttnArgs a, int tiles)
 {
-    const int rows = unit_rows(a, tiles), at = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, quad = lane & 31;
+    const int rows = 16 * tiles, at = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, grp = lane >> 4, d = 8 * (lane & 15);
     const int ui = at / rows, in_block = at - ui * rows;
     if (ui >= a.B * a.H * a.blocks) return;
+    const int2 info = a.info[ui];
     const Unit u = unit_of(a, ui, tiles);
     const int row = u.block * rows + in_block;
-    if (row >= u.n * a.G) return;
-    const int2 info = a.info[ui];
-    if (info.y == 0) return;
+    if (row >= u.n * a.G || info.y == 0) return;            // (nobody wrote the numbers of a unit without rows)
     float M = SQ_NEG_INF, ls = 0.0f;
-    f4 os = {0.f, 0.f, 0.f, 0.f};
-    auto fold = [&](float pm, float pl, f4 po) {
+    f4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+    auto fold = [&](float pm, float pl, f4 px, f4 py) {
         const float mn = fmaxf(M, pm), mu = mn == SQ_NEG_INF ? 0.0f : mn;
         const float fa = exp2f(M - mu), fb = exp2f(pm - mu);
         ls = ls * fa + pl * fb;
-        os = os * fa + po * fb;
+        x = x * fa + px * fb;
+        y = y * fa + py * fb;
         M = mn;
     };
-    auto part = [&](int i) { return a.part + ((size_t)(info.x + i) * rows + in_block) * PART_STRIDE; };
-    int i = half;
-    for (; i + 2 < info.y; i += 4) {
-        const float *p = part(i), *q = part(i + 2);
-        const float2 a0 = *reinterpret_cast<const float2 *>(p), a1 = *reinterpret_cast<const float2 *>(q);
-        const f4 o0 = *reinterpret_cast<const f4 *>(p + 4 + 4 * quad), o1 = *reinterpret_cast<const f4 *>(q + 4 + 4 * quad);
-        fold(a0.x, a0.y, o0);
-        fold(a1.x, a1.y, o1);
-    }
-    if (i < info.y) {
+    auto part = [&](int i) { return a.part + ((size_t)(i == 0 ? info.x : 2 * ((info.x >> 1) + i)) * rows + in_block) * PART_STRIDE; };
+    for (int i = grp; i < info.y; i += 4) {
         const float *p = part(i);
-        fold(p[0], p[1], *reinterpret_cast<const f4 *>(p + 4 + 4 * quad));
+        const float2 ml = *reinterpret_cast<const float2 *>(p);
+        fold(ml.x, ml.y, *reinterpret_cast<const f4 *>(p + 4 + d), *reinterpret_cast<const f4 *>(p + 8 + d));
     }
-    const float m2 = __shfl_xor(M, 32), l2 = __shfl_xor(ls, 32);
-    f4 o2;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) o2[c] = __shfl_xor(os[c], 32);
-    if (half) return;
-    fold(m2, l2, o2);
+    for (int k = 16; k <= 32; k <<= 1) {
+        const float pm = __shfl_xor(M, k), pl = __shfl_xor(ls, k);
+        f4 px, py;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) store_row(a, u, row, 4 * quad + c, M, ls, os[c]);
+        for (int c = 0; c < 4; ++c) {
+            px[c] = __shfl_xor(x[c], k);
+            py[c] = __shfl_xor(y[c], k);
+        }
+        fold(pm, pl, px, py);
+    }
+    if (grp == 0) store_dims(a, u, row, d, M, ls, x, y);
 }
 
-TreePlan tree_plan(int B, int H, int rows)
+TreePlan tree_plan(int B, int H, int rows, long long keys)
 {
     TreePlan p{};
     p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    p.row_waves = rows <= 64 ? 1 : rows <= 128 ? 2 : 4;
-    const int block = 16 * p.tiles * p.row_waves;
-    p.blocks = (rows + block - 1) / block;
-    p.units = (long long)B * H * p.blocks;
-    p.grid = p.units < TREE_GRID ? TREE_GRID : 0;
-    p.parts = p.grid ? (size_t)(TREE_GRID + p.units) * block : 0;
+    p.blocks = (rows + 16 * p.tiles - 1) / (16 * p.tiles);
+    const long long units = (long long)B * H * p.blocks, most = (keys + QT - 1) / QT + 3;      // tiles: of three sources
+    p.units = (int)std::min(units, 0x7fffffffll);
+    p.splits = units > TREE_SHARED_UNITS ? 1 : units * ((most + 3) / 4) <= TREE_GRID ? (int)((most + 3) / 4) : 0;
+    p.grid = p.splits ? (long long)p.units * p.splits : TREE_GRID;
     return p;
 }
 
 hipError_t launch_tree_attn(TreeAttnArgs a, hipStream_t s)
 {
-    const TreePlan p = tree_plan(a.B, a.H, a.G * a.T);
+    const long long keys = (a.ranges ? a.L : 0) + (a.seq_len ? (long long)a.max_pages << a.p_log : 0) + (a.Kd ? a.T : 0);
+    const TreePlan p = tree_plan(a.B, a.H, a.G * a.T, keys);
     const bool wide = ((size_t)a.n_pages * a.H << a.p_log) * D > (1ull << 32);
-    a.row_waves = p.row_waves;
     a.blocks = p.blocks;
-    const int units = (int)p.units, grid = p.grid ? p.grid : (units + 7) / 8 * 8;
     auto *kernel = p.tiles == 1 ? (wide ? tree_attn_kernel<1, true> : tree_attn_kernel<1, false>)
                    : p.tiles == 2 ? (wide ? tree_attn_kernel<2, true> : tree_attn_kernel<2, false>)
                                   : (wide ? tree_attn_kernel<4, true> : tree_attn_kernel<4, false>);
-    hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, a, units, p.grid);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)p.grid), dim3(256), 0, s, a, p);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !p.grid) return e;
-    const long long rows = p.units * 16 * p.tiles * p.row_waves;
+    if (e != hipSuccess || p.splits == 1) return e;
+    const long long rows = (long long)p.units * 16 * p.tiles;
     hipLaunchKernelGGL(tree_merge_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p.tiles);
     return hipGetLastError();
 }

@@ -59,7 +59,7 @@ def attend(q, keys, scale):
     - the score in base 2 plus the value's scale's logarithm is rounded once, the difference to the maximum once: 2^-23 of its size, and
       that logarithm is off by 2^-22 of itself (a function of the GPU);
     - so a probability is off by d = the sum of these times ln 2 of itself, the exponential by 2^-22 more, and where it multiplies a
-      value by 2^-11 (f16), or 2^-39 of the largest of its row if that is more (f16's subnormals, p up to 2^14);
+      value by 2^-11 (f16), or 2^-33 of the largest of its row if that is more (f16's subnormals end at 2^-25, the largest is 2^8 or more);
     - fp32 sums of n terms: n 2^-24 of the sum of their magnitudes.
     """
     rows = len(q)
@@ -85,7 +85,7 @@ def attend(q, keys, scale):
             size = np.abs(x) / np.log(2) + np.abs(np.log2(vs))
             d = (np.abs(kk) @ np.abs(q[r]) * scale * 132 * 2.0 ** -24 + np.log(2) * (size + size.max()) * 2.0 ** -22 + 2.0 ** -21).max()
             weight = w * vs                                       # what is largest decides where f16 ends
-            tail = 2.0 ** -39 * weight.max() / vs
+            tail = 2.0 ** -33 * weight.max() / vs
             mean = w @ np.abs(vv)
             off[r] = mean * (2 * d + 2.0 ** -11 + (n + 64) * 2.0 ** -23) + tail @ np.abs(vv)
             off[r] += np.abs(out[r]) * 2.0 ** -11 + 2.0 ** -25     # the output's own rounding

@@ -294,9 +294,14 @@ def test_many_ranges(C, keep):
     p.run()
 
 
-@pytest.mark.parametrize("B,H,T", [(16, 32, 2), (40, 16, 1), (9, 60, 17)])
-def test_a_workgroup_per_block(B, H, T):
+@pytest.mark.parametrize("B,H,T", [(16, 32, 2), (40, 16, 1), (9, 60, 17), (33, 64, 1), (19, 111, 3)])
+def test_many_sequences_and_heads(B, H, T):
+    """Up to 2048 blocks in shares, more of them with a workgroup each."""
     Problem(B, B, H, 2, T, L=200, C=9, user=30, ragged=True).run()
+
+
+def test_long_rows_with_a_workgroup_per_block():
+    Problem(22, 2, 17, 16, 300, L=150, C=9, user=40, mask=None, ragged=True).run()   # 2 x 17 x 75 blocks
 
 
 def test_more_blocks_than_threads():

@@ -674,7 +674,7 @@ int sq_tree_prepare(const sq_shape_t *shape, const int32_t *parents, const int32
  *      queries see the context and the cache only.
  *      tree_mask u32 [B,T,ceil(T/32)]: draft t sees draft j if bit j of row t is set (any mask: it need be no tree, and a row may be
  *      empty); NULL: a chain, draft t sees drafts 0 .. t -- a prompt behind the context and the cache, of any length.  Bits from n_drafts[b] on
- *      are not looked at.  It must be NULL where K_draft is.
+ *      are not looked at.  It must be NULL where K_draft is, and T at most 32768 where it is not.
  *      One of the three sources at least.  All scales must be positive and normal, finite, and leave the scores in fp32's range.
  *      Input outside this contract never faults and is not reported: at most C ranges are used, entries with count <= 0 are skipped, nothing
  *      outside [0, L) is read, a page that is none has no keys; which keys such a row then attends to is not specified.

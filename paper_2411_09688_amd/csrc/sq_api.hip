@@ -2145,7 +2145,7 @@ int sq_tree_attn_q8(const sq_shape_t *sh, int32_t T, const void *q, const void *
     const long long keys = (ranges ? sh->L : 0) + (cache ? (long long)cache->max_pages * cache->page_tokens : 0) + (K_draft ? T : 0);
     const sq::TreePlan plan = sq::tree_plan(sh->B, sh->H, sh->Lq, keys);
     if ((long long)sh->H * sh->L > 0x7fffffffll || (long long)sh->B * sh->H * sh->Lq > 0x3fffffffll || plan.units > 0x7fffffffll / (keys / 32 + 4 + sq::TREE_AHEAD) ||
-        T > sq::MAX_L)
+        T > sq::MAX_L || (tree_mask && T > sq::MAX_MASKED))
         return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", __func__);
     const size_t B = sh->B, H = sh->H, blocks = (sh->L + sq::KV_BLOCK - 1) / sq::KV_BLOCK, rows = B * H * sh->Lq, drafts = B * H * T;
     Extent x[20] = {{"out", out, rows * sq::D * 2, true},

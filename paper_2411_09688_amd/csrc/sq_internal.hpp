@@ -488,6 +488,7 @@ hipError_t launch_cache_read(ReadArgs a, int B, hipStream_t s);
 constexpr int TREE_GRID = 512;     // workgroups that share the keys of a call
 constexpr int TREE_SHARED_UNITS = 1024;   // blocks of rows up to which they do: each workgroup counts the tiles of all blocks
 constexpr int TREE_AHEAD = 12;     // tiles of 32 keys that take as long as beginning and ending a block
+constexpr int MAX_MASKED = 32768;  // drafts with a mask: offsets into a sequence's have 32 bits
 struct TreeAttnArgs {
     const _Float16 *q;             // [B, H, G, T, D]
     const uint8_t *K8, *V8;

@@ -167,11 +167,13 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
     constexpr bool Q_IN_LDS = TILES == 4;
     // The queries (64 rows of 256 bytes, 16 bytes at place p of row r standing at p ^ (r & 15)) and, behind the keys, two
     // sums of results (likewise).
-    __shared__ __align__(16) char s_mem[2 * 16 * TILES * D * sizeof(float)];
+    // Between them, behind the queries, stands a tile of the drafts' values for each wave.
+    constexpr int V_AT = Q_IN_LDS ? 64 * D * 2 : 0, V_TILE = QT * D * 2, RESULTS = 2 * 16 * TILES * D * sizeof(float);
+    __shared__ __align__(16) char s_mem[RESULTS > V_AT + 4 * V_TILE ? RESULTS : V_AT + 4 * V_TILE];
     __shared__ __align__(16) TreeList<WIDE> s_list[4][2];
     __shared__ __align__(16) offset_t s_none[QT];           // where a wave reads ahead behind its last tile: the first row
     __shared__ int s_group[MAX_GROUPS];
-    __shared__ int s_w[4], s_found[2];
+    __shared__ int s_w[4], s_found[5];
     __shared__ float s_ml[2][4][16 * TILES];
 
     const int wave = uniform(threadIdx.x >> 6), tid = threadIdx.x;
@@ -184,7 +186,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
     if (plan.splits > 0) {
         // A workgroup per unit and part of it, without a look at the other units.
         const TreeAttnArgs &a = arguments();
-        share = blockIdx.x;
+        // (the last units first: of a chain those with the most drafts to see)
+        share = gridDim.x - 1 - blockIdx.x;
         ui = share / plan.splits;
         u = unit_of(a, ui, TILES);
         per = max(4, (u.total + plan.splits - 1) / plan.splits);
@@ -199,9 +202,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
         const int units = plan.units, each = (units + 255) / 256, i_lo = tid * each;
         ahead = TREE_AHEAD;
         int totals[TREE_SHARED_UNITS / 256], mine = 0, all;
+        Counts c[TREE_SHARED_UNITS / 256];
         {
             Unit v[TREE_SHARED_UNITS / 256];
-            Counts c[TREE_SHARED_UNITS / 256];
             v[0] = place_of(a, min(i_lo, units - 1));
 #pragma unroll
             for (int k = 0; k < TREE_SHARED_UNITS / 256; ++k) {
@@ -235,19 +238,25 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
         t1 = min(all, t0 + per);
         if (before <= t0 && t0 < before + mine) {
             int i = i_lo;
+            Counts found = c[0];
 #pragma unroll
             for (int k = 0; k + 1 < TREE_SHARED_UNITS / 256; ++k)
                 if (i == i_lo + k && t0 >= before + totals[k]) {
                     before += totals[k];
+                    found = c[k + 1];
                     ++i;
                 }
             s_found[0] = i;
             s_found[1] = before;
+            s_found[2] = found.nf;
+            s_found[3] = found.nu;
+            s_found[4] = found.n;
         }
         __syncthreads();
         ui = uniform(s_found[0]);
         unit_start = uniform(s_found[1]);
-        u = unit_of(a, ui, TILES);
+        u = place_of(a, ui);
+        count(a, Counts{s_found[2], s_found[3], s_found[4]}, TILES, u);
     }
     // (a share may end, or begin, in what stands in front of a unit's tiles)
     int slot = 2 * share;                                   // of its first unit's partial result; one of a later unit comes behind it
@@ -319,8 +328,12 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
             __syncthreads();
         }
 
-        // This wave's part of the tiles.
-        const int w0 = lo + (int)((long long)(hi - lo) * wave / 4), w1 = lo + (int)((long long)(hi - lo) * (wave + 1) / 4);
+        // This wave's part of the tiles: a quarter of the keys in 8 bits, and of the drafts, from the other end, so that what is left over of
+        // the one goes to other waves than of the other.
+        const int in8 = tf + tu, lo8 = min(lo, in8), n8 = min(hi, in8) - lo8, lod = max(lo - in8, 0), nd = max(hi - in8, 0) - lod;
+        auto quarter = [](int n, int i) { return (int)((long long)n * i / 4); };
+        const int w0 = lo8 + quarter(n8, wave), w1 = lo8 + quarter(n8, wave + 1);
+        const int d0 = lod + quarter(nd, 3 - wave), d1 = lod + quarter(nd, 4 - wave);
         int phase = 0;
 #pragma clang loop unroll(disable)
         for (; phase < 2; ++phase) {
@@ -328,17 +341,19 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
             const bool fixed = phase == 0;
             const TreeAttnArgs &a = arguments();
             const int f0 = fixed ? w0 : max(w0 - tf, 0);    // first tile of the phase, and how many
-            const int tiles = (fixed ? min(w1, tf) : min(w1 - tf, tu)) - f0;
+            const int tiles = (fixed ? min(w1, tf) : w1 - tf) - f0;
             if (tiles <= 0) continue;
             const size_t head = fixed ? (size_t)h * a.L * D : 0;
             const global<uint8_t> Kb = uniform((fixed ? a.K8 : a.cK) + head), Vb = uniform((fixed ? a.V8 : a.cV) + head);
             const global<float> kscale = uniform(fixed ? a.ks : a.cks), vscale = uniform(fixed ? a.vs : a.cvs);
-            const global<int32_t> pages = uniform(a.page_table + (size_t)b * a.max_pages);
             int p = f0 * QT;                                // the next position to list
             int end;                                        // where the keys end
-            // ranges in hand: group gi, its lanes' first positions, where it ends; the group behind it is on its way
+            // ranges in hand: group gi, its lanes' first positions, where it ends
             int gi = 0, first = 0, ends = 0;
-            i2v e = {0, 0}, e_next = {0, 0};                 // user: e.x is the page of position p + lane, read ahead
+            i2v e = {0, 0};
+            // the user's pages: that of position p + lane, read ahead (of kept keys some number that is not used)
+            const global<int32_t> ids = fixed ? (global<int32_t>)rg : uniform(a.page_table + (size_t)b * a.max_pages);
+            int id = 0;
             if (fixed) {
                 int start = 0, listed = 0;                  // keys before group gi, keys of all groups
                 if (groups <= 4) {
@@ -378,105 +393,86 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                 gi = uniform(gi);
                 start = uniform(start);
                 end = min(nf, listed);
-                e_next = range_of(gi + 1);
                 const int c = wave_inclusive_scan(e.y, lane);
                 first = start + c - e.y;
                 ends = uniform(start + __builtin_amdgcn_readlane(c, 63));
             } else {
                 end = nu;
-                e.x = pages[min(p + lane, end - 1) >> a.p_log];
+                id = ids[min(p + lane, end - 1) >> a.p_log];
             }
 
-            float ks = 0.0f, vs = 1.0f;
-            unsigned long long seen = 0ull, seen_next = 0ull;   // slots with a key, of the list in use and the next
+            // (The loop below reads memory in the same order in every round, without a branch around it: what is waited for is then counted
+            // exactly, and the tile ahead stays on its way.  With reads under conditions the compiler drained them all, twice a tile.)
+            float ks, vs;
+            unsigned long long seen, seen_next;             // slots with a key, of the list in use and the next
             // Lists positions p .. p + 63 and starts to read their scales.
             auto list = [&](int buf) {
                 bool ok = p + lane < end;
+                int key = 0, sc = 0;
                 offset_t at = 0;
-                int sc = 0;
                 if (fixed) {
                     // The ranges that reach into these positions, one after the other.
                     bool found = false;
-                    int key = 0;
                     for (;;) {
                         unsigned long long here = __ballot(first < p + 64 && first + e.y > p && e.y > 0);
                         while (here != 0ull) {
                             const int r = __ffsll((long long)here) - 1;
                             here &= here - 1;
                             const int i = p + lane - __builtin_amdgcn_readlane(first, r);
-                            if (i >= 0 && i < __builtin_amdgcn_readlane(e.y, r)) {
-                                key = __builtin_amdgcn_readlane(e.x, r) + i;
-                                found = true;
-                            }
+                            const bool in = i >= 0 && i < __builtin_amdgcn_readlane(e.y, r);
+                            key = in ? __builtin_amdgcn_readlane(e.x, r) + i : key;
+                            found = found || in;
                         }
                         if (ends >= p + 64 || gi + 1 >= groups) break;
                         gi = uniform(gi + 1);
-                        e = in_bounds(e_next, gi);
-                        e_next = range_of(gi + 1);
+                        e = in_bounds(range_of(gi), gi);
                         const int c = wave_inclusive_scan(e.y, lane);
                         first = ends + c - e.y;
                         ends = uniform(min(ends + __builtin_amdgcn_readlane(c, 63), MAX_L + MAX_L));
                     }
                     ok = ok && found;
-                    if (ok) {
-                        key = min(max(key, 0), a.L - 1);
-                        at = (offset_t)key * D;
-                        sc = h * a.sblocks + (key >> 6);
-                    }
+                    key = min(max(key, 0), a.L - 1);
+                    at = (offset_t)key * D;
+                    sc = h * a.sblocks + (key >> 6);
                 } else {
                     const int t = p + lane;
-                    ok = ok && e.x >= 0 && e.x < a.n_pages;
-                    if (ok) {
-                        sc = e.x * a.H + h;
-                        at = (((offset_t)sc << a.p_log) + (t & ((1 << a.p_log) - 1))) * D;
-                    }
-                    e.x = pages[min(t + 64, end - 1) >> a.p_log];
+                    ok = ok && id >= 0 && id < a.n_pages;
+                    sc = id * a.H + h;
+                    at = (((offset_t)sc << a.p_log) + (t & ((1 << a.p_log) - 1))) * D;
                 }
-                ks = 0.0f;
-                vs = 1.0f;
-                if (ok) {
-                    ks = kscale[sc];
-                    vs = vscale[sc];
-                }
+                at = ok ? at : 0;
+                sc = ok ? sc : 0;
+                ks = kscale[sc];
+                vs = vscale[sc];
+                id = ids[fixed ? 0 : max(min(p + 64 + lane, end - 1), 0) >> a.p_log];
                 s_list[wave][buf].at[lane] = at;
                 seen_next = __ballot(ok);
                 p += 64;
                 wave_lds_sync();
             };
             auto list_scales = [&](int buf) {
+                const float v = seen_next >> lane & 1u ? vs : 1.0f;         // (a slot without a key: not looked at, but for this)
                 s_list[wave][buf].mul[lane] = ks * a.scale;
-                s_list[wave][buf].add[lane] = __builtin_amdgcn_logf(vs);
-                s_list[wave][buf].inv[lane] = __builtin_amdgcn_rcpf(vs);
+                s_list[wave][buf].add[lane] = __builtin_amdgcn_logf(v);
+                s_list[wave][buf].inv[lane] = __builtin_amdgcn_rcpf(v);
                 wave_lds_sync();
             };
             u4v k[2][2];                                    // keys c16 and 16 + c16, dimensions 32 g4 ..
             u2v v[8];                                       // keys 4 g4 .. and 16 + 4 g4 .., dimensions 8 c16 ..
-            auto load_k = [&](int t) {
-                const auto *at = t < tiles ? s_list[wave][(t >> 1) & 1].at + (t & 1) * QT : s_none;
+            auto load_k = [&](const offset_t *at) {
                 const offset_t k0 = at[c16] + 32 * g4, k1 = at[16 + c16] + 32 * g4;
                 k[0][0] = *reinterpret_cast<global<u4v>>(Kb + k0);
                 k[0][1] = *reinterpret_cast<global<u4v>>(Kb + k0 + 16);
                 k[1][0] = *reinterpret_cast<global<u4v>>(Kb + k1);
                 k[1][1] = *reinterpret_cast<global<u4v>>(Kb + k1 + 16);
             };
-            auto load_v = [&](int t) {
-                const auto *at = (t < tiles ? s_list[wave][(t >> 1) & 1].at + (t & 1) * QT : s_none) + 4 * g4;
+            auto load_v = [&](const offset_t *at) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    v[i] = *reinterpret_cast<global<u2v>>(Vb + (offset_t)(at[(i < 4 ? 0 : 12) + i] + 8 * c16));
+                    v[i] = *reinterpret_cast<global<u2v>>(Vb + (offset_t)(at[4 * g4 + (i < 4 ? 0 : 12) + i] + 8 * c16));
             };
-
-            list(0);
-            load_k(0);
-            load_v(0);
-            list_scales(0);
-            for (int t = 0; t < tiles; ++t) {
-                const int buf = (t >> 1) & 1, slot = (t & 1) * QT;
-                const bool even = !(t & 1);
-                if (even) {
-                    seen = seen_next;
-                    if (t + 2 < tiles) list(buf ^ 1);
-                }
+            // Folds slots slot .. + 31 of list buf and reads the tile at `next` in their place.
+            auto tile = [&](int buf, int slot, const offset_t *next) {
                 f4 acc[TILES][2];
 #pragma unroll
                 for (int n = 0; n < TILES; ++n) acc[n][0] = acc[n][1] = f4{0.f, 0.f, 0.f, 0.f};
@@ -492,21 +488,19 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                     }
                     if (TILES == 4) __builtin_amdgcn_sched_barrier(0);      // (the queries of one step in registers at a time)
                 }
-                load_k(t + 1);                              // (as soon as the scores have used this tile's)
+                load_k(next);                               // (as soon as the scores have used this tile's)
                 float x[TILES][8], inv[8];
-                {
-                    const TreeList<WIDE> &ls = s_list[wave][buf];
+                const TreeList<WIDE> &ls = s_list[wave][buf];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int at = slot + 16 * j + 4 * g4;
-                        const f4 mul = *reinterpret_cast<const f4 *>(ls.mul + at), add = *reinterpret_cast<const f4 *>(ls.add + at),
-                                 iv = *reinterpret_cast<const f4 *>(ls.inv + at);
+                for (int j = 0; j < 2; ++j) {
+                    const int at = slot + 16 * j + 4 * g4;
+                    const f4 mul = *reinterpret_cast<const f4 *>(ls.mul + at), add = *reinterpret_cast<const f4 *>(ls.add + at),
+                             iv = *reinterpret_cast<const f4 *>(ls.inv + at);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            inv[4 * j + i] = iv[i];
+                    for (int i = 0; i < 4; ++i) {
+                        inv[4 * j + i] = iv[i];
 #pragma unroll
-                            for (int n = 0; n < TILES; ++n) x[n][4 * j + i] = fmaf(acc[n][j][i], mul[i], add[i]);
-                        }
+                        for (int n = 0; n < TILES; ++n) x[n][4 * j + i] = fmaf(acc[n][j][i], mul[i], add[i]);
                     }
                 }
                 uint32_t w[2][8];                           // V: words of dimensions 8 c16 .. + 3 and .. + 7
@@ -519,12 +513,13 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                 if (keys != 0xffffffffu) {                  // slots without a key: what stands in their row is not looked at
                     const uint32_t mine = keys >> (4 * g4);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (!(mine >> (i < 4 ? i : 12 + i) & 1u)) {
+                    for (int i = 0; i < 8; ++i) {
+                        const bool there = mine >> (i < 4 ? i : 12 + i) & 1u;
 #pragma unroll
-                            for (int n = 0; n < TILES; ++n) x[n][i] = SQ_NEG_INF;
-                            w[0][i] = w[1][i] = 0u;
-                        }
+                        for (int n = 0; n < TILES; ++n) x[n][i] = there ? x[n][i] : SQ_NEG_INF;
+                        w[0][i] = there ? w[0][i] : 0u;
+                        w[1][i] = there ? w[1][i] : 0u;
+                    }
                 }
                 h8 pr[TILES];
                 fold_scores<TILES>(st.m, st.l, st.o, x, inv, pr);
@@ -539,23 +534,48 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
 #pragma unroll
                     for (int n = 0; n < TILES; ++n) st.o[n][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pr[n], st.o[n][dt], 0, 0, 0);
                 }
-                load_v(t + 1);
-                if (even && t + 2 < tiles) list_scales(buf ^ 1);
+                load_v(next);
+            };
+
+            list(0);
+            load_k(s_list[wave][0].at);
+            load_v(s_list[wave][0].at);
+            list_scales(0);
+#pragma clang loop unroll(disable)
+            for (int t = 0, buf = 0; t < tiles; t += 2, buf ^= 1) {
+                const offset_t *here = s_list[wave][buf].at, *next = t + 2 < tiles ? s_list[wave][buf ^ 1].at : s_none;
+                seen = seen_next;
+                list(buf ^ 1);
+                tile(buf, 0, t + 1 < tiles ? here + QT : s_none);
+                list_scales(buf ^ 1);
+                if (t + 1 >= tiles) break;
+                tile(buf, QT, next);
             }
         }
 
         // The drafts: f16 rows.
-        const int d0 = max(w0 - tf - tu, 0), d1 = w1 - tf - tu;             // tiles of theirs
         if (d0 < d1 && arguments().Kd) {
             const TreeAttnArgs &a = arguments();
             typedef global<char> bytes;
             const bytes Kd = (bytes)uniform(a.Kd + bh * a.T * D), Vd = (bytes)uniform(a.Vd + bh * a.T * D);
             const int words = (a.T + 31) / 32;
-            int draft[TILES];                               // of the lane's columns
+            const global<uint32_t> mask = uniform(a.mask + (size_t)b * a.T * words);
+            // (in LDS, where the results' maxima stand later: registers are short here)
+            int *const s_draft = reinterpret_cast<int *>(s_ml[0][wave]);    // drafts of the columns
 #pragma unroll
-            for (int n = 0; n < TILES; ++n) draft[n] = min(row0 + n * 16 + c16, end_row - 1) / a.G;
+            for (int n = 0; n < TILES; ++n) s_draft[n * 16 + c16] = min(row0 + n * 16 + c16, end_row - 1) / a.G;
+            wave_lds_sync();
             auto row_at = [&](int key) { return (uint32_t)min(key, n_drafts - 1) * (uint32_t)(D * sizeof(_Float16)); };
-            h8 k[2][4], v[8];
+            // Values go to LDS past the registers: with them on their way in registers, 128 of which hold the output, some were kept in memory.
+            char *const s_v = s_mem + V_AT + wave * V_TILE;
+            const uint32_t lds_v = uniform((int)(uint32_t)(size_t)(__attribute__((address_space(3))) void *)s_v);
+            auto load_v = [&](int t) {                      // rows 4 i + g4, 16 bytes a lane, one after the other
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_v + (uint32_t)(i * 1024)),
+                                 "v"(row_at(t * QT + 4 * i + g4) + 16 * c16), "s"(Vd) : "m0", "memory");
+            };
+            h8 k[2][4];
             auto load_k = [&](int t) {                      // (behind the last tile the last draft, again and again)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
@@ -569,8 +589,6 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
 #pragma clang loop unroll(disable)
             for (int t = d0; t < d1; ++t) {
                 const int key0 = t * QT;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<global<h8>>(Vd + (row_at(key0 + 4 * g4 + (i < 4 ? i : 12 + i)) + 16 * c16));
                 const uint32_t there = n_drafts - key0 >= 32 ? ~0u : (1u << (n_drafts - key0)) - 1u;
                 float one[8];
 #pragma unroll
@@ -583,22 +601,31 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                     f4 acc[PAIR][2];
 #pragma unroll
                     for (int n = 0; n < PAIR; ++n) acc[n][0] = acc[n][1] = f4{0.f, 0.f, 0.f, 0.f};
+                    h8 qs[PAIR];
+#pragma unroll
+                    for (int n = 0; n < PAIR; ++n) qs[n] = q_of(n0 + n, 0);
 #pragma unroll
                     for (int s = 0; s < 4; ++s) {
+                        h8 next[PAIR];                      // (a step ahead: else the products wait for LDS four times)
+#pragma unroll
+                        for (int n = 0; n < PAIR; ++n) next[n] = s < 3 ? q_of(n0 + n, s + 1) : qs[n];
 #pragma unroll
                         for (int n = 0; n < PAIR; ++n) {
-                            const h8 qv = q_of(n0 + n, s);
-                            acc[n][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[0][s], qv, acc[n][0], 0, 0, 0);
-                            acc[n][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[1][s], qv, acc[n][1], 0, 0, 0);
+                            acc[n][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[0][s], qs[n], acc[n][0], 0, 0, 0);
+                            acc[n][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[1][s], qs[n], acc[n][1], 0, 0, 0);
                         }
+                        if (TILES == 4) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int n = 0; n < PAIR; ++n) qs[n] = next[n];
                     }
+                    if (n0 == 0) load_v(t);                 // (behind the wait for this tile's keys)
                     if (n0 + PAIR == TILES) load_k(t + 1);
                     float x[PAIR][8];
 #pragma unroll
                     for (int n = 0; n < PAIR; ++n) {
-                        const int d = draft[n0 + n], own = d - key0;        // a chain: keys up to the draft itself
+                        const int d = s_draft[(n0 + n) * 16 + c16], own = d - key0;         // a chain: keys up to the draft itself
                         uint32_t sees = own >= 31 ? ~0u : own < 0 ? 0u : (2u << own) - 1u;
-                        if (a.mask) sees = a.mask[((size_t)b * a.T + d) * words + t];
+                        if (a.mask) sees = mask[(uint32_t)(d * words + t)];
                         sees &= there;
 #pragma unroll
                         for (int i = 0; i < 8; ++i) x[n][i] = acc[n][i >> 2][i & 3] * a.scale;
@@ -611,6 +638,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                     fold_scores<PAIR>(st.m + n0, st.l + n0, st.o + n0, x, one, pr + n0);
                     if (TILES == 4) __builtin_amdgcn_sched_barrier(0);
                 }
+                // the eight reads of the next keys may still be on their way, the values must not be
+                asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+                h8 v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const h8 *>(s_v + (4 * g4 + (i < 4 ? i : 12 + i)) * (D * 2) + 16 * c16);
                 uint32_t odd = 0;                           // bit 15 or 31: an infinity or NaN among the lane's values
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -653,8 +685,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                     if (!__any(any)) continue;
 #pragma unroll
                     for (int n = 0; n < TILES; ++n) {
-                        bool seen = key <= draft[n];
-                        if (a.mask) seen = a.mask[((size_t)b * a.T + draft[n]) * words + (key >> 5)] >> (key & 31) & 1u;
+                        const int d = s_draft[n * 16 + c16];
+                        bool seen = key <= d;
+                        if (a.mask) seen = mask[(uint32_t)(d * words + (key >> 5))] >> (key & 31) & 1u;
                         if (seen)
 #pragma unroll
                             for (int dt = 0; dt < 8; ++dt)
@@ -739,15 +772,17 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
     }
 }
 
-// Rows of blocks that several workgroups took, a wave each: four groups of 16 lanes fold every fourth partial result, a lane eight
-// dimensions.
-__global__ __launch_bounds__(256) void tree_merge_kernel(TreeAttnArgs a, int tiles)
+// Rows of blocks that several workgroups took: GROUPS times 16 lanes a row, eight dimensions a lane, each group of lanes every GROUPS-th
+// partial result, four of them read side by side.
+template <int GROUPS>
+__global__ __launch_bounds__(256) void tree_merge_kernel(TreeAttnArgs a, TreePlan plan)
 {
-    const int rows = 16 * tiles, at = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, grp = lane >> 4, d = 8 * (lane & 15);
+    const int rows = 16 * plan.tiles, at = (blockIdx.x * 16 + (threadIdx.x >> 4)) / GROUPS, grp = (threadIdx.x >> 4) % GROUPS, d = 8 * (threadIdx.x & 15);
     const int ui = at / rows, in_block = at - ui * rows;
-    if (ui >= a.B * a.H * a.blocks) return;
+    Unit u = place_of(a, ui);                               // (as many threads as rows of units)
+    const Counts c = counts_of(a, u);
     const int2 info = a.info[ui];
-    const Unit u = unit_of(a, ui, tiles);
+    count(a, c, plan.tiles, u);
     const int row = u.block * rows + in_block;
     if (row >= u.n * a.G || info.y == 0) return;            // (nobody wrote the numbers of a unit without rows)
     float M = SQ_NEG_INF, ls = 0.0f;
@@ -760,20 +795,29 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeAttnArgs a, int til
         y = y * fa + py * fb;
         M = mn;
     };
-    auto part = [&](int i) { return a.part + ((size_t)(i == 0 ? info.x : 2 * ((info.x >> 1) + i)) * rows + in_block) * PART_STRIDE; };
-    for (int i = grp; i < info.y; i += 4) {
-        const float *p = part(i);
-        const float2 ml = *reinterpret_cast<const float2 *>(p);
-        fold(ml.x, ml.y, *reinterpret_cast<const f4 *>(p + 4 + d), *reinterpret_cast<const f4 *>(p + 8 + d));
+    for (int i = grp; i < info.y; i += 4 * GROUPS) {
+        float2 ml[4];
+        f4 px[4], py[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int j = min(i + k * GROUPS, info.y - 1);
+            const float *p = a.part + ((size_t)(j == 0 ? info.x : 2 * ((info.x >> 1) + j)) * rows + in_block) * PART_STRIDE;
+            ml[k] = *reinterpret_cast<const float2 *>(p);
+            px[k] = *reinterpret_cast<const f4 *>(p + 4 + d);
+            py[k] = *reinterpret_cast<const f4 *>(p + 8 + d);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i + k * GROUPS < info.y) fold(ml[k].x, ml[k].y, px[k], py[k]);
     }
 #pragma unroll
-    for (int k = 16; k <= 32; k <<= 1) {
+    for (int k = 16; k < 16 * GROUPS; k <<= 1) {
         const float pm = __shfl_xor(M, k), pl = __shfl_xor(ls, k);
         f4 px, py;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            px[c] = __shfl_xor(x[c], k);
-            py[c] = __shfl_xor(y[c], k);
+        for (int e = 0; e < 4; ++e) {
+            px[e] = __shfl_xor(x[e], k);
+            py[e] = __shfl_xor(y[e], k);
         }
         fold(pm, pl, px, py);
     }
@@ -804,8 +848,9 @@ hipError_t launch_tree_attn(TreeAttnArgs a, hipStream_t s)
     hipLaunchKernelGGL(kernel, dim3((unsigned)p.grid), dim3(256), 0, s, a, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    const long long rows = (long long)p.units * 16 * p.tiles;
-    hipLaunchKernelGGL(tree_merge_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p.tiles);
+    // (few units are in many parts each.  us, 16 / 64 lanes a row: 32 units of 16 parts 12.0 / 6.3; 1024 units in two or three 10 / 26)
+    if (p.units <= TREE_GRID / 4) hipLaunchKernelGGL(tree_merge_kernel<4>, dim3((unsigned)(p.units * p.tiles * 4)), dim3(256), 0, s, a, p);
+    else hipLaunchKernelGGL(tree_merge_kernel<1>, dim3((unsigned)(p.units * p.tiles)), dim3(256), 0, s, a, p);
     return hipGetLastError();
 }
 

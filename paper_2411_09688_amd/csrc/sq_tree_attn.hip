@@ -123,6 +123,25 @@ struct Columns {
     f4 o[TILES][8];
 };
 
+// The lane's number, computed where it stands, so that nothing is held for it (or kept in memory, and waited for behind the keys).
+__device__ __forceinline__ int lane_here()
+{
+    int l;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+    return l;
+}
+
+// The largest of eight numbers in four instructions (fmaxf takes as many again to quiet its operands, which here are results).
+__device__ __forceinline__ float largest8(const float (&x)[8])
+{
+    float a, b;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(x[0]), "v"(x[1]), "v"(x[2]));
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(b) : "v"(x[3]), "v"(x[4]), "v"(x[5]));
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(x[6]), "v"(x[7]), "v"(a));
+    asm("v_max_f32 %0, %1, %2" : "=v"(a) : "v"(a), "v"(b));
+    return a;
+}
+
 // Folds a tile's scores x (key 16 u + 4 g4 + i of column c16 in x[n][4 u + i]) into the maxima and sums of N tiles of columns; p in f16 for
 // the second product.
 template <int N>
@@ -132,7 +151,7 @@ __device__ __forceinline__ void fold_scores(float *m, float *l, f4 (*o)[8], cons
     bool more = false;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        mx[n] = fmaxf(fmaxf(fmaxf(x[n][0], x[n][1]), fmaxf(x[n][2], x[n][3])), fmaxf(fmaxf(x[n][4], x[n][5]), fmaxf(x[n][6], x[n][7])));
+        mx[n] = largest8(x[n]);
         more = more || mx[n] > m[n] + SLACK;
     }
     if (__any(more)) {
@@ -407,6 +426,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
             unsigned long long seen, seen_next;             // slots with a key, of the list in use and the next
             // Lists positions p .. p + 63 and starts to read their scales.
             auto list = [&](int buf) {
+                const int lane = lane_here();
                 bool ok = p + lane < end;
                 int key = 0, sc = 0;
                 offset_t at = 0;
@@ -451,6 +471,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                 wave_lds_sync();
             };
             auto list_scales = [&](int buf) {
+                const int lane = lane_here();
                 const float v = seen_next >> lane & 1u ? vs : 1.0f;         // (a slot without a key: not looked at, but for this)
                 s_list[wave][buf].mul[lane] = ks * a.scale;
                 s_list[wave][buf].add[lane] = __builtin_amdgcn_logf(v);
@@ -460,6 +481,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
             u4v k[2][2];                                    // keys c16 and 16 + c16, dimensions 32 g4 ..
             u2v v[8];                                       // keys 4 g4 .. and 16 + 4 g4 .., dimensions 8 c16 ..
             auto load_k = [&](const offset_t *at) {
+                const int l = lane_here(), c16 = l & 15, g4 = l >> 4;
                 const offset_t k0 = at[c16] + 32 * g4, k1 = at[16 + c16] + 32 * g4;
                 k[0][0] = *reinterpret_cast<global<u4v>>(Kb + k0);
                 k[0][1] = *reinterpret_cast<global<u4v>>(Kb + k0 + 16);
@@ -467,6 +489,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                 k[1][1] = *reinterpret_cast<global<u4v>>(Kb + k1 + 16);
             };
             auto load_v = [&](const offset_t *at) {
+                const int l = lane_here(), c16 = l & 15, g4 = l >> 4;
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     v[i] = *reinterpret_cast<global<u2v>>(Vb + (offset_t)(at[4 * g4 + (i < 4 ? 0 : 12) + i] + 8 * c16));
@@ -491,6 +514,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                 load_k(next);                               // (as soon as the scores have used this tile's)
                 float x[TILES][8], inv[8];
                 const TreeList<WIDE> &ls = s_list[wave][buf];
+                const int g4 = lane_here() >> 4;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const int at = slot + 16 * j + 4 * g4;

@@ -2,7 +2,7 @@
 // the fixed context and the pages of the user cache -- and over the drafts' own f16 rows behind a mask, one softmax over all of them.
 //
 // The G * T query rows of a (sequence, K/V head) read the same keys.  They are cut into blocks, row t * G + g the g-th head of draft
-// t, so that a block of a chain sees a prefix of the drafts.  A wave has 16, 32 or 64 rows of a block (TILES of 16 columns of the matrix
+// t, so that a block of a chain sees a prefix of the drafts.  A wave has the 16, 32, 48 or 64 rows of a block (TILES of 16 columns of the matrix
 // products); the four waves of a workgroup have the same rows and a quarter of the keys each, or rows of their own (row_waves) and
 // the same keys.  Keys, laid end to end -- kept ones, the user's, drafts -- are cut into tiles of 32 and the tiles of all blocks into
 // equal shares, one per workgroup; a second launch merges the blocks that several workgroups took.
@@ -183,11 +183,11 @@ template <int TILES, bool WIDE>
 __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see arguments() */, TreePlan plan)
 {
     typedef std::conditional_t<WIDE, unsigned long long, uint32_t> offset_t;
-    constexpr bool Q_IN_LDS = TILES == 4;
+    constexpr bool Q_IN_LDS = TILES >= 3;
     // The queries (64 rows of 256 bytes, 16 bytes at place p of row r standing at p ^ (r & 15)) and, behind the keys, two
     // sums of results (likewise).
     // Between them, behind the queries, stands a tile of the drafts' values for each wave.
-    constexpr int V_AT = Q_IN_LDS ? 64 * D * 2 : 0, V_TILE = QT * D * 2, RESULTS = 2 * 16 * TILES * D * sizeof(float);
+    constexpr int V_AT = Q_IN_LDS ? 16 * TILES * D * 2 : 0, V_TILE = QT * D * 2, RESULTS = 2 * 16 * TILES * D * sizeof(float);
     __shared__ __align__(16) char s_mem[RESULTS > V_AT + 4 * V_TILE ? RESULTS : V_AT + 4 * V_TILE];
     __shared__ __align__(16) TreeList<WIDE> s_list[4][2];
     __shared__ __align__(16) offset_t s_none[QT];           // where a wave reads ahead behind its last tile: the first row
@@ -306,11 +306,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
         h8 q[Q_IN_LDS ? 1 : TILES][4];
         h8 *const sq_ = reinterpret_cast<h8 *>(s_mem);
         if constexpr (Q_IN_LDS) {
-            h8 v[4];
+            h8 v[TILES];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = query(row0 + k * 16 + (tid >> 4))[tid & 15];
+            for (int k = 0; k < TILES; ++k) v[k] = query(row0 + k * 16 + (tid >> 4))[tid & 15];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sq_[(k * 16 + (tid >> 4)) * 16 + ((tid & 15) ^ (tid >> 4))] = v[k];
+            for (int k = 0; k < TILES; ++k) sq_[(k * 16 + (tid >> 4)) * 16 + ((tid & 15) ^ (tid >> 4))] = v[k];
             __syncthreads();
         } else {
 #pragma unroll
@@ -509,7 +509,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                         acc[n][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qv, acc[n][0], 0, 0, 0);
                         acc[n][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qv, acc[n][1], 0, 0, 0);
                     }
-                    if (TILES == 4) __builtin_amdgcn_sched_barrier(0);      // (the queries of one step in registers at a time)
+                    if (Q_IN_LDS) __builtin_amdgcn_sched_barrier(0);      // (the queries of one step in registers at a time)
                 }
                 load_k(next);                               // (as soon as the scores have used this tile's)
                 float x[TILES][8], inv[8];
@@ -619,7 +619,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                 for (int i = 0; i < 8; ++i) one[i] = 1.0f;
                 h8 pr[TILES];
                 // (two columns at a time, which leaves registers for the tile of values that is on its way)
-                constexpr int PAIR = TILES < 2 ? TILES : 2;
+                constexpr int PAIR = TILES == 4 ? 2 : TILES;
 #pragma unroll
                 for (int n0 = 0; n0 < TILES; n0 += PAIR) {
                     f4 acc[PAIR][2];
@@ -638,7 +638,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                             acc[n][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[0][s], qs[n], acc[n][0], 0, 0, 0);
                             acc[n][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[1][s], qs[n], acc[n][1], 0, 0, 0);
                         }
-                        if (TILES == 4) __builtin_amdgcn_sched_barrier(0);
+                        if (Q_IN_LDS) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                         for (int n = 0; n < PAIR; ++n) qs[n] = next[n];
                     }
@@ -660,7 +660,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                         }
                     }
                     fold_scores<PAIR>(st.m + n0, st.l + n0, st.o + n0, x, one, pr + n0);
-                    if (TILES == 4) __builtin_amdgcn_sched_barrier(0);
+                    if (Q_IN_LDS) __builtin_amdgcn_sched_barrier(0);
                 }
                 // the eight reads of the next keys may still be on their way, the values must not be
                 asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
@@ -851,7 +851,8 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeAttnArgs a, TreePla
 TreePlan tree_plan(int B, int H, int rows, long long keys)
 {
     TreePlan p{};
-    p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    // (48 rows to a block where that makes no more blocks: a quarter less of the softmax)
+    p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : (rows + 47) / 48 == (rows + 63) / 64 ? 3 : 4;
     p.blocks = (rows + 16 * p.tiles - 1) / (16 * p.tiles);
     const long long units = (long long)B * H * p.blocks, most = (keys + QT - 1) / QT + 3;      // tiles: of three sources
     p.units = (int)std::min(units, 0x7fffffffll);
@@ -868,6 +869,7 @@ hipError_t launch_tree_attn(TreeAttnArgs a, hipStream_t s)
     a.blocks = p.blocks;
     auto *kernel = p.tiles == 1 ? (wide ? tree_attn_kernel<1, true> : tree_attn_kernel<1, false>)
                    : p.tiles == 2 ? (wide ? tree_attn_kernel<2, true> : tree_attn_kernel<2, false>)
+                   : p.tiles == 3 ? (wide ? tree_attn_kernel<3, true> : tree_attn_kernel<3, false>)
                                   : (wide ? tree_attn_kernel<4, true> : tree_attn_kernel<4, false>);
     hipLaunchKernelGGL(kernel, dim3((unsigned)p.grid), dim3(256), 0, s, a, p);
     hipError_t e = hipGetLastError();

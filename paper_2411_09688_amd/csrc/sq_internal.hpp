@@ -485,7 +485,7 @@ struct ReadArgs {
 };
 hipError_t launch_cache_read(ReadArgs a, int B, hipStream_t s);
 
-constexpr int TREE_GRID = 512;     // workgroups that share the keys of a call
+constexpr int TREE_SHARES = 512;   // workgroups that share the keys of a call, two a compute unit by their registers
 constexpr int TREE_SHARED_UNITS = 1024;   // blocks of rows up to which they do: each workgroup counts the tiles of all blocks
 constexpr int TREE_AHEAD = 12;     // tiles of 32 keys that take as long as beginning and ending a block
 constexpr int MAX_MASKED = 32768;  // drafts with a mask: offsets into a sequence's have 32 bits
@@ -516,7 +516,7 @@ struct TreePlan {
     long long grid;
 };
 TreePlan tree_plan(int B, int H, int rows, long long keys);
-inline size_t tree_parts(const TreePlan &p) { return p.units > TREE_SHARED_UNITS ? 0 : (size_t)2 * TREE_GRID * 16 * p.tiles; }   // rows of partial results
+inline size_t tree_parts(const TreePlan &p) { return p.units > TREE_SHARED_UNITS ? 0 : (size_t)2 * TREE_SHARES * 16 * p.tiles; }   // rows of partial results
 hipError_t launch_tree_attn(TreeAttnArgs a, hipStream_t s);
 
 // Records the calling thread's error message (what sq_last_error returns) and hands back `code`.

@@ -183,7 +183,7 @@ template <int TILES, bool WIDE>
 __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see arguments() */, TreePlan plan)
 {
     typedef std::conditional_t<WIDE, unsigned long long, uint32_t> offset_t;
-    constexpr bool Q_IN_LDS = TILES >= 3;
+    constexpr bool Q_IN_LDS = TILES >= 2;
     // The queries (64 rows of 256 bytes, 16 bytes at place p of row r standing at p ^ (r & 15)) and, behind the keys, two
     // sums of results (likewise).
     // Between them, behind the queries, stands a tile of the drafts' values for each wave.
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
             }
         }
         int before = block_exclusive(mine, tid, s_w, all);
-        const int shares = min(TREE_GRID, (all + 3) / 4), per_xcd = (shares + 7) / 8;      // (at least a tile for each wave)
+        const int shares = min(TREE_SHARES, (all + 3) / 4), per_xcd = (shares + 7) / 8;      // (at least a tile for each wave)
         if (all == 0) return;
         per = (all + shares - 1) / shares;
         share = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);             // (each XCD takes consecutive shares)
@@ -851,13 +851,16 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeAttnArgs a, TreePla
 TreePlan tree_plan(int B, int H, int rows, long long keys)
 {
     TreePlan p{};
-    // (48 rows to a block where that makes no more blocks: a quarter less of the softmax)
-    p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : (rows + 47) / 48 == (rows + 63) / 64 ? 3 : 4;
+    // Rows of a block.  More of them share what a key costs (its codes to f16, its values turned); fewer make more blocks, which are begun and
+    // ended side by side.  us at 64 / 32 rows, 36K keys a head of which 1/8 and 2K user keys: 8 blocks of 64 29.3 / 23.1, 32 32.4 / 30.0, 64
+    // 45.6 / 43.3, 128 63.5 / 68.2, 256 99 / 113.  48 where that makes no more blocks: a quarter less of the softmax (36 rows 44.6 / 37.3).
+    const int at64 = (rows + 63) / 64;
+    p.tiles = rows <= 16 ? 1 : rows <= 32 || (long long)B * H * at64 <= 64 ? 2 : (rows + 47) / 48 == at64 ? 3 : 4;
     p.blocks = (rows + 16 * p.tiles - 1) / (16 * p.tiles);
     const long long units = (long long)B * H * p.blocks, most = (keys + QT - 1) / QT + 3;      // tiles: of three sources
     p.units = (int)std::min(units, 0x7fffffffll);
-    p.splits = units > TREE_SHARED_UNITS ? 1 : units * ((most + 3) / 4) <= TREE_GRID ? (int)((most + 3) / 4) : 0;
-    p.grid = p.splits ? (long long)p.units * p.splits : TREE_GRID;
+    p.splits = units > TREE_SHARED_UNITS ? 1 : units * ((most + 3) / 4) <= TREE_SHARES ? (int)((most + 3) / 4) : 0;
+    p.grid = p.splits ? (long long)p.units * p.splits : TREE_SHARES;
     return p;
 }
 
@@ -875,7 +878,7 @@ hipError_t launch_tree_attn(TreeAttnArgs a, hipStream_t s)
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     // (few units are in many parts each.  us, 16 / 64 lanes a row: 32 units of 16 parts 12.0 / 6.3; 1024 units in two or three 10 / 26)
-    if (p.units <= TREE_GRID / 4) hipLaunchKernelGGL(tree_merge_kernel<4>, dim3((unsigned)(p.units * p.tiles * 4)), dim3(256), 0, s, a, p);
+    if (p.units <= TREE_SHARES / 4) hipLaunchKernelGGL(tree_merge_kernel<4>, dim3((unsigned)(p.units * p.tiles * 4)), dim3(256), 0, s, a, p);
     else hipLaunchKernelGGL(tree_merge_kernel<1>, dim3((unsigned)(p.units * p.tiles)), dim3(256), 0, s, a, p);
     return hipGetLastError();
 }

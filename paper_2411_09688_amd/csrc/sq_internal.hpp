@@ -487,7 +487,9 @@ hipError_t launch_cache_read(ReadArgs a, int B, hipStream_t s);
 
 constexpr int TREE_SHARES = 512;   // workgroups that share the keys of a call, two a compute unit by their registers
 constexpr int TREE_SHARED_UNITS = 1024;   // blocks of rows up to which they do: each workgroup counts the tiles of all blocks
-constexpr int TREE_AHEAD = 12;     // tiles of 32 keys that take as long as beginning and ending a block
+// Tiles of 32 keys that take as long as beginning and ending a block.  us with 4 / 12 / 20 / 32: 64 blocks of 32 rows, 6K keys 34.0 / 31.8 / 30.6 / 30.7;
+// 128 blocks of 64, 8K 68.4 / 64.7 / 63.0 / 65.0; 1024 blocks of a chain that sees itself alone 141 / 96.5 / 96.8 / 101.
+constexpr int TREE_AHEAD = 20;
 constexpr int MAX_MASKED = 32768;  // drafts with a mask: offsets into a sequence's have 32 bits
 struct TreeAttnArgs {
     const _Float16 *q;             // [B, H, G, T, D]

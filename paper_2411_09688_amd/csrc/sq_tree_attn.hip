@@ -1,11 +1,10 @@
 // sq_tree_attn_q8: attention of many query tokens of a sequence (a tree or a chain of drafts) over e4m3 keys and values -- kept ranges of
 // the fixed context and the pages of the user cache -- and over the drafts' own f16 rows behind a mask, one softmax over all of them.
 //
-// The G * T query rows of a (sequence, K/V head) read the same keys.  They are cut into blocks, row t * G + g the g-th head of draft
-// t, so that a block of a chain sees a prefix of the drafts.  A wave has the 16, 32, 48 or 64 rows of a block (TILES of 16 columns of the matrix
-// products); the four waves of a workgroup have the same rows and a quarter of the keys each, or rows of their own (row_waves) and
-// the same keys.  Keys, laid end to end -- kept ones, the user's, drafts -- are cut into tiles of 32 and the tiles of all blocks into
-// equal shares, one per workgroup; a second launch merges the blocks that several workgroups took.
+// The G * T query rows of a (sequence, K/V head) read the same keys.  They are cut into blocks of 16, 32, 48 or 64 (TILES times the 16 columns
+// of a matrix product; see tree_plan), row t * G + g the g-th head of draft t, so that a block of a chain sees a prefix of the drafts.  The four
+// waves of a workgroup have the same rows and a quarter of the keys each.  Keys, laid end to end -- kept ones, the user's, drafts -- are cut into
+// tiles of 32 and the tiles of all blocks into equal shares, one per workgroup; a second launch merges the blocks that several workgroups took.
 //
 //   S^T [32 keys x 16 TILES] = K q^T    codes to f16 (exact), once for all columns
 //   t = S * (key's scale * sm_scale * log2 e) + log2(value's scale),   M: a reference near the maximum of t,   p = 2^(t - M + 8)
@@ -184,9 +183,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
 {
     typedef std::conditional_t<WIDE, unsigned long long, uint32_t> offset_t;
     constexpr bool Q_IN_LDS = TILES >= 2;
-    // The queries (64 rows of 256 bytes, 16 bytes at place p of row r standing at p ^ (r & 15)) and, behind the keys, two
-    // sums of results (likewise).
-    // Between them, behind the queries, stands a tile of the drafts' values for each wave.
+    // The queries (rows of 256 bytes, 16 bytes at place p of row r standing at p ^ (r & 15)), behind them a tile of the drafts' values for each
+    // wave; when all keys are done, in their place two sums of results (of 512 bytes a row, likewise).
     constexpr int V_AT = Q_IN_LDS ? 16 * TILES * D * 2 : 0, V_TILE = QT * D * 2, RESULTS = 2 * 16 * TILES * D * sizeof(float);
     __shared__ __align__(16) char s_mem[RESULTS > V_AT + 4 * V_TILE ? RESULTS : V_AT + 4 * V_TILE];
     __shared__ __align__(16) TreeList<WIDE> s_list[4][2];

@@ -415,3 +415,52 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
     with pytest.raises(sq.SqError):
         call(ws=None)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("G,T", [(1, 8), (4, 7), (3, 15), (4, 40), (8, 100)])
+def test_a_pool_of_more_than_4_gb(G, T):
+    """Pages behind the reach of 32-bit offsets, for each size of a block of rows."""
+    B, H, P = 9, 8, 64
+    n = (1 << 32) // (H * P * 128) + 40
+    p = Problem(G * T, B, H, G, T, L=400, C=9, user=150, page=P, ragged=True)
+    used = B * p.table.shape[1]
+    local = p.table.copy()
+    p.upload()
+    K8, V8 = (torch.zeros(n, H, P, 128, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.ones(n, H, device="cuda") for _ in range(2))
+    far = (n - 1 - p.rng.permutation(used + 2)).astype(np.int32)                # page i of the small pool is page far[i] of the large one
+    at = torch.from_numpy(far).cuda().long()
+    for big, small in ((K8, p.cK), (V8, p.cV), (ks, p.cks.astype(np.float32)), (vs, p.cvs.astype(np.float32))):
+        big[at] = cu(small)
+    p.args[10] = sq.make_cache(K8.view(sq.F8), V8.view(sq.F8), ks, vs, cu(far[local]))
+    p.call()
+    p.check()
+
+
+def test_a_long_chain():
+    """5000 drafts of a prompt, 3 heads: checked at the rows where blocks, tiles and words end."""
+    p = Problem(23, 1, 1, 3, 5000, L=600, C=20, user=200, page=32, mask=None).upload()
+    p.call()
+    keys, _ = p.keys(0, 0)
+    q = p.q[0].transpose(1, 0, 2).reshape(15000, 128).astype(np.float64)
+    out = p.out.cpu().numpy()[0].transpose(1, 0, 2).reshape(15000, 128).astype(np.float64)
+    lse = p.lse.cpu().numpy()[0].T.reshape(15000)
+    rows = np.unique(np.concatenate([[0, 1, 2, 3, 63, 64, 65, 95, 96, 97, 14997, 14998, 14999], p.rng.integers(0, 15000, 60)]))
+    picked = [(k, v, None if seen is None else seen[rows], s) for k, v, seen, s in keys]
+    o, z, off, off_z = plain.attend(q[rows], picked, SCALE)
+    assert (np.abs(out[rows] - o) <= off).all() and (np.abs(lse[rows] - z) <= off_z).all()
+
+
+def test_a_mask_of_many_words():
+    """700 drafts in random order of sight: 22 words a row."""
+    Problem(24, 1, 1, 2, 700, L=100, C=4, user=33, mask="any").run()
+
+
+def test_masks_larger_than_their_offsets_reach_are_refused():
+    p = Problem(25, 1, 1, 1, 4, user=16).upload()
+    shape = sq.make_shape(1, 1, 1, 1, 32769, 0, SCALE)
+    t = lambda *s, dtype=F16: torch.empty(*s, dtype=dtype, device="cuda")  # noqa: E731
+    q, K, mask = t(1, 1, 32769, 128), t(1, 1, 32769, 128), t(1, 32769, 1025, dtype=I32)
+    ws = sq.workspace(shape, sq.SQ_CALL_TREE_ATTN_Q8, "cuda:0")
+    with pytest.raises(sq.SqError, match="too large"):
+        sq.sq_tree_attn_q8(shape, 32769, q, *[None] * 7, p.cache, p.args[11], K, K, mask, None, t(1, 1, 32769, 128), None, ws)

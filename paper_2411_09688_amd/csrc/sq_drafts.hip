@@ -6,7 +6,8 @@
 namespace sq {
 
 // A draft's ancestors have smaller numbers, so a thread that walks up from its draft meets the words of its mask from the last to the
-// first, and holds one at a time.
+// first, and holds one at a time.  16 drafts 1.7 us on the GPU, 64 trees of 256 (some 15 deep) 4.3: the walk, a read of LDS a step, and
+// the calling thread takes 5.4.
 __global__ __launch_bounds__(MAX_DRAFTS) void tree_prepare_kernel(TreeArgs a)
 {
     __shared__ int s_parent[MAX_DRAFTS];
@@ -45,7 +46,8 @@ hipError_t launch_tree_prepare(const TreeArgs &a, int B, hipStream_t s)
     return hipGetLastError();
 }
 
-// One wave per sequence: a lane holds every 64th draft and asks each step whether it is the next one; the lowest number wins.
+// One wave per sequence: a lane holds every 64th draft and asks each step whether it is the next one; the lowest number wins.  16 drafts 1.8 us
+// on the GPU, 256 trees of 64 2.8; the calling thread takes 6.4.
 template <int N>
 __global__ __launch_bounds__(64) void tree_accept_kernel(AcceptArgs a)
 {
@@ -95,8 +97,12 @@ hipError_t launch_tree_accept(const AcceptArgs &a, int B, hipStream_t s)
 // Accepted rows into their pages.  As in sq_cache_append a page is written by one workgroup per head and tensor, which holds its new
 // rows in registers between the maximum and the rounding and shifts the page's earlier codes if the scale rises; here the rows
 // are f16 and stand as they are, so every step is exact but the one rounding.
+//
+// What bounds it is the memory: four prompts of up to 8000 rows, 8 heads (160 MB) 29 us where the caches hold what the call before left, 33
+// where they do not, 4.8 to 5.5 TB/s; eight of 32 heads (1.3 GB) past the caches 208 (221 with them).  Up to six rows of each of 16 sequences: 4.4 us on
+// the GPU, a chain of reads (the length, the page, the rows), the call itself takes the calling thread 5.5.
 // Tokens g, g + 16, .. of a page by 16 lanes each: N of them a thread.
-template <int N>
+template <int N, bool STREAM>
 __global__ __launch_bounds__(256) void cache_commit_kernel(CommitArgs a)
 {
     const int tid = threadIdx.x, j = tid & 15, g = tid >> 4, waves = blockDim.x >> 6;
@@ -118,7 +124,7 @@ __global__ __launch_bounds__(256) void cache_commit_kernel(CommitArgs a)
     for (int i = 0; i < N; ++i) {
         int row = row0 + min(i * 16 + g, n - 1);            // (lanes behind the last read it again, and store nothing)
         if (a.path) row = min(max(a.path[(size_t)b * a.T + row], 0), a.T - 1);
-        const h8 v = *reinterpret_cast<const h8 *>(X + (size_t)row * D + 8 * j);
+        const h8 v = load_once<STREAM>(reinterpret_cast<const h8 *>(X + (size_t)row * D + 8 * j));
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             x[i][e] = (float)v[e];
@@ -146,7 +152,7 @@ __global__ __launch_bounds__(256) void cache_commit_kernel(CommitArgs a)
     }
 #pragma unroll
     for (int i = 0; i < N; ++i)
-        if (i * 16 + g < n) *reinterpret_cast<u2v *>(codes + (size_t)(o + i * 16 + g) * D + 8 * j) = e4m3_encode8(x[i], inv);
+        if (i * 16 + g < n) store_once<STREAM>(reinterpret_cast<u2v *>(codes + (size_t)(o + i * 16 + g) * D + 8 * j), e4m3_encode8(x[i], inv));
     if (tid == 0) *scale = exp2_int(e);
 }
 
@@ -156,62 +162,73 @@ hipError_t launch_cache_commit(CommitArgs a, int B, hipStream_t s)
     const long long blocks = (long long)B * a.per_seq * a.H * 2;
     if (blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
     const int most = a.T < a.P ? a.T : a.P, threads = most < 16 ? (most * 16 + 63) / 64 * 64 : 256;
-    auto *kernel = most > 32 ? cache_commit_kernel<4> : most > 16 ? cache_commit_kernel<2> : cache_commit_kernel<1>;
+    const bool stream = streams((size_t)B * a.H * a.T * 6 * D);
+    auto *kernel = most > 32 ? (stream ? cache_commit_kernel<4, true> : cache_commit_kernel<4, false>)
+                   : most > 16 ? cache_commit_kernel<2, false> : cache_commit_kernel<1, false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, s, a);
     return hipGetLastError();
 }
 
-// Pages back to rows: 64 tokens of a head and tensor per workgroup, 8 codes a lane, 16 lanes a token.  A code times its scale is rounded
-// to f16 once.
+// Pages back to rows: READ_TOKENS tokens of a head and tensor per workgroup, 8 codes a lane, 16 lanes a token, so that a store of a wave
+// fills lines.  A code times its scale is rounded to f16 once.
+//
+// What bounds it is the memory.  Four sequences of up to 8192 tokens, 32 heads, pages of 16 (654 MB): 82 us on the pages that the call before read,
+// 98 on others, 6.7 TB/s (tokens a workgroup: 16 136, 32 98, 64 104, 128 112; 16 codes a lane, whose stores leave gaps in lines, 166; pages read past
+// the caches as well as rows written so 101 for 82).  500 tokens of 8 heads: the calling thread, 5.4.
+constexpr int READ_TOKENS = 32;
+
 template <bool STREAM>
 __global__ __launch_bounds__(256) void cache_read_kernel(ReadArgs a)
 {
+    constexpr int N = READ_TOKENS / 16;
     const int tid = threadIdx.x, j = tid & 15, g = tid >> 4;
     const int chunk = blockIdx.x % a.chunks, bhv = blockIdx.x / a.chunks, hv = bhv % (2 * a.H), b = bhv / (2 * a.H);
     const bool value = hv >= a.H;
     const int h = value ? hv - a.H : hv;
     const int cap = a.max_pages << a.p_log, end = min(max(a.seq_len[b], 0), cap), first = a.first ? max(a.first[b], 0) : 0;
+    const int n = min(a.U, max(end - first, 0));            // tokens of the sequence that are read
+    if (chunk * READ_TOKENS >= n) return;
     const uint8_t *codes = value ? a.V8 : a.K8;
     const float *scales = value ? a.v_scale : a.k_scale;
     _Float16 *out = (value ? a.V : a.K) + ((size_t)b * a.H + h) * a.U * D;
-    u2v c[4];
-    float scale[4];
-    bool there[4];
+    u2v c[N];
+    float scale[N];
+    int page[N];
+    // (token behind the last: the last again, and nothing is stored)
+    auto token = [&](int i) { return first + min(chunk * READ_TOKENS + i * 16 + g, n - 1); };
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int u = chunk * 64 + i * 16 + g;
-        there[i] = u < a.U && first < end && u < end - first;
-        c[i] = u2v{0u, 0u};
-        scale[i] = 0.0f;
-        if (there[i]) {
-            const int t = first + u, page = a.page_table[(size_t)b * a.max_pages + (t >> a.p_log)];
-            if (page >= 0 && page < a.n_pages) {            // (no page: zeros)
-                const size_t ph = (size_t)page * a.H + h;
-                c[i] = load_once<STREAM>(reinterpret_cast<const u2v *>(codes + ((ph << a.p_log) + (t & ((1 << a.p_log) - 1))) * D + 8 * j));
-                scale[i] = scales[ph];
-            }
+    for (int i = 0; i < N; ++i) page[i] = a.page_table[(size_t)b * a.max_pages + (token(i) >> a.p_log)];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const bool ok = page[i] >= 0 && page[i] < a.n_pages;
+        const size_t ph = (size_t)(ok ? page[i] : 0) * a.H + h;
+        c[i] = *reinterpret_cast<const u2v *>(codes + ((ph << a.p_log) + (token(i) & ((1 << a.p_log) - 1))) * D + 8 * j);
+        scale[i] = scales[ph];
+        if (!ok) {                                          // (no page: zeros)
+            c[i] = u2v{0u, 0u};
+            scale[i] = 0.0f;
         }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (!there[i]) continue;
+    for (int i = 0; i < N; ++i) {
+        const int u = chunk * READ_TOKENS + i * 16 + g;
+        if (u >= n) break;
         h8 y;
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-            const uint32_t x = w ? c[i].y : c[i].x;
-            const f2v lo = __builtin_amdgcn_cvt_pk_f32_fp8(x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(x, true);
+            const f2v lo = __builtin_amdgcn_cvt_pk_f32_fp8(c[i][w], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(c[i][w], true);
             y[4 * w] = (_Float16)(lo.x * scale[i]);
             y[4 * w + 1] = (_Float16)(lo.y * scale[i]);
             y[4 * w + 2] = (_Float16)(hi.x * scale[i]);
             y[4 * w + 3] = (_Float16)(hi.y * scale[i]);
         }
-        store_once<STREAM>(reinterpret_cast<h8 *>(out + (size_t)(chunk * 64 + i * 16 + g) * D + 8 * j), y);
+        store_once<STREAM>(reinterpret_cast<h8 *>(out + (size_t)u * D + 8 * j), y);
     }
 }
 
 hipError_t launch_cache_read(ReadArgs a, int B, hipStream_t s)
 {
-    a.chunks = (a.U + 63) / 64;
+    a.chunks = (a.U + READ_TOKENS - 1) / READ_TOKENS;
     const long long blocks = (long long)B * a.H * 2 * a.chunks;
     if (blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
     auto *kernel = streams((size_t)B * a.H * a.U * 6 * D) ? cache_read_kernel<true> : cache_read_kernel<false>;

@@ -191,3 +191,42 @@ def test_what_is_read_back_commits_to_the_same_cache():
     again = [torch.empty_like(K) for _ in range(2)]
     sq.sq_cache_read(sh, other, None, full, *again)
     assert all(torch.equal(x, y) for x, y in zip(back, again))
+
+
+def test_calls_that_pass_the_caches():
+    """From 256 MB on: rows written at once against the same rows written in two halves, and what is read back against torch."""
+    B, H, T, page = 8, 8, 6000, 64
+    g = torch.Generator(device="cuda").manual_seed(3)
+    K, V = (torch.randn(B, H, T, 128, generator=g, device="cuda").half() for _ in range(2))
+    width = -(-(T + 50) // page)
+    rng = np.random.default_rng(3)
+    pages = rng.permutation(B * width).reshape(B, width).astype(np.int32)
+    made = []
+    for _ in range(2):
+        codes = [torch.full((B * width, H, page, 128), 0x11, dtype=torch.uint8, device="cuda").view(sq.F8) for _ in range(2)]
+        made.append(sq.make_cache(*codes, *(torch.full((B * width, H), 2.0 ** -9, device="cuda") for _ in range(2)), cu(pages)))
+    old = cu(rng.integers(0, 50, B).astype(np.int32))
+    sh = sq.make_shape(B, H, 1, 1, T, T + 50, 1.0)
+    assert B * H * T * 128 * 6 >= 256 << 20
+    sq.sq_cache_commit(sh, made[0], old, None, None, K, V)
+    # (from whole pages on, so that no page's scale is decided in two calls)
+    cut = ((old + T // 2) // page * page - old).int()
+    for b in range(B):                                          # each sequence's halves end at its own page
+        one = sq.make_shape(1, H, 1, 1, T, 0, 1.0)
+        c = sq.make_cache(*made[1].tensors[:4], made[1].tensors[4][b:b + 1].clone())
+        n = int(cut[b])
+        start = old[b:b + 1].clone()
+        sq.sq_cache_commit(one, c, start, None, torch.full((1,), n, dtype=I32, device="cuda"), K[b:b + 1].contiguous(), V[b:b + 1].contiguous())
+        rest = [torch.cat([x[b:b + 1, :, n:], x[b:b + 1, :, :n]], 2).contiguous() for x in (K, V)]
+        sq.sq_cache_commit(one, c, start + n, None, torch.full((1,), T - n, dtype=I32, device="cuda"), *rest)
+    for x, y in zip(made[0].tensors[:4], made[1].tensors[:4]):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    out = [torch.full((B, H, T + 50, 128), 3.0, dtype=F16, device="cuda") for _ in range(2)]
+    held = old + T
+    sq.sq_cache_read(sh, made[0], None, held.int(), *out)
+    t = torch.arange(T + 50, device="cuda")
+    at = cu(pages).long()[:, (t // page).clamp(max=width - 1)]
+    for i in range(2):
+        codes = made[0].tensors[i].view(torch.uint8)[at, :, t % page].view(sq.F8).float() * made[0].tensors[2 + i][at][..., None]
+        want = torch.where((t < held.view(-1, 1))[:, :, None, None], codes.half(), torch.tensor(3.0, dtype=F16, device="cuda"))
+        assert torch.equal(out[i], want.transpose(1, 2))

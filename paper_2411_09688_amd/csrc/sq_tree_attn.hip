@@ -12,6 +12,16 @@
 //   l                       += p / value's scale                       (the unrounded p)
 // With the value's scale in the exponent P needs no factor, whatever the scales are: it is at most 2^15, and has its 11 bits down to 2^-22
 // of the largest.  out = O / l, log-sum-exp = (M - 8 + log2 l) ln 2.
+//
+// What bounds it, and the two launches on the GPU (us; 8 K/V heads of 4 query heads):
+//   1 sequence, 5K keys, a few rows     8.1 + 4.0   the launches, and a search, a prologue and a few tiles whose first reads come from HBM
+//   1 sequence of 64 drafts, 32K + 1K keys, 1/8 kept     23.6 + 4.8   the same, and 2 to 3 tiles a wave: floor 4.2
+//   16 sequences of 13 drafts, 128K keys, 1/16 kept, 4K user's     102 + 7   the reads: 370 MB, at 5 TB/s while the loops run (72 us), the rest
+//     beginning and ending blocks.  (Sequences are not joined: the keys that any of them keeps are 280 MB.)
+//   a chain of 2048, the same 32K + 1K keys     ~300 + 10   the vector units (conversion, softmax) and the matrix units, which at two waves
+//     a SIMD hardly overlap: 205 GFLOP at 690 TFLOP/s in all, 850 to 890 in the loop over codes, half as much in the loop over drafts
+// Tried there: three workgroups a CU at 32 rows 31.5 -> 37 us, one wave a SIMD 1.55 times the time, 48 / 32 rows of a long chain 303 -> 333 / 372,
+// raised or lowered wave priority 5 to 10 % slower either way.
 #include <algorithm>
 
 #include "sq_decode_q8.hpp"
@@ -795,7 +805,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
 }
 
 // Rows of blocks that several workgroups took: GROUPS times 16 lanes a row, eight dimensions a lane, each group of lanes every GROUPS-th
-// partial result, four of them read side by side.
+// partial result, four of them read side by side.  Bound by the chain of reads: 4 to 7 us for what is a few MB (10 for the rows of a long chain).
 template <int GROUPS>
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeAttnArgs a, TreePlan plan)
 {
@@ -875,8 +885,9 @@ hipError_t launch_tree_attn(TreeAttnArgs a, hipStream_t s)
     hipLaunchKernelGGL(kernel, dim3((unsigned)p.grid), dim3(256), 0, s, a, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    // (few units are in many parts each.  us, 16 / 64 lanes a row: 32 units of 16 parts 12.0 / 6.3; 1024 units in two or three 10 / 26)
-    if (p.units <= TREE_SHARES / 4) hipLaunchKernelGGL(tree_merge_kernel<4>, dim3((unsigned)(p.units * p.tiles * 4)), dim3(256), 0, s, a, p);
+    // (few units are in many parts each.  us, 16 / 64 lanes a row: 32 units of 32 rows 8.7 / 5.5, 64 6.9 / 5.2, 128 5.6 / 6.2, 128 of 64 rows
+    // 6.8 / 9.1, 1024 in two or three parts 10 / 26)
+    if (p.units <= TREE_SHARES / 8) hipLaunchKernelGGL(tree_merge_kernel<4>, dim3((unsigned)(p.units * p.tiles * 4)), dim3(256), 0, s, a, p);
     else hipLaunchKernelGGL(tree_merge_kernel<1>, dim3((unsigned)(p.units * p.tiles)), dim3(256), 0, s, a, p);
     return hipGetLastError();
 }

@@ -14,7 +14,7 @@
 // of the largest.  out = O / l, log-sum-exp = (M - 8 + log2 l) ln 2.
 //
 // What bounds it, and the two launches on the GPU (us; 8 K/V heads of 4 query heads):
-//   1 sequence, 5K keys, a few rows     8.1 + 4.0   the launches, and a search, a prologue and a few tiles whose first reads come from HBM
+//   4 heads of 8 drafts, 4K + 128 keys, 1/4 kept     8.1 + 4.0   the launches, and a search, a prologue and a tile whose reads come from HBM
 //   1 sequence of 64 drafts, 32K + 1K keys, 1/8 kept     23.6 + 4.8   the same, and 2 to 3 tiles a wave: floor 4.2
 //   16 sequences of 13 drafts, 128K keys, 1/16 kept, 4K user's     102 + 7   the reads: 370 MB, at 5 TB/s while the loops run (72 us), the rest
 //     beginning and ending blocks.  (Sequences are not joined: the keys that any of them keeps are 280 MB.)

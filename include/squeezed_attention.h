@@ -680,7 +680,8 @@ int sq_tree_prepare(const sq_shape_t *shape, const int32_t *parents, const int32
  *      outside [0, L) is read, a page that is none has no keys; which keys such a row then attends to is not specified.
  * Out: out f16 [B,H*G,T,d]; lse f32 [B,H*G,T], or NULL.  A row without visible keys gets out = 0 and lse = -inf.  Rows of drafts from
  *      n_drafts[b] on are left as they were.  out and lse must not overlap the inputs.
- *      A key that a row does not see has no influence on it, whatever its rows hold; infinities and NaN that it sees make it not finite.
+ *      A key that a row does not see has no influence on it, whatever its rows hold; infinities and NaN among the values that it sees, and scores
+ *      of NaN or +inf, make it not finite, and a score of -inf has no weight (a row of nothing else counts as one without keys).
  *      The keys of all (sequence, head)s are divided into equal shares, so that the order of a row's sums, and with it its last bits, follows
  *      from the number of keys of all of them.
  * Workspace: sq_workspace_bytes(shape, SQ_CALL_TREE_ATTN_Q8).

@@ -1956,9 +1956,13 @@ int sq_sparse_attn_decode_q8(const sq_shape_t *sh, int32_t one_set, const void *
 
 namespace {
 
-int check_drafts(const char *fn, const sq_shape_t *sh)
+// (a launch has fewer than 2^32 threads)
+bool too_many(long long workgroups, int threads) { return workgroups > 0xffffffffll / threads; }
+
+int check_drafts(const char *fn, const sq_shape_t *sh, int threads)
 {
     if (sh->Lq > SQ_MAX_DRAFTS) return fail(SQ_ERR_UNSUPPORTED, "%s: Lq = %d drafts, at most %d are supported", fn, sh->Lq, SQ_MAX_DRAFTS);
+    if (too_many(sh->B, threads)) return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", fn);
     return SQ_OK;
 }
 
@@ -1980,7 +1984,7 @@ int sq_tree_prepare(const sq_shape_t *sh, const int32_t *parents, const int32_t 
                     uint32_t *tree_mask, int32_t *positions, void *stream)
 {
     if (int rc = check_shape(sh, __func__, false)) return rc;
-    if (int rc = check_drafts(__func__, sh)) return rc;
+    if (int rc = check_drafts(__func__, sh, (sh->Lq + 63) / 64 * 64)) return rc;
     SQ_REQUIRE_PTR(parents);
     SQ_OPTIONAL_PTR(n_drafts);
     SQ_OPTIONAL_PTR(first_position);
@@ -2005,7 +2009,7 @@ int sq_tree_accept(const sq_shape_t *sh, const int32_t *parents, const int32_t *
                    const int32_t *seq_len, int32_t *n_accepted, int32_t *path, int32_t *next_token, int32_t *new_len, void *stream)
 {
     if (int rc = check_shape(sh, __func__, false)) return rc;
-    if (int rc = check_drafts(__func__, sh)) return rc;
+    if (int rc = check_drafts(__func__, sh, 64)) return rc;
     SQ_REQUIRE_PTR(parents);
     SQ_OPTIONAL_PTR(n_drafts);
     SQ_REQUIRE_PTR(tokens);
@@ -2040,7 +2044,9 @@ int sq_cache_commit(const sq_shape_t *sh, const sq_cache_t *cache, const int32_t
     SQ_REQUIRE_PTR(V);
     const size_t B = sh->B, rows = B * sh->H * sh->Lq;
     // (the grid: a workgroup for each page that may be touched, head and tensor)
-    if ((long long)B * sh->H * 2 > 0x7fffffffll / ((sh->Lq - 1) / cache->page_tokens + 2) || sh->Lq > sq::MAX_L)
+    const long long pages = sq::commit_pages(sh->Lq, cache->page_tokens);
+    if ((long long)B * sh->H * 2 > 0x7fffffffll / pages || sh->Lq > sq::MAX_L ||
+        too_many((long long)B * sh->H * 2 * pages, sq::commit_threads(sh->Lq, cache->page_tokens)))
         return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", __func__);
     Extent x[10] = {{"seq_len", seq_len, B * 4, false},
                     {"path", path, B * sh->Lq * 4, false},
@@ -2082,7 +2088,8 @@ int sq_cache_read(const sq_shape_t *sh, const sq_cache_t *cache, const int32_t *
     SQ_REQUIRE_PTR(K_out);
     SQ_REQUIRE_PTR(V_out);
     const size_t B = sh->B, rows = B * sh->H * sh->U;
-    if ((long long)B * sh->H * 2 > 0x7fffffffll / ((sh->U + 63) / 64)) return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", __func__);
+    const long long chunks = ((long long)sh->U + sq::READ_TOKENS - 1) / sq::READ_TOKENS;
+    if ((long long)B * sh->H * 2 > 0x7fffffffll / chunks || too_many((long long)B * sh->H * 2 * chunks, 256)) return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", __func__);
     Extent x[9] = {{"seq_len", seq_len, B * 4, false},
                    {"first", first, B * 4, false},
                    {"K_out", K_out, rows * sq::D * 2, true},
@@ -2145,7 +2152,7 @@ int sq_tree_attn_q8(const sq_shape_t *sh, int32_t T, const void *q, const void *
     const long long keys = (ranges ? sh->L : 0) + (cache ? (long long)cache->max_pages * cache->page_tokens : 0) + (K_draft ? T : 0);
     const sq::TreePlan plan = sq::tree_plan(sh->B, sh->H, sh->Lq, keys);
     if ((long long)sh->H * sh->L > 0x7fffffffll || (long long)sh->B * sh->H * sh->Lq > 0x3fffffffll || plan.units > 0x7fffffffll / (keys / 32 + 4 + sq::TREE_AHEAD) ||
-        T > sq::MAX_L || (tree_mask && T > sq::MAX_MASKED))
+        T > sq::MAX_L || (tree_mask && T > sq::MAX_MASKED) || too_many(plan.grid, 256))
         return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", __func__);
     const size_t B = sh->B, H = sh->H, blocks = (sh->L + sq::KV_BLOCK - 1) / sq::KV_BLOCK, rows = B * H * sh->Lq, drafts = B * H * T;
     Extent x[20] = {{"out", out, rows * sq::D * 2, true},

@@ -158,10 +158,10 @@ __global__ __launch_bounds__(256) void cache_commit_kernel(CommitArgs a)
 
 hipError_t launch_cache_commit(CommitArgs a, int B, hipStream_t s)
 {
-    a.per_seq = (a.T + a.P - 2) / a.P + 1;
+    a.per_seq = commit_pages(a.T, a.P);
     const long long blocks = (long long)B * a.per_seq * a.H * 2;
     if (blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
-    const int most = a.T < a.P ? a.T : a.P, threads = most < 16 ? (most * 16 + 63) / 64 * 64 : 256;
+    const int most = a.T < a.P ? a.T : a.P, threads = commit_threads(a.T, a.P);
     const bool stream = streams((size_t)B * a.H * a.T * 6 * D);
     auto *kernel = most > 32 ? (stream ? cache_commit_kernel<4, true> : cache_commit_kernel<4, false>)
                    : most > 16 ? cache_commit_kernel<2, false> : cache_commit_kernel<1, false>;
@@ -175,8 +175,6 @@ hipError_t launch_cache_commit(CommitArgs a, int B, hipStream_t s)
 // What bounds it is the memory.  Four sequences of up to 8192 tokens, 32 heads, pages of 16 (654 MB): 82 us on the pages that the call before read,
 // 98 on others, 6.7 TB/s (tokens a workgroup: 16 136, 32 98, 64 104, 128 112; 16 codes a lane, whose stores leave gaps in lines, 166; pages read past
 // the caches as well as rows written so 101 for 82).  500 tokens of 8 heads: the calling thread, 5.4.
-constexpr int READ_TOKENS = 32;
-
 template <bool STREAM>
 __global__ __launch_bounds__(256) void cache_read_kernel(ReadArgs a)
 {
@@ -228,7 +226,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(ReadArgs a)
 
 hipError_t launch_cache_read(ReadArgs a, int B, hipStream_t s)
 {
-    a.chunks = (a.U + READ_TOKENS - 1) / READ_TOKENS;
+    a.chunks = (int)(((long long)a.U + READ_TOKENS - 1) / READ_TOKENS);
     const long long blocks = (long long)B * a.H * 2 * a.chunks;
     if (blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
     auto *kernel = streams((size_t)B * a.H * a.U * 6 * D) ? cache_read_kernel<true> : cache_read_kernel<false>;

@@ -473,8 +473,11 @@ struct CommitArgs {
     int H, T, P, n_pages, max_pages;
     int per_seq;                   // (the launcher's) pages that a sequence can append to
 };
+inline int commit_pages(int T, int P) { return (int)(((long long)T + P - 2) / P + 1); }        // that a sequence can append to
+inline int commit_threads(int T, int P) { const int most = T < P ? T : P; return most < 16 ? (most * 16 + 63) / 64 * 64 : 256; }
 hipError_t launch_cache_commit(CommitArgs a, int B, hipStream_t s);
 
+constexpr int READ_TOKENS = 32;     // of a workgroup of cache_read_kernel
 struct ReadArgs {
     const uint8_t *K8, *V8;
     const float *k_scale, *v_scale;

@@ -113,6 +113,22 @@ def test_attention_refuses(sq):  # noqa: F811
     refused(sq, call(shape=sq.make_shape(2, 3, 100, 5, 28, 0, 0.1, d=64)), UNS, b"head dim")
 
 
+def test_grids_of_more_threads_than_32_bits(sq):  # noqa: F811
+    """Calls whose tensors would fit the memory, but not one launch: 2^32 threads and more are refused."""
+    UNS = sq.SQ_ERR_UNSUPPORTED
+    far = lambda i: i + 1 << 44  # noqa: E731
+    call = lambda name, shape, *args: getattr(sq.lib(), name)(C.byref(shape), *args, None)  # noqa: E731
+    deep = sq.make_shape(1 << 22, 1, 1, 1, 1024, 0, 1.0)
+    refused(sq, call("sq_tree_prepare", deep, far(0), None, None, None, far(1)), UNS, b"too large")
+    refused(sq, call("sq_tree_accept", sq.make_shape(1 << 26, 1, 1, 1, 2, 0, 1.0), far(0), None, far(1), far(2), None, far(3), far(4), None, None), UNS, b"too large")
+    many = cache(sq, n_pages=1)
+    refused(sq, call("sq_cache_commit", sq.make_shape(1 << 13, 1 << 9, 1, 1, 16, 0, 1.0), many, far(0), None, None, far(1), far(2)), UNS, b"too large")
+    refused(sq, call("sq_cache_read", sq.make_shape(1 << 12, 1 << 6, 1, 1, 1, 1 << 10, 1.0), many, None, far(0), far(1), far(2)), UNS, b"too large")
+    one = sq.make_shape(1 << 24, 1, 1, 1, 1, 0, 1.0)
+    none = [None] * 7
+    refused(sq, call("sq_tree_attn_q8", one, 1, far(0), *none, None, None, far(1), far(2), None, None, far(3), None, far(4), 1 << 50), UNS, b"too large")
+
+
 def test_the_plain_trees():
     parents = np.array([[-1, 0, 0, 1, 3, 9, 2, 5]])
     bits, positions = plain.prepare(parents, [8], [100])

@@ -359,13 +359,14 @@ DecodeQ8Ws carve_decode_q8(Carver &cv, const sq_shape_t *sh)
     return w;
 }
 
-// Attention of drafts: partial results of the shares, and which of them are a unit's.
+// Attention of drafts: partial results of the shares, and which of them are a unit's (of no keys, which is the plan with the most units).
 DecodeQ8Ws carve_tree(Carver &cv, const sq_shape_t *sh)
 {
     const sq::TreePlan p = sq::tree_plan(sh->B, sh->H, sh->Lq, 0);
     DecodeQ8Ws w{};
-    if (sq::tree_parts(p) == 0) return w;
-    w.part = cv.take<float>(sq::tree_parts(p) * sq::PART_STRIDE);
+    const size_t parts = sq::tree_parts(p, sh->Lq);
+    if (parts == 0) return w;
+    w.part = cv.take<float>(parts * sq::PART_STRIDE);
     w.info = cv.take<int2>((size_t)p.units);
     return w;
 }

@@ -493,6 +493,7 @@ constexpr int TREE_SHARED_UNITS = 1024;   // blocks of rows up to which they do:
 // Tiles of 32 keys that take as long as beginning and ending a block.  us with 4 / 12 / 20 / 32: 64 blocks of 32 rows, 6K keys 34.0 / 31.8 / 30.6 / 30.7;
 // 128 blocks of 64, 8K 68.4 / 64.7 / 63.0 / 65.0; 1024 blocks of a chain that sees itself alone 141 / 96.5 / 96.8 / 101.
 constexpr int TREE_AHEAD = 20;
+constexpr long long TREE_FEW_KEYS = 3ll << 20;   // keys of all blocks of 64 rows up to which a few blocks are cut in halves (see tree_plan)
 constexpr int MAX_MASKED = 32768;  // drafts with a mask: offsets into a sequence's have 32 bits
 struct TreeAttnArgs {
     const _Float16 *q;             // [B, H, G, T, D]
@@ -521,7 +522,8 @@ struct TreePlan {
     long long grid;
 };
 TreePlan tree_plan(int B, int H, int rows, long long keys);
-inline size_t tree_parts(const TreePlan &p) { return p.units > TREE_SHARED_UNITS ? 0 : (size_t)2 * TREE_SHARES * 16 * p.tiles; }   // rows of partial results
+// Rows of partial results, for blocks of up to 64 rows (of more than 32 rows a call may make either size, by its keys).
+inline size_t tree_parts(const TreePlan &p, int rows) { return p.units > TREE_SHARED_UNITS ? 0 : (size_t)2 * TREE_SHARES * 16 * (rows > 32 ? 4 : p.tiles); }
 hipError_t launch_tree_attn(TreeAttnArgs a, hipStream_t s);
 
 // Records the calling thread's error message (what sq_last_error returns) and hands back `code`.

@@ -347,10 +347,16 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
             return i2v{min(max(e.x, -MAX_L), MAX_L), ok ? min(max(e.y, 0), a.L) : 0};
         };
         if (groups > 4) {
-            for (int gi = wave; gi < groups; gi += 4) {
-                // (counts that sum to more than a head can have are cut, far from overflow)
-                const int n = min(wave_sum_i(in_bounds(range_of(gi), gi).y), MAX_L);
-                if (lane == 0) s_group[gi] = n;
+            for (int g0 = wave; g0 < groups; g0 += 16) {    // (four groups read side by side: 77 groups 49.9 -> 47.2 us)
+                i2v some[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) some[k] = range_of(g0 + 4 * k);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    // (counts that sum to more than a head can have are cut, far from overflow)
+                    const int n = min(wave_sum_i(in_bounds(some[k], g0 + 4 * k).y), MAX_L);
+                    if (lane == 0 && g0 + 4 * k < groups) s_group[g0 + 4 * k] = n;
+                }
             }
             __syncthreads();
         }
@@ -860,10 +866,14 @@ TreePlan tree_plan(int B, int H, int rows, long long keys)
 {
     TreePlan p{};
     // Rows of a block.  More of them share what a key costs (its codes to f16, its values turned); fewer make more blocks, which are begun and
-    // ended side by side.  us at 64 / 32 rows, 36K keys a head of which 1/8 and 2K user keys: 8 blocks of 64 29.3 / 23.1, 32 32.4 / 30.0, 64
-    // 45.6 / 43.3, 128 63.5 / 68.2, 256 99 / 113.  48 where that makes no more blocks: a quarter less of the softmax (36 rows 44.6 / 37.3).
+    // ended side by side, but read the keys again.  us at 64 / 32 rows, 36K keys a head of which 1/8 and 2K user keys: 8 blocks of 64 29.3 / 23.1,
+    // 32 32.4 / 30.0, 64 45.6 / 43.3, 128 63.5 / 68.2, 256 99 / 113; with 1/16, 1/8 and 0.3 kept: 64 blocks, 32K keys 33 / 28, 39 / 33, 53 / 51;
+    // 32, 128K 39 / 34, 53 / 53, 89 / 106; 64, 128K 53 / 51, 78 / 80, 141 / 169.  Up to 64 blocks, then, and 3M keys of all of them (what is
+    // kept is not known here).  48 where that makes no more blocks: a quarter less of the softmax (36 rows 44.6 / 37.3).
     const int at64 = (rows + 63) / 64;
-    p.tiles = rows <= 16 ? 1 : rows <= 32 || (long long)B * H * at64 <= 64 ? 2 : (rows + 47) / 48 == at64 ? 3 : 4;
+    const long long blocks64 = (long long)B * H * at64;
+    const bool few = blocks64 <= 64 && blocks64 * keys <= TREE_FEW_KEYS;
+    p.tiles = rows <= 16 ? 1 : rows <= 32 || few ? 2 : (rows + 47) / 48 == at64 ? 3 : 4;
     p.blocks = (rows + 16 * p.tiles - 1) / (16 * p.tiles);
     const long long units = (long long)B * H * p.blocks, most = (keys + QT - 1) / QT + 3;      // tiles: of three sources
     p.units = (int)std::min(units, 0x7fffffffll);

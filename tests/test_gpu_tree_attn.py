@@ -156,6 +156,16 @@ def test_sizes(B, H, G, T, L, C, user, page, mask, ragged):
     Problem(T * 31 + G, B, H, G, T, L, C, user=user, page=page, mask=mask, ragged=ragged).run()
 
 
+@pytest.mark.parametrize("B,H,G,T,mask,ragged", [(1, 2, 4, 16, "tree", False), (2, 3, 4, 9, "any", True), (3, 2, 3, 25, None, True), (2, 1, 8, 30, "tree", True)])
+def test_tables_of_many_pages(B, H, G, T, mask, ragged):
+    """Room for 2M tokens a sequence, the most that there can be, few of them there: the most keys that there can be choose the size of a block, 48 or 64 rows here."""
+    p = Problem(B * T, B, H, G, T, L=700, C=20, user=90, mask=mask, ragged=ragged)
+    p.table = np.concatenate([p.table, np.full((B, (1 << 21) // 16 - p.table.shape[1]), -1, np.int32)], 1)
+    p.run()
+    p.held[-1] = 5000                                           # (pages that are none have no keys)
+    p.run()
+
+
 @pytest.mark.parametrize("mask", ["tree", None, "any"])
 @pytest.mark.parametrize("sources", ["drafts", "context", "cache", "context+cache", "context+drafts", "cache+drafts"])
 def test_sources(sources, mask):

@@ -662,7 +662,8 @@ int sq_tree_prepare(const sq_shape_t *shape, const int32_t *parents, const int32
 /*
  * Attention of T drafts of every sequence: exact softmax attention of each draft's query heads over ONE kept set of the fixed context
  * per (sequence, K/V head), the seq_len[b] tokens of its sequence in the paged cache, and the drafts that the draft sees, one softmax
- * over the union; fp32 accumulation, the probabilities rounded to f16 (11 bits, down to 2^-22 of the largest) where they multiply values.
+ * over the union; fp32 accumulation, the probabilities times their values' scales rounded to f16 (11 bits, down to 2^-22 of the row's largest
+ * such product, of which less than 2^-33 is lost) where they multiply codes.
  * Lq of the shape is the number of query rows per K/V head, Lq = G * T for G query heads (1 .. 64) per K/V head: the shape that scored
  * them (logits [B,H,Lq,C]).
  * In:  q f16 [B,H*G,T,d] (q_out of sq_head_norm_rotate);
@@ -675,7 +676,8 @@ int sq_tree_prepare(const sq_shape_t *shape, const int32_t *parents, const int32
  *      tree_mask u32 [B,T,ceil(T/32)]: draft t sees draft j if bit j of row t is set (any mask: it need be no tree, and a row may be
  *      empty); NULL: a chain, draft t sees drafts 0 .. t -- a prompt behind the context and the cache, of any length.  Bits from n_drafts[b] on
  *      are not looked at.  It must be NULL where K_draft is, and T at most 32768 where it is not.
- *      One of the three sources at least.  All scales must be positive and normal, finite, and leave the scores in fp32's range.
+ *      One of the three sources at least.  Scales of keys: any finite ones that leave the scores in fp32's range.  Scales of values: from 0
+ *      to 2^40; those below 2^-40 count as 2^-40 (values of less than 2^-31 either way, where f16 has steps of 2^-24).
  *      Input outside this contract never faults and is not reported: at most C ranges are used, entries with count <= 0 are skipped, nothing
  *      outside [0, L) is read, a page that is none has no keys; which keys such a row then attends to is not specified.
  * Out: out f16 [B,H*G,T,d]; lse f32 [B,H*G,T], or NULL.  A row without visible keys gets out = 0 and lse = -inf.  Rows of drafts from

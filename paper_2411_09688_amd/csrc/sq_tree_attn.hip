@@ -10,8 +10,12 @@
 //   t = S * (key's scale * sm_scale * log2 e) + log2(value's scale),   M: a reference near the maximum of t,   p = 2^(t - M + 8)
 //   O^T [128 x 16 TILES]    += V^T P^T  codes to f16 (exact), P rounded to f16
 //   l                       += p / value's scale                       (the unrounded p)
-// With the value's scale in the exponent P needs no factor, whatever the scales are: it is at most 2^15, and has its 11 bits down to 2^-22
-// of the largest.  out = O / l, log-sum-exp = (M - 8 + log2 l) ln 2.
+// With the value's scale in the exponent P needs no factor: it is at most 2^15, and has its 11 bits down to 2^-22 of the largest.
+// out = O / l, log-sum-exp = (M - 8 + log2 l) ln 2.
+// The sum takes p / scale from p, so that scales must not lie too far apart: those below 2^-40 count as 2^-40 (LEAST_SCALE; a value is then off by
+// less than 448 * 2^-40 < 2^-31, where f16 has steps of 2^-24), and above 2^40 is outside the contract.  Within 2^80 of one another a key drops
+// out of the sum (its p, or the factor by which a reference moves, below fp32's 2^-126) only where its weight is under 2^-46 of the largest: 2^23
+// such keys are one part in 2^23.  And no term overflows: 2^15 * 2^40 a key.
 //
 // What bounds it, and the two launches on the GPU (us; 8 K/V heads of 4 query heads):
 //   4 heads of 8 drafts, 4K + 128 keys, 1/4 kept     8.1 + 4.0   the launches, and a search, a prologue and a tile whose reads come from HBM
@@ -35,6 +39,7 @@ constexpr int MAX_GROUPS = SELECT_MAX_C / GROUP;
 // The reference M of a column follows its largest t once that is more than 2^SLACK times it: of 64 columns one finds a new maximum in most
 // tiles, and moving a reference costs as much as half a tile.
 constexpr float LIFT = 8.0f, SLACK = 7.0f;   // p is at most 2^15
+constexpr float LEAST_SCALE = 0x1p-40f;      // of values
 
 // 64 keys of a wave: where they stand (as in KeyList), and what their scales make of a score and of a probability.
 template <bool WIDE>
@@ -486,7 +491,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
             };
             auto list_scales = [&](int buf) {
                 const int lane = lane_here();
-                const float v = seen_next >> lane & 1u ? vs : 1.0f;         // (a slot without a key: not looked at, but for this)
+                // (a slot without a key: not looked at, but for this.  A comparison in fmaxf's place: 50 registers more in memory at 64 rows, chain 302 -> 337 us)
+                const float v = seen_next >> lane & 1u ? fmaxf(vs, LEAST_SCALE) : 1.0f;
                 s_list[wave][buf].mul[lane] = ks * a.scale;
                 s_list[wave][buf].add[lane] = __builtin_amdgcn_logf(v);
                 s_list[wave][buf].inv[lane] = __builtin_amdgcn_rcpf(v);

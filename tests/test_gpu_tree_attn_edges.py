@@ -1,0 +1,74 @@
+"""sq_tree_attn_q8 where its arithmetic has least room: scales of values at both ends of what they may be."""
+import numpy as np
+import pytest
+import torch
+
+import drafts_reference as plain
+import q8_reference as ref
+from test_gpu_tree_attn import SCALE, Problem
+
+pytestmark = pytest.mark.gpu
+
+# Scales of values below 2^-40 count as 2^-40: a value, at most 448 times its scale, is then off by less than 448 * 2^-40 < 2^-31, and so is an
+# output, a mean of values.
+LEAST, OFF = 2.0 ** -40, 2.0 ** -31
+
+
+def check(p):
+    """Outputs where the oracle's are within f16's range, and all log-sum-exps."""
+    out, lse = p.out.cpu().numpy().astype(np.float64), p.lse.cpu().numpy().astype(np.float64)
+    for b in range(p.B):
+        for h in range(p.H):
+            keys, n = p.keys(b, h)
+            keys = [(k, v, seen, np.maximum(s, LEAST)) for k, v, seen, s in keys]
+            rows = p.q[b, h * p.G:h * p.G + p.G, :n].transpose(1, 0, 2).reshape(n * p.G, 128).astype(np.float64)
+            o, z, off, off_z = plain.attend(rows, keys, SCALE)
+            got = out[b, h * p.G:h * p.G + p.G, :n].transpose(1, 0, 2).reshape(n * p.G, 128)
+            got_z = lse[b, h * p.G:h * p.G + p.G, :n].T.reshape(n * p.G)
+            assert np.array_equal(np.isneginf(z), np.isneginf(got_z)), (b, h)
+            ok = np.isfinite(z)
+            assert np.all(np.abs(got_z - z)[ok] <= off_z[ok]), (b, h, got_z[:4], z[:4])
+            near = np.abs(o) + off < 65504
+            assert np.all(np.abs(got - o)[near] <= off[near] + OFF), (b, h)
+
+
+@pytest.mark.parametrize("least", [0.0, 2.0 ** -126, 2.0 ** -120, 2.0 ** -113, 2.0 ** -41])
+@pytest.mark.parametrize("share", [1.0, 0.5])
+@pytest.mark.parametrize("G,T", [(2, 9), (4, 40), (8, 90)])
+def test_small_scales_of_values(least, share, G, T):
+    """Pages and blocks that hold next to nothing, beside ordinary ones or alone; keys' scales of zero among them."""
+    p = Problem(T, 2, 2, G, T, L=900, C=25, keep=0.5, user=130, page=32)
+    for a in (p.vs, p.cvs):
+        a[p.rng.random(a.shape) < share] = least
+    p.ks[:, ::5] = 0
+    p.upload().call()
+    check(p)
+
+
+def test_a_wave_of_small_scales_beside_waves_of_ordinary_ones():
+    """Of 512 kept keys the first quarter, one wave's, stands in blocks of a scale of 2^-120."""
+    p = Problem(31, 1, 2, 4, 12, L=512, C=4, user=0, drafts=False)
+    p.ranges[:] = [[[[0, 128], [128, 128], [256, 128], [384, 128]]] * 2]
+    p.nr[:], p.nk[:] = 4, 512
+    p.vs[:, :2] = 2.0 ** -120
+    p.upload().call()
+    check(p)
+
+
+@pytest.mark.parametrize("least", [0.0, 2.0 ** -126, 2.0 ** -64])
+def test_the_sum_keeps_keys_of_small_scales_beside_one_of_the_largest(least):
+    """4096 keys, each with 2^-7 of the probability of a key whose scale is 2^40 and whose codes are zeros: 32 times its weight in all."""
+    p = Problem(32, 1, 1, 1, 5, L=4096 + 64, C=2, user=0, drafts=False)
+    p.ranges[:] = [[[[0, 1], [64, 4096]]]]
+    p.nr[:], p.nk[:] = 2, 4097
+    p.q[:] = 1
+    p.K8[:] = 0
+    p.K8[0, 0] = ref.encode(np.full(128, 1.0))
+    p.ks[:] = 7 * np.log(2) / (128 * SCALE)                     # (the first key's score is 7 ln 2, the others' 0)
+    p.ks = p.ks.astype(np.float32).astype(np.float64)
+    p.V8[0, 0] = 0
+    p.vs[:] = least
+    p.vs[0, 0] = 2.0 ** 40
+    p.upload().call()
+    check(p)
+    assert np.abs(p.lse.cpu().numpy() - np.log(128 + 4096)).max() < 1e-3 and (p.out == 0).all()

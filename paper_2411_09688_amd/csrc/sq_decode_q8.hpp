@@ -67,12 +67,6 @@ __device__ __forceinline__ void transpose4(uint32_t &a, uint32_t &b, uint32_t &c
     d = __builtin_amdgcn_perm(u1, t1, 0x07060302u);
 }
 
-__device__ __forceinline__ h8 codes_f16(uint32_t lo, uint32_t hi)
-{
-    const h2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
-    const h2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
-    return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
 __device__ __forceinline__ b8 codes_bf16(uint32_t lo, uint32_t hi)
 {
     const b2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);

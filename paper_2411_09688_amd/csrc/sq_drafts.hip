@@ -170,11 +170,12 @@ hipError_t launch_cache_commit(CommitArgs a, int B, hipStream_t s)
 }
 
 // Pages back to rows: READ_TOKENS tokens of a head and tensor per workgroup, 8 codes a lane, 16 lanes a token, so that a store of a wave
-// fills lines.  A code times its scale is rounded to f16 once.
+// fills lines.  A code times its scale is rounded to f16 once: by the conversion itself where the scale is a power of two, else as
+// a product.
 //
 // What bounds it is the memory.  Four sequences of up to 8192 tokens, 32 heads, pages of 16 (654 MB): 82 us on the pages that the call before read,
 // 98 on others, 6.7 TB/s (tokens a workgroup: 16 136, 32 98, 64 104, 128 112; 16 codes a lane, whose stores leave gaps in lines, 166; pages read past
-// the caches as well as rows written so 101 for 82).  500 tokens of 8 heads: the calling thread, 5.4.
+// the caches as well as rows written so 101 for 82; products in fp32 and a conversion, with the test of the scales, 102 for 100 on cold pages).  500 tokens of 8 heads: the calling thread, 5.4.
 template <bool STREAM>
 __global__ __launch_bounds__(256) void cache_read_kernel(ReadArgs a)
 {
@@ -207,20 +208,33 @@ __global__ __launch_bounds__(256) void cache_read_kernel(ReadArgs a)
             scale[i] = 0.0f;
         }
     }
+    auto store = [&](int i, h8 y) {
+        const int u = chunk * READ_TOKENS + i * 16 + g;
+        if (u < n) store_once<STREAM>(reinterpret_cast<h8 *>(out + (size_t)u * D + 8 * j), y);
+    };
+    uint32_t other = 0;                                     // (not zero: a scale among them is negative, infinite or no power of two)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int u = chunk * READ_TOKENS + i * 16 + g;
-        if (u >= n) break;
-        h8 y;
+        const uint32_t f = __builtin_bit_cast(uint32_t, scale[i]);
+        other |= (f | (f + 0x800000u)) & 0x807fffffu;
+    }
+    if (__builtin_expect(__all(other == 0u), 1)) {
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            const f2v lo = __builtin_amdgcn_cvt_pk_f32_fp8(c[i][w], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(c[i][w], true);
-            y[4 * w] = (_Float16)(lo.x * scale[i]);
-            y[4 * w + 1] = (_Float16)(lo.y * scale[i]);
-            y[4 * w + 2] = (_Float16)(hi.x * scale[i]);
-            y[4 * w + 3] = (_Float16)(hi.y * scale[i]);
+        for (int i = 0; i < N; ++i) store(i, codes_f16(c[i].x, c[i].y, scale[i]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            h8 y;
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const f2v lo = __builtin_amdgcn_cvt_pk_f32_fp8(c[i][w], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(c[i][w], true);
+                y[4 * w] = (_Float16)product_unbiased(lo.x, scale[i]);
+                y[4 * w + 1] = (_Float16)product_unbiased(lo.y, scale[i]);
+                y[4 * w + 2] = (_Float16)product_unbiased(hi.x, scale[i]);
+                y[4 * w + 3] = (_Float16)product_unbiased(hi.y, scale[i]);
+            }
+            store(i, y);
         }
-        store_once<STREAM>(reinterpret_cast<h8 *>(out + (size_t)u * D + 8 * j), y);
     }
 }
 

@@ -46,6 +46,15 @@ __device__ __forceinline__ int exponent_holding(float scale)
     return min(max(e, E4M3_EXP_MIN), E4M3_EXP_MAX);
 }
 
+// Eight codes to f16, exact; times a power of two (a normal one, or 0 as some power far below f16's least value), rounded once, past f16's end to
+// an infinity.
+__device__ __forceinline__ h8 codes_f16(uint32_t lo, uint32_t hi, float scale = 1.0f)
+{
+    const h2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, true);
+    const h2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, true);
+    return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
 // |x| as bits for a maximum over a block: infinities and NaN count as nothing.
 __device__ __forceinline__ uint32_t finite_abs(float x)
 {
@@ -78,6 +87,17 @@ __device__ __forceinline__ uint32_t e4m3_rescale4(uint32_t w, float f)
 {
     const f2v a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
     return e4m3_pair<true>(b.x * f, b.y * f, e4m3_pair<false>(a.x * f, a.y * f, 0u));
+}
+
+// x * f in fp32 so that rounding it once more, to 12 significant bits or fewer, gives what rounding the product would have given: where it lies on
+// a border of the coarser rounding (its low 12 bits are zero) and is not the product itself, the neighbour on the product's side is taken.  (The
+// error e is exact unless the product is near fp32's least values.)
+__device__ __forceinline__ float product_unbiased(float x, float f)
+{
+    const float p = x * f, e = fmaf(x, f, -p);
+    const uint32_t b = __builtin_bit_cast(uint32_t, p);
+    const uint32_t towards = (__builtin_bit_cast(uint32_t, e) ^ b) >> 31 ? b - 1u : b + 1u;
+    return (b & 0xfffu) == 0u && fabsf(e) > 0.0f && (b & 0x7f800000u) != 0x7f800000u ? __builtin_bit_cast(float, towards) : p;
 }
 
 // Double to float so that rounding the float once more, to 12 significant bits or fewer, gives what rounding the double

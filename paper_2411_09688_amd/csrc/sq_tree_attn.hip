@@ -605,10 +605,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
             const int words = (a.T + 31) / 32;
             const global<uint32_t> mask = uniform(a.mask + (size_t)b * a.T * words);
             // (in LDS, where the results' maxima stand later: registers are short here)
-            int *const s_draft = reinterpret_cast<int *>(s_ml[0][wave]);    // drafts of the columns
+            float *const s_draft = s_ml[0][wave];           // drafts of the columns, as a float's bits
 #pragma unroll
-            for (int n = 0; n < TILES; ++n) s_draft[n * 16 + c16] = min(row0 + n * 16 + c16, end_row - 1) / a.G;
+            for (int n = 0; n < TILES; ++n) s_draft[n * 16 + c16] = __builtin_bit_cast(float, min(row0 + n * 16 + c16, end_row - 1) / a.G);
             wave_lds_sync();
+            auto draft_of = [&](int n) { return __builtin_bit_cast(int, s_draft[n * 16 + c16]); };
             auto row_at = [&](int key) { return (uint32_t)min(key, n_drafts - 1) * (uint32_t)(D * sizeof(_Float16)); };
             // Values go to LDS past the registers: with them on their way in registers, 128 of which hold the output, some were kept in memory.
             char *const s_v = s_mem + V_AT + wave * V_TILE;
@@ -667,7 +668,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                     float x[PAIR][8];
 #pragma unroll
                     for (int n = 0; n < PAIR; ++n) {
-                        const int d = s_draft[(n0 + n) * 16 + c16], own = d - key0;         // a chain: keys up to the draft itself
+                        const int d = draft_of(n0 + n), own = d - key0;         // a chain: keys up to the draft itself
                         uint32_t sees = own >= 31 ? ~0u : own < 0 ? 0u : (2u << own) - 1u;
                         if (a.mask) sees = mask[(uint32_t)(d * words + t)];
                         sees &= there;
@@ -729,7 +730,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                     if (!__any(any)) continue;
 #pragma unroll
                     for (int n = 0; n < TILES; ++n) {
-                        const int d = s_draft[n * 16 + c16];
+                        const int d = draft_of(n);
                         bool seen = key <= d;
                         if (a.mask) seen = mask[(uint32_t)(d * words + (key >> 5))] >> (key & 31) & 1u;
                         if (seen)
@@ -746,6 +747,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
         // its columns, i = 0 .. 3.
         const TreeAttnArgs &r = arguments();
         const bool whole = lo == 0 && hi == total;
+        wave_lds_sync();                                    // (s_draft has been read)
         auto out = [&](int buffer, int row, int place) {    // four dimensions of a row
             return reinterpret_cast<f4 *>(s_mem) + (buffer * 16 * TILES + row) * (D / 4) + (place ^ (row & 15));
         };

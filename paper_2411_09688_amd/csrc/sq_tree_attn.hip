@@ -615,6 +615,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
             char *const s_v = s_mem + V_AT + wave * V_TILE;
             const uint32_t lds_v = uniform((int)(uint32_t)(size_t)(__attribute__((address_space(3))) void *)s_v);
             auto load_v = [&](int t) {                      // rows 4 i + g4, 16 bytes a lane, one after the other
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (the values in their place have been read)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_v + (uint32_t)(i * 1024)),
@@ -683,8 +684,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
                     fold_scores<PAIR>(st.m + n0, st.l + n0, st.o + n0, x, one, pr + n0);
                     if (Q_IN_LDS) __builtin_amdgcn_sched_barrier(0);
                 }
-                // the eight reads of the next keys may still be on their way, the values must not be
-                asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+                // (for the values, which the compiler does not count; the next keys have been waited for already, with the words of the mask)
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 h8 v[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const h8 *>(s_v + (4 * g4 + (i < 4 ? i : 12 + i)) * (D * 2) + 16 * c16);

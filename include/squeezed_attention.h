@@ -685,7 +685,8 @@ int sq_tree_prepare(const sq_shape_t *shape, const int32_t *parents, const int32
  *      A key that a row does not see has no influence on it, whatever its rows hold; infinities and NaN among the values that it sees, and scores
  *      of NaN or +inf, make it not finite, and a score of -inf has no weight (a row of nothing else counts as one without keys).
  *      The keys of all (sequence, head)s are divided into equal shares, so that the order of a row's sums, and with it its last bits, follows
- *      from the number of keys of all of them.
+ *      from the number of keys of all of them, and from the most that there could be: L, max_pages, page_tokens and T decide how many rows and
+ *      shares the work has (a table with much more room than its sequences use costs a small call up to 40 % more).
  * Workspace: sq_workspace_bytes(shape, SQ_CALL_TREE_ATTN_Q8).
  */
 int sq_tree_attn_q8(const sq_shape_t *shape, int32_t T, const void *q, const void *K8, const void *V8, const float *k_scale,

@@ -878,7 +878,10 @@ TreePlan tree_plan(int B, int H, int rows, long long keys)
     // ended side by side, but read the keys again.  us at 64 / 32 rows, 36K keys a head of which 1/8 and 2K user keys: 8 blocks of 64 29.3 / 23.1,
     // 32 32.4 / 30.0, 64 45.6 / 43.3, 128 63.5 / 68.2, 256 99 / 113; with 1/16, 1/8 and 0.3 kept: 64 blocks, 32K keys 33 / 28, 39 / 33, 53 / 51;
     // 32, 128K 39 / 34, 53 / 53, 89 / 106; 64, 128K 53 / 51, 78 / 80, 141 / 169.  Up to 64 blocks, then, and 3M keys of all of them (what is
-    // kept is not known here).  48 where that makes no more blocks: a quarter less of the softmax (36 rows 44.6 / 37.3).
+    // kept is not known here).  Of a cache the room that its table has counts, since what it holds is not known here either: with room for 2M tokens and
+    // 512 held, blocks of 64 rows are made where 32 were better (8 blocks 27 / 22 us, 16 29.6 / 24.1, 32 32 / 28, 64 over the cache alone 28 / 20; four blocks over 4K keys in shares
+    // and not in parts of their own 12.7 / 11.5); counted as 16K at most, caches that are full would have 32 where 64 are better, which costs more
+    // (128K held: 8 blocks 94 / 68, 16 174 / 117, 32 304 / 221).  48 where that makes no more blocks: a quarter less of the softmax (36 rows 44.6 / 37.3).
     const int at64 = (rows + 63) / 64;
     const long long blocks64 = (long long)B * H * at64;
     const bool few = blocks64 <= 64 && blocks64 * keys <= TREE_FEW_KEYS;

@@ -674,8 +674,8 @@ int sq_tree_prepare(const sq_shape_t *shape, const int32_t *parents, const int32
  *      K_draft, V_draft f16 [B,H,T,d] (k_out and v_out of sq_head_norm_rotate), the drafts' own keys and values; both may be NULL: the
  *      queries see the context and the cache only.
  *      tree_mask u32 [B,T,ceil(T/32)]: draft t sees draft j if bit j of row t is set (any mask: it need be no tree, and a row may be
- *      empty); NULL: a chain, draft t sees drafts 0 .. t -- a prompt behind the context and the cache, of any length.  Bits from n_drafts[b] on
- *      are not looked at.  It must be NULL where K_draft is, and T at most 32768 where it is not.
+ *      empty); NULL: a chain, draft t sees drafts 0 .. t -- a prompt behind the context and the cache, of up to 2^21 drafts.  Bits from
+ *      n_drafts[b] on are not looked at.  It must be NULL where K_draft is, and T at most 32768 where it is not.
  *      One of the three sources at least.  Scales of keys: any finite ones that leave the scores in fp32's range.  Scales of values: from 0
  *      to 2^40; those below 2^-40 count as 2^-40 (values of less than 2^-31 either way, where f16 has steps of 2^-24).
  *      Input outside this contract never faults and is not reported: at most C ranges are used, entries with count <= 0 are skipped, nothing
@@ -687,6 +687,8 @@ int sq_tree_prepare(const sq_shape_t *shape, const int32_t *parents, const int32
  *      The keys of all (sequence, head)s are divided into equal shares, so that the order of a row's sums, and with it its last bits, follows
  *      from the number of keys of all of them, and from the most that there could be: L, max_pages, page_tokens and T decide how many rows and
  *      shares the work has (a table with much more room than its sequences use costs a small call up to 40 % more).
+ * Limits: H * L below 2^31 and B * H * Lq below 2^30; 2^24 blocks of rows (16 to 64 of a (sequence, head) each), and 2^35 pairs of such a block and
+ *      32 keys that there could be.
  * Workspace: sq_workspace_bytes(shape, SQ_CALL_TREE_ATTN_Q8).
  */
 int sq_tree_attn_q8(const sq_shape_t *shape, int32_t T, const void *q, const void *K8, const void *V8, const float *k_scale,

@@ -2152,7 +2152,7 @@ int sq_tree_attn_q8(const sq_shape_t *sh, int32_t T, const void *q, const void *
     if (!ranges && !cache && !K_draft) return fail(SQ_ERR_INVALID_ARG, "%s: neither ranges of a fixed context nor a cache nor drafts' keys", __func__);
     const long long keys = (ranges ? sh->L : 0) + (cache ? (long long)cache->max_pages * cache->page_tokens : 0) + (K_draft ? T : 0);
     const sq::TreePlan plan = sq::tree_plan(sh->B, sh->H, sh->Lq, keys);
-    if ((long long)sh->H * sh->L > 0x7fffffffll || (long long)sh->B * sh->H * sh->Lq > 0x3fffffffll || plan.units > 0x7fffffffll / (keys / 32 + 4 + sq::TREE_AHEAD) ||
+    if ((long long)sh->H * sh->L > 0x7fffffffll || (long long)sh->B * sh->H * sh->Lq > 0x3fffffffll || plan.units > sq::TREE_MOST_TILES / (keys / 32 + 4 + sq::TREE_AHEAD) ||
         T > sq::MAX_L || (tree_mask && T > sq::MAX_MASKED) || too_many(plan.grid, 256))
         return fail(SQ_ERR_UNSUPPORTED, "%s: problem too large", __func__);
     const size_t B = sh->B, H = sh->H, blocks = (sh->L + sq::KV_BLOCK - 1) / sq::KV_BLOCK, rows = B * H * sh->Lq, drafts = B * H * T;

@@ -494,6 +494,8 @@ constexpr int TREE_SHARED_UNITS = 1024;   // blocks of rows up to which they do:
 // 128 blocks of 64, 8K 68.4 / 64.7 / 63.0 / 65.0; 1024 blocks of a chain that sees itself alone 141 / 96.5 / 96.8 / 101.
 constexpr int TREE_AHEAD = 20;
 constexpr long long TREE_FEW_KEYS = 3ll << 20;   // keys of all blocks of 64 rows up to which a few blocks are cut in halves (see tree_plan)
+// Tiles of all blocks: a minute's work.  (They are counted through only where workgroups share them: up to 1024 blocks of 6M keys, 2^28.)
+constexpr long long TREE_MOST_TILES = 1ll << 35;
 constexpr int MAX_MASKED = 32768;  // drafts with a mask: offsets into a sequence's have 32 bits
 struct TreeAttnArgs {
     const _Float16 *q;             // [B, H, G, T, D]

@@ -5,6 +5,8 @@ import torch
 
 import drafts_reference as plain
 import q8_reference as ref
+from paper_2411_09688_amd import binding as sq
+from test_gpu_q8_rows import cu
 from test_gpu_tree_attn import SCALE, Problem
 
 pytestmark = pytest.mark.gpu
@@ -72,3 +74,32 @@ def test_the_sum_keeps_keys_of_small_scales_beside_one_of_the_largest(least):
     p.upload().call()
     check(p)
     assert np.abs(p.lse.cpu().numpy() - np.log(128 + 4096)).max() < 1e-3 and (p.out == 0).all()
+
+
+def test_a_batch_of_chains_behind_the_widest_tables():
+    """8 prompts of 2048 tokens, 128 heads, and room for 2M tokens each: more tiles that there could be than 31 bits count, in 32768 blocks of their own."""
+    B, H, G, T, P = 8, 8, 16, 2048, 16
+    small = Problem(40, B, H, 1, 1, user=50, page=P, drafts=False)
+    table = np.full((B, (1 << 21) // P), -1, np.int32)
+    table[:, :small.table.shape[1]] = small.table
+    g = torch.Generator(device="cuda").manual_seed(40)
+    q = torch.randn(B, H * G, T, 128, generator=g, device="cuda", dtype=torch.float16)
+    K, V = (torch.randn(B, H, T, 128, generator=g, device="cuda", dtype=torch.float16) for _ in range(2))
+    n = np.array([T, 1900, 64, 1, 0, T, T - 1, 777], np.int32)
+    sh = sq.make_shape(B, H, 1, 1, G * T, 0, SCALE)
+    blocks = B * H * (G * T // 64)
+    assert blocks * (((1 << 21) + T) // 32) > 0x7fffffff and sq.workspace_bytes(sh, sq.SQ_CALL_TREE_ATTN_Q8) == 0
+    cache = sq.make_cache(cu(small.cK).view(sq.F8), cu(small.cV).view(sq.F8), cu(small.cks.astype(np.float32)), cu(small.cvs.astype(np.float32)), cu(table))
+    out, lse = torch.full_like(q, 9), torch.full((B, H * G, T), 9.0, device="cuda")
+    sq.sq_tree_attn_q8(sh, T, q, *[None] * 7, cache, cu(small.held), K, V, None, cu(n), out, lse, None)
+    for b, h, t in ((0, 0, 0), (0, 7, 2047), (1, 3, 1899), (2, 5, 63), (3, 1, 0), (5, 2, 1024), (6, 6, 2046), (7, 7, 776)):
+        held = np.arange(small.held[b])
+        at = (small.table[b, held // P], h, held % P)
+        keys = [(ref.VALUES[small.cK[at]] * small.cks[at[:2]][:, None], ref.VALUES[small.cV[at]] * small.cvs[at[:2]][:, None], None, small.cvs[at[:2]]),
+                (K[b, h, :t + 1].cpu().numpy().astype(np.float64), V[b, h, :t + 1].cpu().numpy().astype(np.float64), None, np.ones(t + 1))]
+        rows = q[b, h * G:h * G + G, t].cpu().numpy().astype(np.float64)
+        o, z, off, off_z = plain.attend(rows, keys, SCALE)
+        got, got_z = (x[b, h * G:h * G + G, t].cpu().numpy().astype(np.float64) for x in (out, lse))
+        assert np.all(np.abs(got - o) <= off) and np.all(np.abs(got_z - z) <= off_z), (b, h, t)
+    for b in range(B):
+        assert (out[b, :, int(n[b]):] == 9).all() and (lse[b, :, int(n[b]):] == 9).all()

@@ -1,4 +1,5 @@
-"""sq_tree_attn_q8 where its arithmetic has least room: scales of values at both ends of what they may be."""
+"""sq_tree_attn_q8 where its arithmetic and its division have least room: scales of values at both ends of what they may be, drafts that are not finite in
+blocks of every size, as many blocks as workgroups share, the widest tables."""
 import numpy as np
 import pytest
 import torch
@@ -103,3 +104,93 @@ def test_a_batch_of_chains_behind_the_widest_tables():
         assert np.all(np.abs(got - o) <= off) and np.all(np.abs(got_z - z) <= off_z), (b, h, t)
     for b in range(B):
         assert (out[b, :, int(n[b]):] == 9).all() and (lse[b, :, int(n[b]):] == 9).all()
+
+
+# For each size of a block of rows: heads a K/V head, drafts, room of the table (the most keys that there could be choose 48 and 64 rows).
+SIZES = {16: (2, 8, 0), 32: (2, 16, 0), 48: (4, 12, 1 << 21), 64: (3, 20, 1 << 21), "64, three of them": (4, 40, 1 << 21), "64, by their number": (8, 90, 0)}
+
+
+def of_size(size, seed, **kw):
+    G, T, room = SIZES[size]
+    p = Problem(seed, 3 if size == "64, by their number" else 2, 2, G, T, **{**dict(L=300, C=10, user=50, mask="any"), **kw})
+    if room and p.held is not None:
+        p.table = np.concatenate([p.table, np.full((p.B, room // p.page - p.table.shape[1]), -1, np.int32)], 1)
+    return p
+
+
+def rows_of(p, x, b, h):
+    """[B, H*G, T, ..] -> [(t, g), ..] of a K/V head."""
+    x = x.cpu().numpy().astype(np.float64)[b, h * p.G:h * p.G + p.G]
+    return np.swapaxes(x, 0, 1).reshape(p.T * p.G, *x.shape[2:])
+
+
+@pytest.mark.parametrize("alone", [False, True])
+@pytest.mark.parametrize("what", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("size", SIZES)
+def test_drafts_keys_that_are_not_finite(size, what, alone):
+    """A score of +inf or NaN makes the rows that see it not finite; one of -inf has no weight, and a row of nothing else counts as one without keys."""
+    p = of_size(size, 50, **(dict(L=0, C=0, user=16) if alone else {}))
+    if alone:
+        p.held[:] = 0
+    nothing = 0
+    odd = [0, 3, p.T - 1]
+    p.bits[:, 2] = False
+    p.bits[:, 2, odd[1]] = True                                 # (a row that sees one such key alone)
+    p.mask = plain.words(p.bits)
+    for j in odd:
+        p.Kd[:, :, j, 7 + j % 3] = what
+    assert (p.q != 0).all()
+    p.upload().call()
+    p.Kd = np.where(np.isfinite(p.Kd), p.Kd, 0)                 # (for the oracle: such keys are not seen, or the row is not looked at)
+    for b in range(p.B):
+        for h in range(p.H):
+            q, out, lse = p.q[b, h * p.G:h * p.G + p.G].transpose(1, 0, 2).reshape(p.T * p.G, 128).astype(np.float64), rows_of(p, p.out, b, h), rows_of(p, p.lse, b, h)
+            seen = np.repeat(p.bits[b], p.G, 0)
+            up = np.zeros_like(seen[:, 0])
+            for j in odd:
+                up |= seen[:, j] & (np.isnan(what) | (q[:, 7 + j % 3] * np.sign(what) > 0))
+                seen[:, j] = False
+            assert up.any() and not up.all()
+            assert not np.isfinite(out[up]).any() and not np.isfinite(lse[up]).any()
+            keys = [(k, v, seen if s is not None else None, sv) for k, v, s, sv in p.keys(b, h)[0]]
+            o, z, off, off_z = plain.attend(q, keys, SCALE)
+            fine, some = ~up, ~up & np.isfinite(z)
+            assert np.all(np.abs(out - o)[fine] <= off[fine]) and np.array_equal(np.isneginf(lse[fine]), np.isneginf(z[fine]))
+            assert np.all(np.abs(lse[some] - z[some]) <= off_z[some])
+            assert (out[np.isneginf(z) & fine] == 0).all()
+            nothing += (np.isneginf(z) & fine)[2 * p.G:3 * p.G].sum()
+    assert (nothing > 0) == (alone and not np.isnan(what))
+
+
+@pytest.mark.parametrize("what", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("size", SIZES)
+def test_drafts_values_that_are_not_finite(size, what):
+    """They reach the rows that see them, in their dimension, and nothing else."""
+    p = of_size(size, 51)
+    odd = [0, 5, p.T - 1]
+    for j in odd:
+        p.Vd[:, :, j, 7 + j % 3] = what
+    p.upload().call()
+    p.Vd = np.where(np.isfinite(p.Vd), p.Vd, 0)
+    for b in range(p.B):
+        for h in range(p.H):
+            q, out, lse = p.q[b, h * p.G:h * p.G + p.G].transpose(1, 0, 2).reshape(p.T * p.G, 128).astype(np.float64), rows_of(p, p.out, b, h), rows_of(p, p.lse, b, h)
+            hit = np.zeros(out.shape, bool)
+            for j in odd:
+                hit[:, 7 + j % 3] |= np.repeat(p.bits[b][:, j], p.G)
+            assert hit.any() and not np.isfinite(out[hit]).any()
+            o, z, off, off_z = plain.attend(q, p.keys(b, h)[0], SCALE)
+            some = np.isfinite(z)
+            assert np.all(np.abs(out - o)[~hit] <= off[~hit]) and np.all(np.abs(lse[some] - z[some]) <= off_z[some]) and np.array_equal(np.isneginf(lse), ~some)
+
+
+@pytest.mark.parametrize("B,H,G,T", [(24, 32, 2, 5), (33, 31, 2, 5), (32, 32, 2, 5), (25, 41, 2, 5), (16, 16, 10, 25), (5, 41, 10, 25)])
+def test_as_many_blocks_as_are_shared(B, H, G, T):
+    """768, 1023 and 1024 blocks are shared among 512 workgroups, four a thread where they are counted; 1025 and more have one each and need no workspace."""
+    p = Problem(B + T, B, H, G, T, L=100, C=5, user=20, ragged=True)
+    p.n[1] = 0
+    blocks = B * H * -(-G * T // 64)
+    p.upload()
+    assert (sq.workspace_bytes(p.shape, sq.SQ_CALL_TREE_ATTN_Q8) > 0) == (blocks <= 1024)
+    p.call()
+    p.check()

@@ -6,8 +6,8 @@
 namespace sq {
 
 // A draft's ancestors have smaller numbers, so a thread that walks up from its draft meets the words of its mask from the last to the
-// first, and holds one at a time.  16 drafts 1.7 us on the GPU, 64 trees of 256 (some 15 deep) 4.3: the walk, a read of LDS a step, and
-// the calling thread takes 5.4.
+// first, and holds one at a time.  16 drafts 1.8 us on the GPU, 64 trees of 256 (some 15 deep) 4.7: the walk, a read of LDS a step, and
+// the calling thread takes 5.2.
 __global__ __launch_bounds__(MAX_DRAFTS) void tree_prepare_kernel(TreeArgs a)
 {
     __shared__ int s_parent[MAX_DRAFTS];
@@ -46,8 +46,8 @@ hipError_t launch_tree_prepare(const TreeArgs &a, int B, hipStream_t s)
     return hipGetLastError();
 }
 
-// One wave per sequence: a lane holds every 64th draft and asks each step whether it is the next one; the lowest number wins.  16 drafts 1.8 us
-// on the GPU, 256 trees of 64 2.8; the calling thread takes 6.4.
+// One wave per sequence: a lane holds every 64th draft and asks each step whether it is the next one; the lowest number wins.  16 drafts 1.6 us
+// on the GPU, 256 trees of 64 3.0; the calling thread takes 6.2.
 template <int N>
 __global__ __launch_bounds__(64) void tree_accept_kernel(AcceptArgs a)
 {
@@ -99,7 +99,7 @@ hipError_t launch_tree_accept(const AcceptArgs &a, int B, hipStream_t s)
 // are f16 and stand as they are, so every step is exact but the one rounding.
 //
 // What bounds it is the memory: four prompts of up to 8000 rows, 8 heads (160 MB) 29 us where the caches hold what the call before left, 33
-// where they do not, 4.8 to 5.5 TB/s; eight of 32 heads (1.3 GB) past the caches 208 (221 with them).  Up to six rows of each of 16 sequences: 4.4 us on
+// where they do not, 4.8 to 5.5 TB/s; eight of 32 heads (1.3 GB) past the caches 208 (221 with them).  Up to six rows of each of 16 sequences: 4.6 us on
 // the GPU, a chain of reads (the length, the page, the rows), the call itself takes the calling thread 5.5.
 // Tokens g, g + 16, .. of a page by 16 lanes each: N of them a thread.
 template <int N, bool STREAM>
@@ -174,8 +174,9 @@ hipError_t launch_cache_commit(CommitArgs a, int B, hipStream_t s)
 // a product.
 //
 // What bounds it is the memory.  Four sequences of up to 8192 tokens, 32 heads, pages of 16 (654 MB): 82 us on the pages that the call before read,
-// 98 on others, 6.7 TB/s (tokens a workgroup: 16 136, 32 98, 64 104, 128 112; 16 codes a lane, whose stores leave gaps in lines, 166; pages read past
-// the caches as well as rows written so 101 for 82; products in fp32 and a conversion, with the test of the scales, 102 for 100 on cold pages).  500 tokens of 8 heads: the calling thread, 5.4.
+// 98 to 100 on others, 6.6 TB/s (tokens a workgroup: 16 136, 32 98, 64 104, 128 112; 16 codes a lane, whose stores leave gaps in lines, 166; pages
+// read past the caches as well as rows written so 101 for 82; products in fp32 and a conversion, with the test of the scales, 102 for 100).
+// 500 tokens of 8 heads: 3.1 on the GPU, the calling thread takes 5.3.
 template <bool STREAM>
 __global__ __launch_bounds__(256) void cache_read_kernel(ReadArgs a)
 {

@@ -11,19 +11,23 @@
 //   O^T [128 x 16 TILES]    += V^T P^T  codes to f16 (exact), P rounded to f16
 //   l                       += p / value's scale                       (the unrounded p)
 // With the value's scale in the exponent P needs no factor: it is at most 2^15, and has its 11 bits down to 2^-22 of the largest.
+// (Rounded to f16 as in the prefill steps: as two bf16 numbers, as in decode, the second product would be made twice, where the units are the bound.  Against
+// 64 bits the results are off by 2.8e-4 of their size, 2.1e-4 of it the f16 output's own rounding.)
 // out = O / l, log-sum-exp = (M - 8 + log2 l) ln 2.
 // The sum takes p / scale from p, so that scales must not lie too far apart: those below 2^-40 count as 2^-40 (LEAST_SCALE; a value is then off by
 // less than 448 * 2^-40 < 2^-31, where f16 has steps of 2^-24), and above 2^40 is outside the contract.  Within 2^80 of one another a key drops
 // out of the sum (its p, or the factor by which a reference moves, below fp32's 2^-126) only where its weight is under 2^-46 of the largest: 2^23
 // such keys are one part in 2^23.  And no term overflows: 2^15 * 2^40 a key.
 //
-// What bounds it, and the two launches on the GPU (us; 8 K/V heads of 4 query heads):
-//   4 heads of 8 drafts, 4K + 128 keys, 1/4 kept     8.1 + 4.0   the launches, and a search, a prologue and a tile whose reads come from HBM
-//   1 sequence of 64 drafts, 32K + 1K keys, 1/8 kept     23.6 + 4.8   the same, and 2 to 3 tiles a wave: floor 4.2
-//   16 sequences of 13 drafts, 128K keys, 1/16 kept, 4K user's     102 + 7   the reads: 370 MB, at 5 TB/s while the loops run (72 us), the rest
-//     beginning and ending blocks.  (Sequences are not joined: the keys that any of them keeps are 280 MB.)
-//   a chain of 2048, the same 32K + 1K keys     ~300 + 10   the vector units (conversion, softmax) and the matrix units, which at two waves
+// What bounds it, and what a call takes, both launches, one call after the other (us; 8 K/V heads of 4 query heads):
+//   4 heads of 8 drafts, 4K + 128 keys, 1/4 kept     11.5   the launches, and a search, a prologue and a tile whose reads come from HBM
+//   1 sequence of 64 drafts, 32K + 512 keys, 1/8 kept     27.5   the same, and 2 to 3 tiles a wave: floor 4.2
+//   16 sequences of 13 drafts, 128K keys, 1/16 kept, 4K user's     98 to 102 by card   the reads: 370 MB, at 5 TB/s while the loops run (72 us), the
+//     rest beginning and ending blocks.  (Sequences are not joined: the keys that any of them keeps are 280 MB.)
+//   a chain of 2048, 32K + 1K keys, 1/8 kept     297   the vector units (conversion, softmax) and the matrix units, which at two waves
 //     a SIMD hardly overlap: 205 GFLOP at 690 TFLOP/s in all, 850 to 890 in the loop over codes, half as much in the loop over drafts
+//   the cache alone, 32K tokens of 64 drafts     68   34 GFLOP and 68 MB, the same units; 16 sequences of up to 4K of 13 drafts     44   106 MB
+// The merge is 4 to 7 of it, of the chain 10.
 // Tried there: three workgroups a CU at 32 rows 31.5 -> 37 us, one wave a SIMD 1.55 times the time, 48 / 32 rows of a long chain 303 -> 333 / 372,
 // raised or lowered wave priority 5 to 10 % slower either way.
 #include <algorithm>

@@ -30,7 +30,7 @@ def check(p):
             got_z = lse[b, h * p.G:h * p.G + p.G, :n].T.reshape(n * p.G)
             assert np.array_equal(np.isneginf(z), np.isneginf(got_z)), (b, h)
             ok = np.isfinite(z)
-            assert np.all(np.abs(got_z - z)[ok] <= off_z[ok]), (b, h, got_z[:4], z[:4])
+            assert np.all(np.abs(got_z[ok] - z[ok]) <= off_z[ok]), (b, h, got_z[:4], z[:4])
             near = np.abs(o) + off < 65504
             assert np.all(np.abs(got - o)[near] <= off[near] + OFF), (b, h)
 
@@ -194,3 +194,24 @@ def test_as_many_blocks_as_are_shared(B, H, G, T):
     assert (sq.workspace_bytes(p.shape, sq.SQ_CALL_TREE_ATTN_Q8) > 0) == (blocks <= 1024)
     p.call()
     p.check()
+
+
+@pytest.mark.parametrize("size", SIZES)
+def test_numbers_below_the_normal_ones_of_f16(size):
+    """Queries, drafts' keys and drafts' values of 2^-15 and less, with scales and sources that make them count."""
+    p = of_size(size, 52, L=0, C=0, mask=None, drafts=False)
+    p.q = (p.q * np.float16(2.0 ** -17)).astype(np.float16)
+    p.cks[:] = 2.0 ** 8                                         # (scores of some hundredths)
+    p.upload().call()
+    check(p)
+    assert np.ptp(p.lse.cpu().numpy()[0]) > 0.01                # (ln 50 for all rows, were they zeros)
+    p = of_size(size, 53, L=0, C=0, user=16)
+    p.held[:] = 0
+    p.bits[:] = np.tril(np.ones(p.bits.shape[1:], bool))
+    p.mask = plain.words(p.bits)
+    p.q = (p.q * np.float16(2.0 ** 9)).astype(np.float16)
+    p.Kd, p.Vd = ((x * np.float16(2.0 ** -s)).astype(np.float16) for x, s in ((p.Kd, 17), (p.Vd, 18)))
+    p.upload().call()
+    check(p)
+    out = np.abs(p.out.cpu().numpy().astype(np.float64))
+    assert 0 < out.max() < 2.0 ** -15

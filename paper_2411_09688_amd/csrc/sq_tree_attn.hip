@@ -11,8 +11,8 @@
 //   O^T [128 x 16 TILES]    += V^T P^T  codes to f16 (exact), P rounded to f16
 //   l                       += p / value's scale                       (the unrounded p)
 // With the value's scale in the exponent P needs no factor: it is at most 2^15, and has its 11 bits down to 2^-22 of the largest.
-// (Rounded to f16 as in the prefill steps: as two bf16 numbers, as in decode, the second product would be made twice, where the units are the bound.  Against
-// 64 bits the results are off by 2.8e-4 of their size, 2.1e-4 of it the f16 output's own rounding.)
+// (Rounded to f16 as in the prefill steps: as two bf16 numbers, as in decode, the second product would be made twice, where the units are the
+// bound.  Against 64 bits the results are off by 2.8e-4 of their size, 2.1e-4 of it the f16 output's own rounding.)
 // out = O / l, log-sum-exp = (M - 8 + log2 l) ln 2.
 // The sum takes p / scale from p, so that scales must not lie too far apart: those below 2^-40 count as 2^-40 (LEAST_SCALE; a value is then off by
 // less than 448 * 2^-40 < 2^-31, where f16 has steps of 2^-24), and above 2^40 is outside the contract.  Within 2^80 of one another a key drops
@@ -495,7 +495,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs /* see a
             };
             auto list_scales = [&](int buf) {
                 const int lane = lane_here();
-                // (a slot without a key: not looked at, but for this.  A comparison in fmaxf's place: 50 registers more in memory at 64 rows, chain 302 -> 337 us)
+                // (a slot without a key: not looked at, but for this.  A comparison in fmaxf's place keeps 50 more registers in memory at 64 rows:
+                // chain 302 -> 337 us)
                 const float v = seen_next >> lane & 1u ? fmaxf(vs, LEAST_SCALE) : 1.0f;
                 s_list[wave][buf].mul[lane] = ks * a.scale;
                 s_list[wave][buf].add[lane] = __builtin_amdgcn_logf(v);
